@@ -326,7 +326,8 @@ def work(case):
         n, w = case["seqs"] * case["steps"] * case["width"], case["seqs"] * case["width"]
         read = int(_lengths(case["seqs"], case["steps"]).sum()) * case["width"] if case["ragged"] else n
         if case["train"]:          # x, gate, y, dy in; dx, dgate out; y0, dyT in, dy0 out
-            return {"bytes": es * (4 * read + 2 * n) + 12 * w, "flops": 24 * read}
+            inputs = 4 if case["coupled"] else 3      # the uncoupled form's gradients do not depend on x
+            return {"bytes": es * (inputs * read + 2 * n) + 12 * w, "flops": 24 * read}
         return {"bytes": es * (2 * read + n) + 8 * w, "flops": 10 * read}
     n, w = case["rows"] * case["width"], case["width"]
     if case["op"] == "residual":
