@@ -292,6 +292,117 @@ mpode_status mpode_collect_profile(mpode_ctx* ctx, double* ms, long long* launch
 const char* mpode_status_string(mpode_status s);
 const char* mpode_last_error(const mpode_ctx* ctx);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------------------------
+ * Operators of sequence and residual networks around a block that the caller evaluates (the paper has no counterpart; its formats, its
+ * stored trajectory and its adjoint scaling carry over).  The velocities above are built in; a caller whose block is its own code takes
+ * the steps of Alg. 1 and Alg. 2 with these calls.  They need no context.  Conventions beyond those at the top of this file:
+ *   - Every call only queues kernels on `cuda_stream`: no allocation, no synchronisation, nothing kept between calls, so calls may be
+ *     captured into a CUDA graph and run at the same time.  All buffers live on the current device.
+ *   - Arguments are checked before anything is queued; mpode_operator_error returns the message of the last call of this host thread that failed.
+ *   - The low format is that of the block's tensors; states, adjoints, statistics, weights and weight gradients are float32.  Results are
+ *     rounded to the low format once, when written, and are the same bits in every run.
+ *   - Strides count elements and 0 means contiguous; channels lie side by side.  Any element-aligned pointer is taken; rows that are multiples
+ *     of 16 bytes (4 bytes in the recurrence) from pointers aligned like that are read and written in wider accesses.
+ *   - flag_dev (device word, or NULL) is set to 1 when a low-format value that was written is not finite, and left alone otherwise: the finiteness test of Alg. 2.
+ */
+const char* mpode_operator_error(void);
+
+/*
+ * Gated linear recurrence along a sequence.  With b = sigmoid(gate), per channel and for i = 0 .. length - 1, y_{-1} = y0:
+ *     coupled != 0 : y_i = y_{i-1} + b_i (x_i - y_{i-1}), the implicit Euler step of y' = lambda (x - y) with gate = log(h lambda), so that a
+ *                    grid's steps enter by adding log h_i to the gate;
+ *     coupled == 0 : y_i = (1 - b_i) y_{i-1} + x_i.
+ * The time loop of this linear equation runs as a scan in one pass over the data, split over the SMs where a batch has few channels.
+ * The state is float32 and never rounded; what is stored is Q16(y_i).
+ */
+typedef struct {
+    mpode_dtype low;              /* x, gate, y and their cotangents */
+    int n_seq, n_steps, width;    /* sequences, longest sequence, channels */
+    int coupled;
+    long long in_seq_stride, in_step_stride;   /* x, gate, dL_dx, dL_dgate: element (s, i, c) at s * in_seq_stride + i * in_step_stride + c */
+    long long out_seq_stride, out_step_stride; /* y, dL_dy; 0 = [n_seq][n_steps][width].  Rows must not overlap. */
+} mpode_recurrence_desc;
+
+/*
+ * y0_dev: fp32 [n_seq][width] or NULL (zero).  lengths_dev: int [n_seq] or NULL (all n_steps); values are clamped to 0 .. n_steps.  Elements of x,
+ * gate and y behind a sequence's length are neither read nor written.  yT_dev: NULL, or fp32 [n_seq][width], the state behind the last step (y0
+ * where the length is 0); it may be y0_dev.  y_dev may be x_dev.  n_steps = 1 with yT_dev = y0_dev is the form for serving token by token.
+ */
+mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
+                                      const float* y0_dev, const int* lengths_dev, void* y_dev, float* yT_dev);
+
+/*
+ * Backward pass from the stored trajectory y_dev (Alg. 2's reading: derivatives are taken at the stored states, y_{-1} = y0 in float32).
+ * dL_dy_dev: NULL (zero) or the cotangent of the stored y.  dL_dyT_dev: NULL (zero) or fp32, that of yT.  dL_dx_dev and dL_dgate_dev are written up to
+ * each sequence's length and left alone behind it; dL_dy0_dev may be NULL.  dL_dx_dev may be dL_dy_dev where the strides agree, dL_dgate_dev may be
+ * gate_dev, dL_dy0_dev may be dL_dyT_dev.  x_dev is not read when coupled == 0.
+ * All cotangents carry the same power-of-two scale, whatever it is.
+ */
+mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
+                                       const float* y0_dev, const int* lengths_dev, const void* y_dev, const void* dL_dy_dev,
+                                       const float* dL_dyT_dev, void* dL_dx_dev, void* dL_dgate_dev, float* dL_dy0_dev, unsigned* flag_dev);
+
+/*
+ * Residual step: one forward Euler step of the float32 state around the caller's block, with the norms before and after the block, its gate, its
+ * residual scale and dropout in one pass:
+ *     n = N_post(u),  y' = y + h * scale * drop(sigmoid(gate) * w_post * n),  z = Q16(w_pre * N_pre(y'))
+ * with u the output of the block that read the previous z, and z the input of the next block.  Without u the call is the norm in front of the first
+ * block (y' = y), without z the step behind the last one.
+ */
+typedef enum {
+    MPODE_NORM_NONE = 0,    /* v */
+    MPODE_NORM_RMS = 1,     /* v / sqrt(mean(v^2) + eps) over the row */
+    MPODE_NORM_MEANVAR = 2  /* the same of v - mean(v) */
+} mpode_norm;
+
+typedef struct {
+    mpode_dtype low;              /* u, gate, z and their cotangents */
+    int width;                    /* 1 .. 16384 */
+    mpode_norm post_norm, pre_norm;
+    float eps;                    /* > 0 */
+    float h;                      /* step size */
+    float p_drop;                 /* probability of a zero, rounded to a multiple of 2^-16 (the kept values' factor goes with the rounded one) */
+    unsigned site;                /* number of this dropout, see mpode_dropout */
+    long long ld_y, ld_u, ld_gate, ld_z; /* row lengths: y, y' and their adjoints; u and dL_du; gate and dL_dgate; z and dL_dz.  0 = width */
+} mpode_residual_desc;
+
+/*
+ * y_dev fp32 [rows][width]; u_dev, gate_dev low or NULL; w_post_dev, scale_dev, w_pre_dev fp32 [width] or NULL (ones); rng_dev as in mpode_dropout,
+ * NULL when p_drop is 0.  Out: y_out_dev fp32 (may be y_dev; may be NULL without u); z_dev low or NULL; stats_dev NULL, or fp32 [rows][4] (16-byte aligned): mean and reciprocal
+ * deviation of u, then of y' (0 and 1 where there is no norm, no u or no z), which the backward pass needs.  gate_dev may be a slice of the buffer that holds u.
+ */
+mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_stream, int rows, const float* y_dev, const void* u_dev,
+                                    const void* gate_dev, const float* w_post_dev, const float* scale_dev, const float* w_pre_dev,
+                                    const void* rng_dev, float* y_out_dev, void* z_dev, float* stats_dev);
+
+/*
+ * y_new_dev: the state behind the step, as written by the forward pass (read only with dL_dz_dev).  dL_dy_new_dev: NULL (zero) or fp32, the adjoint of y';
+ * dL_dz_dev: NULL (zero) or low, the cotangent of z.  With the adjoint scale S = 2^scale_exp of Alg. 2 (-100 .. 100): dL_dz_dev is read as S times the
+ * cotangent, dL_du_dev and dL_dgate_dev are written as Q16(S times theirs), everything in float32 is unscaled.  Out: dL_dy_dev fp32 (may be
+ * dL_dy_new_dev), dL_du_dev low (may be u_dev), dL_dgate_dev low (may be gate_dev), and the weights' gradients fp32 [width], each NULL or overwritten (added to when
+ * accumulate != 0).  Those need mpode_residual_workspace_bytes of device memory, 256-byte aligned, which holds nothing between calls; calls
+ * that overlap on the GPU, captured graphs among them, need a workspace each.
+ */
+size_t mpode_residual_workspace_bytes(const mpode_residual_desc* desc, int rows);
+mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda_stream, int rows, const float* y_new_dev, const void* u_dev,
+                                     const void* gate_dev, const float* w_post_dev, const float* scale_dev, const float* w_pre_dev,
+                                     const void* rng_dev, const float* stats_dev, const float* dL_dy_new_dev, const void* dL_dz_dev,
+                                     int scale_exp, float* dL_dy_dev, void* dL_du_dev, void* dL_dgate_dev, float* dL_dw_post_dev,
+                                     float* dL_dscale_dev, float* dL_dw_pre_dev, int accumulate, unsigned* flag_dev, void* workspace_dev,
+                                     size_t workspace_bytes);
+
+/*
+ * Dropout from a counter-based generator: out = 0 with probability p (rounded to a multiple of 2^-16), else x / (1 - p).  The mask is never stored: it is a
+ * function of rng_dev, site, row and column alone, so the same call on the cotangent is the backward pass, and Alg. 2's recompute meets the forward
+ * pass's mask again.  rng_dev: two 64-bit device words {seed, step}, read when the kernel runs (a replayed graph takes what they hold then).
+ * Element (r, c) is kept when 16 bits of the words Philox4x32-10(counter = {G mod 2^32, G / 2^32, step mod 2^32, site}, key = {seed mod 2^32,
+ * seed / 2^32}), G = r * ceil(width / 8) + c / 8, are at least round(65536 p): of word (c mod 8) / 2, the low half for even c, the high half for odd.
+ * Dropped values are zero whatever x holds there.  out_dev may be x_dev where the strides agree.
+ */
+mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long long rows, int width, const void* x_dev, long long ld_x, void* out_dev,
+                           long long ld_out, float p, const void* rng_dev, unsigned site, unsigned* flag_dev);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,7 @@ DTYPES = {"f32": 0, "bf16": 1, "f16": 2}
 SCALINGS = {"none": 0, "none_safe": 1, "dynamic": 2}
 ACTS = {"none": 0, "tanh": 1, "softplus": 2, "relu": 3}
 KINDS = {"mlp": 0, "linear": 0, "conv": 1, "cnf": 2, "scalar_poly": 3, "parabolic": 4, "cnf_hyper": 5}
+NORMS = {"none": 0, "rms": 1, "meanvar": 2}
 NO_OVERRIDE = -2147483648
 
 EXPORTS = [
@@ -29,7 +30,8 @@ EXPORTS = [
     "mpode_state_width", "mpode_workspace_bytes", "mpode_trajectory_bytes", "mpode_forward", "mpode_backward",
     "mpode_io_bytes", "mpode_forward_host", "mpode_backward_host", "mpode_get_stats", "mpode_status_string",
     "mpode_last_error", "mpode_set_profiling", "mpode_collect_profile", "mpode_backward_static_workspace",
-    "mpode_debug_waits", "mpode_backward_ex",
+    "mpode_debug_waits", "mpode_backward_ex", "mpode_operator_error", "mpode_recurrence_forward", "mpode_recurrence_backward",
+    "mpode_residual_workspace_bytes", "mpode_residual_forward", "mpode_residual_backward", "mpode_dropout",
 ]
 STATIC_WORKSPACE_BYTES = 32 * 1024 * 1024
 
@@ -59,6 +61,18 @@ class Stats(C.Structure):
     _fields_ = [("kernel_launches", C.c_longlong), ("retries", C.c_longlong), ("host_syncs", C.c_longlong),
                 ("tc_contractions", C.c_longlong), ("simt_contractions", C.c_longlong), ("fused_launches", C.c_longlong),
                 ("whole_solve_launches", C.c_longlong), ("step_waits", C.c_longlong)]
+
+
+class RecurrenceDesc(C.Structure):
+    _fields_ = [("low", C.c_int), ("n_seq", C.c_int), ("n_steps", C.c_int), ("width", C.c_int), ("coupled", C.c_int),
+                ("in_seq_stride", C.c_longlong), ("in_step_stride", C.c_longlong), ("out_seq_stride", C.c_longlong),
+                ("out_step_stride", C.c_longlong)]
+
+
+class ResidualDesc(C.Structure):
+    _fields_ = [("low", C.c_int), ("width", C.c_int), ("post_norm", C.c_int), ("pre_norm", C.c_int), ("eps", C.c_float), ("h", C.c_float),
+                ("p_drop", C.c_float), ("site", C.c_uint), ("ld_y", C.c_longlong), ("ld_u", C.c_longlong), ("ld_gate", C.c_longlong),
+                ("ld_z", C.c_longlong)]
 
 
 _lib = None
@@ -112,6 +126,20 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.mpode_status_string.restype = C.c_char_p
     lib.mpode_last_error.argtypes = [vp]
     lib.mpode_last_error.restype = C.c_char_p
+    lib.mpode_operator_error.argtypes = []
+    lib.mpode_operator_error.restype = C.c_char_p
+    lib.mpode_recurrence_forward.argtypes = [C.POINTER(RecurrenceDesc)] + [vp] * 7
+    lib.mpode_recurrence_forward.restype = i32
+    lib.mpode_recurrence_backward.argtypes = [C.POINTER(RecurrenceDesc)] + [vp] * 12
+    lib.mpode_recurrence_backward.restype = i32
+    lib.mpode_residual_workspace_bytes.argtypes = [C.POINTER(ResidualDesc), i32]
+    lib.mpode_residual_workspace_bytes.restype = sz
+    lib.mpode_residual_forward.argtypes = [C.POINTER(ResidualDesc), vp, i32] + [vp] * 10
+    lib.mpode_residual_forward.restype = i32
+    lib.mpode_residual_backward.argtypes = [C.POINTER(ResidualDesc), vp, i32] + [vp] * 10 + [i32] + [vp] * 6 + [i32, vp, vp, sz]
+    lib.mpode_residual_backward.restype = i32
+    lib.mpode_dropout.argtypes = [i32, vp, C.c_longlong, i32, vp, C.c_longlong, vp, C.c_longlong, C.c_float, vp, C.c_uint, vp]
+    lib.mpode_dropout.restype = i32
     _lib = lib
     return lib
 
@@ -343,3 +371,258 @@ class Context:
     def debug_waits(self, wait_limit_ns: int = 0, starve_forward: bool = False):
         """Test hook of the bounded device-side waits (see mpode_debug_waits)."""
         self.lib.mpode_debug_waits(self.h, int(wait_limit_ns), 1 if starve_forward else 0)
+
+
+# ---- operators of sequence and residual networks (mpode_recurrence_*, mpode_residual_*, mpode_dropout).  They need no Context: results go to new
+# tensors or to the caller's, on the current stream of the inputs' device.
+def _refuse(message: str):
+    raise MpodeError(ERR_INVALID_ARG, message)
+
+
+def _operator_check(st: int):
+    if st != OK:
+        lib = load_library()
+        raise MpodeError(st, lib.mpode_operator_error().decode() or lib.mpode_status_string(st).decode())
+
+
+def _low_of(t) -> int:
+    low = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}.get(str(t.dtype))
+    if low is None:
+        _refuse("dtype %s is not one of float32, bfloat16, float16" % t.dtype)
+    return low
+
+
+def _on_device(first, *others):
+    """All tensors on the CUDA device of the first one; returns (device guard, raw stream)."""
+    import torch
+    if not first.is_cuda:
+        _refuse("the tensors have to be on a CUDA device")
+    for t in others:
+        if t is not None and t.device != first.device:
+            _refuse("tensors on %s and %s" % (first.device, t.device))
+    return torch.cuda.device(first.device), int(torch.cuda.current_stream(first.device).cuda_stream)
+
+
+def _expect(name: str, t, shape, dtype):
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous()):
+        _refuse("%s has to be a contiguous %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+
+
+def _layout(name: str, t, shape, dtype):
+    """(sequence stride, step stride) of a [n_seq, n_steps, width] tensor whose channels lie side by side; 0 where a dimension has one entry."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        _refuse("%s has to be a %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if shape[2] > 1 and t.stride(2) != 1:
+        _refuse("the channels of %s have to lie side by side" % name)
+    out = tuple(t.stride(k) if shape[k] > 1 else 0 for k in (0, 1))
+    if any(s == 0 and shape[k] > 1 for k, s in enumerate(out)):
+        _refuse("%s is broadcast along a dimension" % name)
+    return out
+
+
+def _same_layout(name: str, t, shape, dtype, layout):
+    if t is not None and _layout(name, t, shape, dtype) != layout:
+        _refuse("%s has to have the strides %s" % (name, layout))
+
+
+def _like(t, fill_zero: bool):
+    """A tensor of the strides of t (a slice's gaps included)."""
+    import torch
+    out = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
+    return out.zero_() if fill_zero else out
+
+
+def _recurrence_desc(x, gate, coupled, out_layout=(0, 0)):
+    if x.dim() != 3:
+        _refuse("x has to be [n_seq, n_steps, width]")
+    shape = tuple(x.shape)
+    layout = _layout("x", x, shape, x.dtype)
+    _same_layout("gate", gate, shape, x.dtype, layout)
+    d = RecurrenceDesc(_low_of(x), shape[0], shape[1], shape[2], 1 if coupled else 0, layout[0], layout[1], out_layout[0], out_layout[1])
+    # a dimension of one entry has no stride; the other one's default would not know of a gap
+    if d.in_step_stride == 0:
+        d.in_step_stride = shape[2]
+    if d.in_seq_stride == 0:
+        d.in_seq_stride = max(shape[2], 1)
+    if d.out_step_stride == 0:
+        d.out_step_stride = shape[2]
+    if d.out_seq_stride == 0:
+        d.out_seq_stride = max(shape[2], 1)
+    return d, shape, layout
+
+
+def recurrence_forward(x, gate, y0=None, lengths=None, coupled: bool = True, y=None, yT=None):
+    """mpode_recurrence_forward on x, gate [n_seq, n_steps, width] (any strides with the channels side by side, the same for both).
+    Returns (y, yT): the stored trajectory (zero behind a sequence's length when allocated here, left alone there when given) and the float32 state
+    behind the last step.  yT may be y0."""
+    import torch
+    if y is None:
+        # time-major inputs get a time-major trajectory
+        n, T, w = x.shape if x.dim() == 3 else (0, 0, 0)
+        new = torch.zeros if lengths is not None else torch.empty
+        if n > 1 and T > 1 and x.stride(0) < x.stride(1):
+            y = new((T, n, w), dtype=x.dtype, device=x.device).transpose(0, 1)
+        else:
+            y = new((n, T, w), dtype=x.dtype, device=x.device)
+    d, shape, _ = _recurrence_desc(x, gate, coupled, _layout("y", y, tuple(x.shape), x.dtype) if x.dim() == 3 else (0, 0))
+    if yT is None:
+        yT = torch.empty((shape[0], shape[2]), dtype=torch.float32, device=x.device)
+    _expect("y0", y0, (shape[0], shape[2]), torch.float32)
+    _expect("yT", yT, (shape[0], shape[2]), torch.float32)
+    _expect("lengths", lengths, (shape[0],), torch.int32)
+    guard, stream = _on_device(x, gate, y0, lengths, y, yT)
+    with guard:
+        _operator_check(load_library().mpode_recurrence_forward(C.byref(d), stream, _ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(yT)))
+    return y, yT
+
+
+def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, coupled: bool = True, dL_dx=None, dL_dgate=None, dL_dy0=None, flag=None):
+    """mpode_recurrence_backward from the stored trajectory y.  dL_dy (or None) has the strides of y, dL_dx and dL_dgate those of x.
+    Returns (dL_dx, dL_dgate, dL_dy0); the first two are zero behind a sequence's length when allocated here, left alone there when given.
+    flag: int32 tensor of one element, set to 1 when a low-format gradient is not finite."""
+    import torch
+    if x.dim() != 3:
+        _refuse("x has to be [n_seq, n_steps, width]")
+    out_layout = _layout("y", y, tuple(x.shape), x.dtype)
+    d, shape, layout = _recurrence_desc(x, gate, coupled, out_layout)
+    _same_layout("dL_dy", dL_dy, shape, x.dtype, out_layout)
+    if dL_dx is None:
+        dL_dx = _like(x, lengths is not None)
+    if dL_dgate is None:
+        dL_dgate = _like(x, lengths is not None)
+    if dL_dy0 is None:
+        dL_dy0 = torch.empty((shape[0], shape[2]), dtype=torch.float32, device=x.device)
+    _same_layout("dL_dx", dL_dx, shape, x.dtype, layout)
+    _same_layout("dL_dgate", dL_dgate, shape, x.dtype, layout)
+    for name, t in (("y0", y0), ("dL_dyT", dL_dyT), ("dL_dy0", dL_dy0)):
+        _expect(name, t, (shape[0], shape[2]), torch.float32)
+    _expect("lengths", lengths, (shape[0],), torch.int32)
+    _expect("flag", flag, (1,), torch.int32)
+    guard, stream = _on_device(x, gate, y, dL_dy, dL_dyT, y0, lengths, dL_dx, dL_dgate, dL_dy0, flag)
+    with guard:
+        _operator_check(load_library().mpode_recurrence_backward(C.byref(d), stream, _ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(dL_dy),
+                                                                 _ptr(dL_dyT), _ptr(dL_dx), _ptr(dL_dgate), _ptr(dL_dy0), _ptr(flag)))
+    return dL_dx, dL_dgate, dL_dy0
+
+
+def _rows(name: str, t, shape, dtype) -> int:
+    """Row length of a [rows, width] tensor whose columns lie side by side."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        _refuse("%s has to be a %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if shape[1] > 1 and t.stride(1) != 1:
+        _refuse("the columns of %s have to lie side by side" % name)
+    if shape[0] <= 1:
+        return shape[1]
+    if t.stride(0) < shape[1]:
+        _refuse("the rows of %s overlap" % name)
+    return t.stride(0)
+
+
+def _same_rows(shape, dtype, *named) -> int:
+    lds = {_rows(name, t, shape, dtype) for name, t in named if t is not None}
+    if len(lds) > 1:
+        _refuse("%s have to have the same row length" % ", ".join(name for name, t in named if t is not None))
+    return lds.pop() if lds else 0
+
+
+class ResidualStep:
+    """mpode_residual_forward / mpode_residual_backward with a fixed width and settings.  The object holds the settings only: nothing of one call is
+    kept for the next, and a call's scratch memory comes from torch's allocator, so that calls on several streams do not meet in it."""
+
+    def __init__(self, width: int, low: str = "bf16", post_norm: str = "rms", pre_norm: str = "rms", eps: float = 1e-5, h: float = 1.0,
+                 p: float = 0.0, site: int = 0):
+        import torch
+        self.width, self.p, self.h, self.eps, self.site = int(width), float(p), float(h), float(eps), int(site)
+        self.low, self.post_norm, self.pre_norm = DTYPES[low], NORMS[post_norm], NORMS[pre_norm]
+        self.low_torch = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[low]
+
+    def _desc(self, ld_y, ld_u, ld_gate, ld_z):
+        return ResidualDesc(self.low, self.width, self.post_norm, self.pre_norm, self.eps, self.h, self.p, self.site, ld_y, ld_u, ld_gate, ld_z)
+
+    def _common(self, y, weights, rng):
+        import torch
+        if y.dim() != 2:
+            _refuse("the state has to be [rows, width]")
+        for name, w in weights:
+            _expect(name, w, (self.width,), torch.float32)
+        _expect("rng", rng, (2,), torch.int64)
+        return (y.shape[0], self.width)
+
+    def forward(self, y, u=None, gate=None, w_post=None, scale=None, w_pre=None, rng=None, y_out=None, z=None, want_z: bool = True):
+        """Returns (y', z, stats): the state behind the step (y itself without u), the next block's input (None with want_z=False) and the statistics
+        that backward needs.  y_out may be y."""
+        import torch
+        shape = self._common(y, (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)), rng)
+        if u is not None and y_out is None:
+            y_out = torch.empty_strided(y.shape, y.stride(), dtype=y.dtype, device=y.device)
+        if want_z and z is None:
+            z = torch.empty(shape, dtype=self.low_torch, device=y.device)
+        stats = torch.empty((shape[0], 4), dtype=torch.float32, device=y.device)
+        d = self._desc(_same_rows(shape, torch.float32, ("y", y), ("y_out", y_out)), _rows("u", u, shape, self.low_torch),
+                       _rows("gate", gate, shape, self.low_torch), _rows("z", z, shape, self.low_torch))
+        guard, stream = _on_device(y, u, gate, w_post, scale, w_pre, rng, y_out, z)
+        with guard:
+            _operator_check(load_library().mpode_residual_forward(C.byref(d), stream, shape[0], _ptr(y), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale),
+                                                                  _ptr(w_pre), _ptr(rng), _ptr(y_out), _ptr(z), _ptr(stats)))
+        return (y if y_out is None else y_out), z, stats
+
+    def backward(self, y_new, u=None, stats=None, dL_dy=None, dL_dz=None, gate=None, w_post=None, scale=None, w_pre=None, rng=None, scale_exp: int = 0,
+                 accumulate_into: Optional[dict] = None, want_weights: bool = True, flag=None):
+        """dL_dy: adjoint of y' (float32), dL_dz: cotangent of z (low format, times 2^scale_exp).  Returns a dict with "dy" (adjoint of y), "du" and "dgate" (low
+        format, times 2^scale_exp; None without u, gate) and the gradients "dw_post", "dscale", "dw_pre" of the weights that were given (added to the
+        tensors of that name in accumulate_into when given).  flag: int32 tensor of one element, set to 1 when du or dgate is not finite."""
+        import torch
+        shape = self._common(y_new, (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)), rng)
+        _expect("stats", stats, (shape[0], 4), torch.float32)
+        _expect("flag", flag, (1,), torch.int32)
+        out = dict(dy=torch.empty_strided(y_new.shape, y_new.stride(), dtype=torch.float32, device=y_new.device),
+                   du=None if u is None else torch.empty_strided(u.shape, u.stride(), dtype=u.dtype, device=u.device),
+                   dgate=None if gate is None else torch.empty_strided(gate.shape, gate.stride(), dtype=gate.dtype, device=gate.device))
+        for key, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
+            out[key] = None
+            if want_weights and w is not None:
+                out[key] = accumulate_into[key] if accumulate_into is not None else torch.empty(self.width, dtype=torch.float32, device=y_new.device)
+                _expect(key, out[key], (self.width,), torch.float32)
+        grads = [out[k] for k in ("dw_post", "dscale", "dw_pre")]
+        d = self._desc(_same_rows(shape, torch.float32, ("y_new", y_new), ("dL_dy", dL_dy), ("dy", out["dy"])),
+                       _same_rows(shape, self.low_torch, ("u", u), ("du", out["du"])), _same_rows(shape, self.low_torch, ("gate", gate), ("dgate", out["dgate"])),
+                       _rows("dL_dz", dL_dz, shape, self.low_torch))
+        lib = load_library()
+        guard, stream = _on_device(y_new, u, stats, dL_dy, dL_dz, gate, w_post, scale, w_pre, rng, flag, *grads)
+        with guard:
+            ws, nbytes = None, 0
+            if any(g is not None for g in grads) and shape[0] > 0:
+                nbytes = int(lib.mpode_residual_workspace_bytes(C.byref(d), shape[0]))
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=y_new.device)
+            _operator_check(lib.mpode_residual_backward(C.byref(d), stream, shape[0], _ptr(y_new), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre),
+                                                        _ptr(rng), _ptr(stats), _ptr(dL_dy), _ptr(dL_dz), int(scale_exp), _ptr(out["dy"]), _ptr(out["du"]),
+                                                        _ptr(out["dgate"]), *[_ptr(g) for g in grads], 1 if accumulate_into is not None else 0, _ptr(flag),
+                                                        _ptr(ws), nbytes))
+        return out
+
+
+def dropout(x, p: float, rng, site: int = 0, out=None, flag=None):
+    """mpode_dropout on the rows of x [..., width] (2-D with any row length, or contiguous); on a cotangent it is the backward pass.
+    rng: int64 tensor {seed, step} on the device.  out may be x."""
+    import torch
+    if x.dim() == 0:
+        _refuse("x has to have rows")
+    shape = (x.numel() // max(x.shape[-1], 1), x.shape[-1])
+    if x.dim() != 2 and not x.is_contiguous():
+        _refuse("x has to be contiguous, or 2-D with its columns side by side")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if tuple(out.shape) != tuple(x.shape) or (out.dim() != 2 and not out.is_contiguous()):
+        _refuse("out has to have the shape of x, and be contiguous or 2-D")
+    low = _low_of(x)
+    _expect("rng", rng, (2,), torch.int64)
+    _expect("flag", flag, (1,), torch.int32)
+    rows_x = _rows("x", x if x.dim() == 2 else x.view(shape), shape, x.dtype)
+    rows_out = _rows("out", out if out.dim() == 2 else out.view(shape), shape, x.dtype)
+    guard, stream = _on_device(x, rng, out, flag)
+    with guard:
+        _operator_check(load_library().mpode_dropout(low, stream, shape[0], shape[1], _ptr(x), rows_x, _ptr(out), rows_out, float(p), _ptr(rng), int(site),
+                                                     _ptr(flag)))
+    return out

@@ -1,0 +1,66 @@
+// Dropout whose mask is never stored: the call that is given the cotangent with the same {seed, step}, site and shape is its backward pass,
+// and a recompute of the stages (Alg. 2) finds the forward pass's mask again.
+#include "operators.h"
+#include "philox.cuh"
+#include "rows.cuh"
+
+namespace mpode {
+namespace {
+
+struct DropArgs {
+    const void* x; void* out;
+    long long ld_x, ld_out, groups;      // groups of eight columns in all rows
+    int width, groups_row;
+    Dropout d;
+    unsigned* flag;
+};
+
+// One thread, one group of eight columns at a time: 16-byte loads where the layout allows, bound by those bytes and the generator alike
+template <typename T, bool VEC> __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs p) {
+    const uint64_t seed = p.d.rng[0], step = p.d.rng[1];
+    bool bad = false;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < p.groups; i += (long long)gridDim.x * 256) {
+        const long long row = i / p.groups_row;
+        const int col = (int)(i - row * p.groups_row) * 8, n = min(8, p.width - col);
+        float f[8];
+        load8<T, VEC>((const T*)p.x + row * p.ld_x + col, n, f);
+        const uint32_t keep = keep_bits((uint64_t)i, seed, step, p.d.site, p.d.threshold);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (keep >> j) & 1u ? f[j] * p.d.scale : 0.f;
+        bad |= store8<T, VEC>((T*)p.out + row * p.ld_out + col, n, f);
+    }
+    warp_flag_or(p.flag, bad);
+}
+
+}  // namespace
+}  // namespace mpode
+
+using namespace mpode;
+
+extern "C" mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long long rows, int width, const void* x_dev, long long ld_x, void* out_dev,
+                                      long long ld_out, float p, const void* rng_dev, unsigned site, unsigned* flag_dev) {
+    if (!known_dtype(low)) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: unknown format %d", (int)low);
+    if (rows < 0 || width < 1) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: %lld rows of width %d", rows, width);
+    if (!(p >= 0.f && p <= 1.f)) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: p = %g is not a probability", (double)p);
+    if (ld_x == 0) ld_x = width;
+    if (ld_out == 0) ld_out = width;
+    if (ld_x < width || ld_out < width) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: rows overlap");
+    if (rows == 0) return MPODE_OK;
+    if (rows > (1ll << 40)) return operator_fail(MPODE_ERR_UNSUPPORTED, "mpode_dropout: %lld rows", rows);
+    if (!x_dev || !out_dev || !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: null pointer argument");
+    const size_t es = low_size(low);
+    if (misaligned(x_dev, es) || misaligned(out_dev, es) || misaligned(rng_dev, 8) || misaligned(flag_dev, 4))
+        return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: a pointer is not aligned to its elements");
+    DropArgs a{x_dev, out_dev, ld_x, ld_out, 0, width, (width + 7) / 8, make_dropout(p, rng_dev, site), flag_dev};
+    a.groups = rows * a.groups_row;
+    const bool vec = width % 8 == 0 && !misaligned(x_dev, 16) && !misaligned(out_dev, 16) && (ld_x * es) % 16 == 0 && (ld_out * es) % 16 == 0;
+    const long long blocks = (a.groups + 255) / 256, most = 148 * 8;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    with_low(low, [&](auto t) {
+        using T = decltype(t);
+        if (vec) dropout_kernel<T, true><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+        else dropout_kernel<T, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+        return cudaSuccess;
+    });
+    return operator_launched(cudaGetLastError(), "mpode_dropout");
+}
