@@ -9,13 +9,16 @@
 // then every warp runs its steps again from the state in front of them: the data is read once and written once, nothing is kept in device
 // memory and no block waits for another but at the cluster's barrier.
 //
-// Precision: the smaller one of a and b is formed without cancellation and kept with a sign that says which one it is (s = b >= +0, or s = -a <= -0),
-// so that memories of a million steps (b = 1e-6) and resets (a = 0) are both exact to rounding.  A composed map keeps the product A of the a
-// and, for slow channels, its complement C = 1 - A, which a product of numbers near one would lose.
+// Precision: b is formed with a relative error (no cancellation for g << 0), and every decay is written y - b y in one rounding, so that memories of
+// a million steps (b = 1e-6) decay at the right rate, where a rounded a = 1 - b would not, and b = 1 forgets everything, exactly.  For the same reason a
+// composed map is kept as y -> y - C y + u with C = 1 - A.
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <math.h>
+
 #include "operators.h"
+#include "rows.cuh"
 
 namespace mpode {
 namespace {
@@ -32,33 +35,44 @@ struct RecArgs {
     int n_seq, n_steps, width;
 };
 
-// one 32-bit word of channels (two 16-bit ones or a float), or a single 16-bit channel where widths or addresses are odd
+// V channels of a row as one access: two (a 32-bit word, or 64 bits of float32), or one where widths or addresses are odd
 template <typename T, int V> struct Word;
 template <> struct Word<float, 1> {
     using type = float;
-    static __device__ __forceinline__ void get(float w, float* f) { f[0] = w; }
-    static __device__ __forceinline__ float put(const float* f) { return f[0]; }
+    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = w; }
+    static __device__ __forceinline__ type put(const float (&f)[1]) { return f[0]; }
+    static __device__ __forceinline__ type negate(type w) { return -w; }
+};
+template <> struct Word<float, 2> {
+    using type = float2;
+    static __device__ __forceinline__ void get(type w, float (&f)[2]) { f[0] = w.x; f[1] = w.y; }
+    static __device__ __forceinline__ type put(const float (&f)[2]) { return make_float2(f[0], f[1]); }
+    static __device__ __forceinline__ type negate(type w) { return make_float2(-w.x, -w.y); }
 };
 template <> struct Word<__nv_bfloat16, 1> {
     using type = __nv_bfloat16;
-    static __device__ __forceinline__ void get(type w, float* f) { f[0] = __bfloat162float(w); }
-    static __device__ __forceinline__ type put(const float* f) { return __float2bfloat16_rn(f[0]); }
+    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = __bfloat162float(w); }
+    static __device__ __forceinline__ type put(const float (&f)[1]) { return __float2bfloat16_rn(f[0]); }
+    static __device__ __forceinline__ type negate(type w) { return __hneg(w); }
 };
 template <> struct Word<__half, 1> {
     using type = __half;
-    static __device__ __forceinline__ void get(type w, float* f) { f[0] = __half2float(w); }
-    static __device__ __forceinline__ type put(const float* f) { return __float2half_rn(f[0]); }
+    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = __half2float(w); }
+    static __device__ __forceinline__ type put(const float (&f)[1]) { return __float2half_rn(f[0]); }
+    static __device__ __forceinline__ type negate(type w) { return __hneg(w); }
 };
-template <> struct Word<__nv_bfloat16, 2> {
-    using type = __nv_bfloat162;
-    static __device__ __forceinline__ void get(type w, float* f) { float2 t = __bfloat1622float2(w); f[0] = t.x; f[1] = t.y; }
-    static __device__ __forceinline__ type put(const float* f) { return __floats2bfloat162_rn(f[0], f[1]); }
+template <typename T> struct Word<T, 2> {
+    using type = uint32_t;
+    static __device__ __forceinline__ void get(type w, float (&f)[2]) { const float2 t = Pair<T>::get(w); f[0] = t.x; f[1] = t.y; }
+    static __device__ __forceinline__ type put(const float (&f)[2]) { return Pair<T>::put(f[0], f[1]); }
+    static __device__ __forceinline__ type negate(type w) { return w ^ 0x80008000u; }
 };
-template <> struct Word<__half, 2> {
-    using type = __half2;
-    static __device__ __forceinline__ void get(type w, float* f) { float2 t = __half22float2(w); f[0] = t.x; f[1] = t.y; }
-    static __device__ __forceinline__ type put(const float* f) { return __floats2half2_rn(f[0], f[1]); }
-};
+template <typename T, int V> __device__ __forceinline__ typename Word<T, V>::type word_of(float v) {
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = v;
+    return Word<T, V>::put(f);
+}
 template <typename T, int V> __device__ __forceinline__ bool word_nonfinite(typename Word<T, V>::type w) {
     float f[V];
     Word<T, V>::get(w, f);
@@ -68,21 +82,70 @@ template <typename T, int V> __device__ __forceinline__ bool word_nonfinite(type
     return bad;
 }
 
-// s = sigmoid(g) where that is at most a half, else -(1 - sigmoid(g)); the sign bit tells the two apart even at zero
-__device__ __forceinline__ float signed_gate(float g) {
-    const float e = expf(-fabsf(g));
-    const float small = __fdividef(e, 1.f + e);
-    return copysignf(small, -g);
-}
-__device__ __forceinline__ bool resets(float s) { return (int)__float_as_uint(s) < 0; }     // a is the smaller one
+// a b + c and a + b on all channels of a lane; two of them are one instruction
+template <int V> struct Ops {
+    static __device__ __forceinline__ void fma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
+        if constexpr (V == 2) {
+            asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]), "f"(c[0]), "f"(c[1]));
+        } else d[0] = fmaf(a[0], b[0], c[0]);
+    }
+    static __device__ __forceinline__ void add(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+        if constexpr (V == 2) {
+            asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+        } else d[0] = a[0] + b[0];
+    }
+    static __device__ __forceinline__ void mul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+        if constexpr (V == 2) {
+            asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+        } else d[0] = a[0] * b[0];
+    }
+};
 
-template <bool COUPLED> __device__ __forceinline__ float step_forward(float s, float x, float y) {
-    if (COUPLED) return fmaf(s, x - y, resets(s) ? x : y);
-    return fmaf(-s, y, (resets(s) ? 0.f : y) + x);
+// -sigmoid(g) = -b and the slope b (1 - b), which is e b^2 with e = exp(-g).  16-bit gates: the device's approximate power and quotient (2^-22
+// relative, and the argument's rounding adds |g| 2^-24), which cost 5 instructions where the accurate ones of float32 cost 15; the exponent is
+// kept below 2^126, so that e b^2 is finite: b is 1e-38 instead of less, which no float32 state feels.
+template <typename T> __device__ __forceinline__ void negated_gate(float g, float& nb, float& slope) {
+    float e;
+    if constexpr (sizeof(T) == 4) {
+        e = expf(-g);
+        const float b = __fdividef(1.f, 1.f + e);
+        nb = -b;
+        slope = b * (e > 1.f ? 1.f - b : e * b);
+    } else {
+        asm("min.NaN.f32 %0, %1, %2;" : "=f"(e) : "f"(g * -1.4426950408889634f), "f"(126.f));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb) : "f"(-1.f - e));
+        slope = e * nb * nb;
+    }
 }
-__device__ __forceinline__ float decay(float s, float l) { return fmaf(-s, l, resets(s) ? 0.f : l); }     // a l
 
-// y -> A y + u, C = 1 - A
+// one step, nb = -b; x is negated when coupled
+template <bool COUPLED, int V> __device__ __forceinline__ void step_forward(float (&y)[V], const float (&nb)[V], const float (&x)[V]) {
+    float kept[V];
+    Ops<V>::fma(kept, nb, y, y);
+    if constexpr (COUPLED) Ops<V>::fma(y, nb, x, kept);
+    else Ops<V>::add(y, kept, x);
+}
+// The composed map y -> A y + u of some steps, C = 1 - A: A exact to its last bits where it is small (a reset leaves A = 0), C where the steps
+// forget little.  Kept per lane as A, -C and u.
+template <int V> struct Map {
+    float A[V], nC[V], u[V];
+    __device__ __forceinline__ Map() {
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.f; nC[v] = 0.f; u[v] = 0.f; }
+    }
+    __device__ __forceinline__ void decay(const float (&nb)[V]) {
+        float one[V], left[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) one[v] = 1.f;
+        Ops<V>::fma(A, nb, A, A);
+        Ops<V>::add(left, one, nC);
+        Ops<V>::fma(nC, nb, left, nC);
+    }
+};
 struct Affine { float A, C, u; };
 __device__ __forceinline__ float apply(const Affine& m, float y) { return (m.A < 0.5f ? m.A * y : fmaf(-m.C, y, y)) + m.u; }
 // first m, then n
@@ -112,14 +175,14 @@ template <int V> __device__ __forceinline__ Affine fetch(const float (&t)[3][32 
 
 // The state in front of this warp's steps, from the state in front of all of this round's steps (`carry`, replaced by the one behind them).
 // Called by all threads of the cluster with the same number of blocks.
-template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, int set, const Affine (&own)[V], float (&carry)[V], float (&start)[V],
+template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, int set, const Map<V>& own, float (&carry)[V], float (&start)[V],
                                                           int blocks, int rank) {
     const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        ex.warp[set][warp][0][v * 32 + lane] = own[v].A;
-        ex.warp[set][warp][1][v * 32 + lane] = own[v].C;
-        ex.warp[set][warp][2][v * 32 + lane] = own[v].u;
+        ex.warp[set][warp][0][v * 32 + lane] = own.A[v];
+        ex.warp[set][warp][1][v * 32 + lane] = -own.nC[v];
+        ex.warp[set][warp][2][v * 32 + lane] = own.u[v];
     }
     __syncthreads();
     if (blocks == 1) {
@@ -176,6 +239,23 @@ template <int V> __device__ __forceinline__ Place place(const RecArgs& p, int bl
     return q;
 }
 
+// A warp's tile of one array: L steps of V channels a lane, from step t0 on (step: the stride; negative backwards in time), `n` of which exist; the
+// others hold `fill`
+template <typename T, int V, int L> __device__ __forceinline__ void load_tile(typename Word<T, V>::type (&w)[L], const T* p, long long step, int n, float fill) {
+    using word = typename Word<T, V>::type;
+    if (n >= L) {
+#pragma unroll
+        for (int i = 0; i < L; ++i, p += step) w[i] = *(const word*)p;
+    } else {
+        const word none = word_of<T, V>(fill);
+#pragma unroll
+        for (int i = 0; i < L; ++i, p += step) {
+            w[i] = none;
+            if (i < n) w[i] = *(const word*)p;
+        }
+    }
+}
+
 template <typename T, int V, bool COUPLED, int L>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const int blocks) {
     using W = Word<T, V>;
@@ -191,49 +271,52 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
     float carry[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = p.y0 != nullptr && q.on ? p.y0[(long long)q.seq * p.width + q.col + v] : 0.f;
+    long long t0 = (q.rank * (int)blockDim.y + (int)threadIdx.y) * L;
+    // steps that do not exist keep the state: x = 0, gate = -inf
+    int n = q.on ? (int)max(0ll, min((long long)L, q.len - t0)) : 0;
+    word xw[L], gw[L];
+    load_tile<T, V, L>(xw, x + t0 * p.in_step, p.in_step, n, 0.f);
+    load_tile<T, V, L>(gw, g + t0 * p.in_step, p.in_step, n, -INFINITY);
     if (blocks > 1) cluster_wait();
     int set = 0;
     for (long long base = 0; base < q.len; base += stride, set ^= 1) {
-        const long long t0 = base + (q.rank * (int)blockDim.y + (int)threadIdx.y) * L;
-        const int n = q.on ? (int)max(0ll, min((long long)L, q.len - t0)) : 0;
-        word xw[L], gw[L];
-#pragma unroll
-        for (int i = 0; i < L; ++i)
-            if (i < n) {
-                xw[i] = *(const word*)(x + (t0 + i) * p.in_step);
-                gw[i] = *(const word*)(g + (t0 + i) * p.in_step);
-            }
-        float s[L][V], xs[L][V], start[V];
-        Affine own[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) { own[v] = {1.f, 0.f, 0.f}; start[v] = carry[v]; }
+        float nb[L][V], start[V];
+        word now[L];
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            if (i < n) {
-                float gf[V];
-                W::get(gw[i], gf);
-                W::get(xw[i], xs[i]);
+            float f[V], slope;
+            W::get(gw[i], f);
 #pragma unroll
-                for (int v = 0; v < V; ++v) s[i][v] = signed_gate(gf[v]);
-                if (!alone) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float sv = s[i][v];
-                        own[v].A = decay(sv, own[v].A);
-                        own[v].C = step_forward<true>(sv, 1.f, own[v].C);
-                        own[v].u = step_forward<COUPLED>(sv, xs[i][v], own[v].u);
-                    }
-                }
-            }
+            for (int v = 0; v < V; ++v) negated_gate<T>(f[v], nb[i][v], slope);
+            now[i] = COUPLED ? W::negate(xw[i]) : xw[i];
         }
-        if (!alone) exchange<V>(ex, set, own, carry, start, blocks, q.rank);
+        // the next round's steps are on their way while this one's are summed
+        const int m = n;
+        T* const o = out + t0 * p.out_step;
+        t0 += stride;
+        n = q.on ? (int)max(0ll, min((long long)L, q.len - t0)) : 0;
+        load_tile<T, V, L>(xw, x + t0 * p.in_step, p.in_step, n, 0.f);
+        load_tile<T, V, L>(gw, g + t0 * p.in_step, p.in_step, n, -INFINITY);
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            if (i < n) {
+        for (int v = 0; v < V; ++v) start[v] = carry[v];
+        if (!alone) {
+            Map<V> own;
 #pragma unroll
-                for (int v = 0; v < V; ++v) start[v] = step_forward<COUPLED>(s[i][v], xs[i][v], start[v]);
-                *(word*)(out + (t0 + i) * p.out_step) = W::put(start);
+            for (int i = 0; i < L; ++i) {
+                float xs[V];
+                W::get(now[i], xs);
+                own.decay(nb[i]);
+                step_forward<COUPLED, V>(own.u, nb[i], xs);
             }
+            exchange<V>(ex, set, own, carry, start, blocks, q.rank);
+        }
+        T* to = o;
+#pragma unroll
+        for (int i = 0; i < L; ++i, to += p.out_step) {
+            float xs[V];
+            W::get(now[i], xs);
+            step_forward<COUPLED, V>(start, nb[i], xs);
+            if (i < m) *(word*)to = W::put(start);
         }
         if (alone) {
 #pragma unroll
@@ -246,7 +329,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
     }
 }
 
-// Steps counted from the end: step i of a warp is time t = len - 1 - (tau0 + i)
+// Steps counted from the end: step i of a warp is time t0 - i
 template <typename T, int V, bool COUPLED, int L>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const int blocks) {
     using W = Word<T, V>;
@@ -263,67 +346,71 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
     bool bad = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr && q.on ? p.dyT[w0 + v] : 0.f;
+    long long t0 = (long long)q.len - 1 - (q.rank * (int)blockDim.y + (int)threadIdx.y) * L;
+    int n = q.on ? (int)max(0ll, min((long long)L, t0 + 1)) : 0;
+    word xw[L], gw[L], dw[L], yw[L];
+    auto load = [&]() {
+        load_tile<T, V, L>(gw, g + t0 * p.in_step, -p.in_step, n, -INFINITY);
+        load_tile<T, V, L>(dw, dy + t0 * p.out_step, -p.out_step, p.dy != nullptr ? n : 0, 0.f);
+        if (COUPLED) load_tile<T, V, L>(xw, x + t0 * p.in_step, -p.in_step, n, 0.f);
+        load_tile<T, V, L>(yw, y + (t0 - 1) * p.out_step, -p.out_step, (int)min((long long)n, t0), 0.f);      // the states in front of the steps
+    };
+    load();
     if (blocks > 1) cluster_wait();
     int set = 0;
     for (long long base = 0; base < q.len; base += stride, set ^= 1) {
-        const long long t0 = q.len - 1 - (base + (q.rank * (int)blockDim.y + (int)threadIdx.y) * L);
-        const int n = q.on ? (int)max(0ll, min((long long)L, t0 + 1)) : 0;
-        word xw[L], gw[L], dw[L], yw[L];
-#pragma unroll
-        for (int i = 0; i < L; ++i)
-            if (i < n) {
-                gw[i] = *(const word*)(g + (t0 - i) * p.in_step);
-                if (p.dy != nullptr) dw[i] = *(const word*)(dy + (t0 - i) * p.out_step);
-                if (COUPLED) xw[i] = *(const word*)(x + (t0 - i) * p.in_step);
-                if (t0 - i > 0) yw[i] = *(const word*)(y + (t0 - i - 1) * p.out_step);
-            }
-        float s[L][V], ds[L][V], start[V];
-        Affine own[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) { own[v] = {1.f, 0.f, 0.f}; start[v] = carry[v]; }
+        float nb[L][V], slope[L][V], start[V];
+        word now[L], before[L], given[L];
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            if (i < n) {
-                float gf[V];
-                W::get(gw[i], gf);
+            float f[V];
+            W::get(gw[i], f);
 #pragma unroll
-                for (int v = 0; v < V; ++v) { s[i][v] = signed_gate(gf[v]); ds[i][v] = 0.f; }
-                if (p.dy != nullptr) W::get(dw[i], ds[i]);
-                if (!alone) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float sv = s[i][v];
-                        own[v].A = decay(sv, own[v].A);
-                        own[v].C = step_forward<true>(sv, 1.f, own[v].C);
-                        own[v].u = decay(sv, own[v].u + ds[i][v]);
-                    }
-                }
-            }
+            for (int v = 0; v < V; ++v) negated_gate<T>(f[v], nb[i][v], slope[i][v]);
+            now[i] = xw[i]; before[i] = yw[i]; given[i] = dw[i];
         }
-        if (!alone) exchange<V>(ex, set, own, carry, start, blocks, q.rank);
+        const int m = n, first = t0 < L ? (int)t0 : L;                       // index of time 0
+        const long long at = t0 * p.in_step;
+        t0 -= stride;
+        n = q.on ? (int)max(0ll, min((long long)L, t0 + 1)) : 0;
+        load();
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            if (i < n) {
-                float before[V], xs[V], gx[V], gg[V];
+        for (int v = 0; v < V; ++v) start[v] = carry[v];
+        if (!alone) {
+            Map<V> own;
 #pragma unroll
-                for (int v = 0; v < V; ++v) before[v] = xs[v] = 0.f;
-                if (t0 - i > 0) W::get(yw[i], before);
-                else if (p.y0 != nullptr) {
+            for (int i = 0; i < L; ++i) {
+                float d[V], l[V];
+                W::get(given[i], d);
+                own.decay(nb[i]);
+                Ops<V>::add(l, own.u, d);
+                Ops<V>::fma(own.u, nb[i], l, l);
+            }
+            exchange<V>(ex, set, own, carry, start, blocks, q.rank);
+        }
+        T *ox = dx + at, *og = dg + at;
 #pragma unroll
-                    for (int v = 0; v < V; ++v) before[v] = p.y0[w0 + v];
-                }
-                if (COUPLED) W::get(xw[i], xs);
+        for (int i = 0; i < L; ++i, ox -= p.in_step, og -= p.in_step) {
+            float xs[V], ys[V], d[V], l[V], gx[V], gg[V];
+            W::get(given[i], d);
+            W::get(before[i], ys);
+            if (i == first && p.y0 != nullptr && q.on) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float sv = s[i][v], small = fabsf(sv), big = 1.f - small, l = start[v] + ds[i][v];
-                    gx[v] = COUPLED ? (resets(sv) ? big : small) * l : l;
-                    gg[v] = l * (small * big) * (COUPLED ? xs[v] - before[v] : -before[v]);
-                    start[v] = decay(sv, l);
-                }
+                for (int v = 0; v < V; ++v) ys[v] = p.y0[w0 + v];
+            }
+            Ops<V>::add(l, start, d);
+            Ops<V>::fma(start, nb[i], l, l);
+            if (COUPLED) W::get(now[i], xs);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                gx[v] = COUPLED ? -nb[i][v] * l[v] : l[v];
+                gg[v] = slope[i][v] * l[v] * (COUPLED ? xs[v] - ys[v] : -ys[v]);
+            }
+            if (i < m) {
                 const word wx = W::put(gx), wg = W::put(gg);
                 bad |= word_nonfinite<T, V>(wx) || word_nonfinite<T, V>(wg);
-                *(word*)(dx + (t0 - i) * p.in_step) = wx;
-                *(word*)(dg + (t0 - i) * p.in_step) = wg;
+                *(word*)ox = wx;
+                *(word*)og = wg;
             }
         }
         if (alone) {
@@ -363,17 +450,18 @@ cudaError_t launch(void (*kernel)(const RecArgs, const int), const RecArgs& a, c
     return cudaLaunchKernelEx(&cfg, kernel, a, s.blocks);
 }
 
-constexpr int kForwardSteps = 16, kBackwardSteps = 8;
+template <typename T, int V> constexpr int kForwardSteps = sizeof(T) * V > 4 ? 8 : 16;
+template <typename T, int V> constexpr int kBackwardSteps = sizeof(T) * V > 4 ? 4 : 8;
 
 template <typename T, int V> cudaError_t run_forward(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
-    const Shape s = shape_of(d, 32 * V, kForwardSteps);
-    return d.coupled ? launch(recurrence_forward_kernel<T, V, true, kForwardSteps>, a, s, st)
-                     : launch(recurrence_forward_kernel<T, V, false, kForwardSteps>, a, s, st);
+    constexpr int L = kForwardSteps<T, V>;
+    const Shape s = shape_of(d, 32 * V, L);
+    return d.coupled ? launch(recurrence_forward_kernel<T, V, true, L>, a, s, st) : launch(recurrence_forward_kernel<T, V, false, L>, a, s, st);
 }
 template <typename T, int V> cudaError_t run_backward(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
-    const Shape s = shape_of(d, 32 * V, kBackwardSteps);
-    return d.coupled ? launch(recurrence_backward_kernel<T, V, true, kBackwardSteps>, a, s, st)
-                     : launch(recurrence_backward_kernel<T, V, false, kBackwardSteps>, a, s, st);
+    constexpr int L = kBackwardSteps<T, V>;
+    const Shape s = shape_of(d, 32 * V, L);
+    return d.coupled ? launch(recurrence_backward_kernel<T, V, true, L>, a, s, st) : launch(recurrence_backward_kernel<T, V, false, L>, a, s, st);
 }
 
 // the checks that both directions share; fills in strides that are zero
@@ -399,13 +487,13 @@ mpode_status check(const mpode_recurrence_desc* d, RecArgs& a) {
     a.n_seq = d->n_seq; a.n_steps = d->n_steps; a.width = d->width;
     return MPODE_OK;
 }
-// 32-bit words of two channels need even widths and strides and 4-byte aligned rows
+// two channels an access need even widths and strides and rows aligned to two elements
 bool words_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
     if (d.width & 1) return false;
     if ((a.in_step | a.in_seq | a.out_step | a.out_seq) & 1) return false;
     const void* const all[] = {a.x, a.gate, a.y, a.dy, a.out, a.out2};
     for (const void* q : all)
-        if (misaligned(q, 4)) return false;
+        if (misaligned(q, 2 * low_size(d.low))) return false;
     return true;
 }
 mpode_status check_pointers(const mpode_recurrence_desc& d, const RecArgs& a) {
@@ -455,7 +543,7 @@ mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* c
     if (off != MPODE_OK) return off;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (desc->low == MPODE_F32) e = run_forward<float, 1>(*desc, a, st);
+    if (desc->low == MPODE_F32) e = words_fit(*desc, a) ? run_forward<float, 2>(*desc, a, st) : run_forward<float, 1>(*desc, a, st);
     else if (desc->low == MPODE_BF16) e = words_fit(*desc, a) ? run_forward<__nv_bfloat16, 2>(*desc, a, st) : run_forward<__nv_bfloat16, 1>(*desc, a, st);
     else e = words_fit(*desc, a) ? run_forward<__half, 2>(*desc, a, st) : run_forward<__half, 1>(*desc, a, st);
     return operator_launched(e, "mpode_recurrence_forward");
@@ -476,7 +564,7 @@ mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* 
     if (off != MPODE_OK) return off;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (desc->low == MPODE_F32) e = run_backward<float, 1>(*desc, a, st);
+    if (desc->low == MPODE_F32) e = words_fit(*desc, a) ? run_backward<float, 2>(*desc, a, st) : run_backward<float, 1>(*desc, a, st);
     else if (desc->low == MPODE_BF16) e = words_fit(*desc, a) ? run_backward<__nv_bfloat16, 2>(*desc, a, st) : run_backward<__nv_bfloat16, 1>(*desc, a, st);
     else e = words_fit(*desc, a) ? run_backward<__half, 2>(*desc, a, st) : run_backward<__half, 1>(*desc, a, st);
     return operator_launched(e, "mpode_recurrence_backward");
