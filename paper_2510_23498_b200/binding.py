@@ -374,50 +374,75 @@ class Context:
 
 
 # ---- operators of sequence and residual networks (mpode_recurrence_*, mpode_residual_*, mpode_dropout).  They need no Context: results go to new
-# tensors or to the caller's, on the current stream of the inputs' device.
+# tensors or to the caller's, on the current stream of the inputs' device.  A call for one token runs a few microseconds on the GPU, so what the host does
+# for it is kept short: shapes and strides are compared as they are, and a device guard is entered only where another device is current.
+_torch = None
+_LOW = {}
+_raw_stream = None
+
+
+def _load():
+    """(library, torch), loaded once."""
+    global _torch, _raw_stream
+    if _torch is None:
+        import torch
+        # the current stream's handle without the Stream object around it (3 us less a call)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _LOW.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        load_library()
+        _torch = torch
+    return _lib, _torch
+
+
 def _refuse(message: str):
     raise MpodeError(ERR_INVALID_ARG, message)
 
 
-def _operator_check(st: int):
-    if st != OK:
-        lib = load_library()
-        raise MpodeError(st, lib.mpode_operator_error().decode() or lib.mpode_status_string(st).decode())
-
-
 def _low_of(t) -> int:
-    low = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}.get(str(t.dtype))
+    low = _LOW.get(t.dtype)
     if low is None:
         _refuse("dtype %s is not one of float32, bfloat16, float16" % t.dtype)
     return low
 
 
-def _on_device(first, *others):
-    """All tensors on the CUDA device of the first one; returns (device guard, raw stream)."""
-    import torch
-    if not first.is_cuda:
+def _run(entry, desc, tensors, args):
+    """entry(desc, stream, *args) on the CUDA device of the first tensor, where all of them have to be."""
+    lib, torch = _load()
+    device = tensors[0].get_device()
+    if device < 0:
         _refuse("the tensors have to be on a CUDA device")
-    for t in others:
-        if t is not None and t.device != first.device:
-            _refuse("tensors on %s and %s" % (first.device, t.device))
-    return torch.cuda.device(first.device), int(torch.cuda.current_stream(first.device).cuda_stream)
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            _refuse("tensors on %s and %s" % (tensors[0].device, t.device))
+    if torch.cuda.current_device() == device:
+        st = entry(desc, _raw_stream(device), *args)
+    else:
+        with torch.cuda.device(device):
+            st = entry(desc, _raw_stream(device), *args)
+    if st != OK:
+        raise MpodeError(st, lib.mpode_operator_error().decode() or lib.mpode_status_string(st).decode())
 
 
 def _expect(name: str, t, shape, dtype):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous()):
+    if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
         _refuse("%s has to be a contiguous %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 
 def _layout(name: str, t, shape, dtype):
-    """(sequence stride, step stride) of a [n_seq, n_steps, width] tensor whose channels lie side by side; 0 where a dimension has one entry."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    """(sequence stride, step stride) of a [n_seq, n_steps, width] tensor whose channels lie side by side; the width where a dimension has one entry."""
+    if t.shape != shape or t.dtype != dtype:
         _refuse("%s has to be a %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-    if shape[2] > 1 and t.stride(2) != 1:
+    n, steps, width = shape
+    a, b, c = t.stride()
+    if c != 1 and width > 1:
         _refuse("the channels of %s have to lie side by side" % name)
-    out = tuple(t.stride(k) if shape[k] > 1 else 0 for k in (0, 1))
-    if any(s == 0 and shape[k] > 1 for k, s in enumerate(out)):
+    if n <= 1:
+        a = width
+    if steps <= 1:
+        b = width
+    if a == 0 or b == 0:
         _refuse("%s is broadcast along a dimension" % name)
-    return out
+    return a, b
 
 
 def _same_layout(name: str, t, shape, dtype, layout):
@@ -425,54 +450,34 @@ def _same_layout(name: str, t, shape, dtype, layout):
         _refuse("%s has to have the strides %s" % (name, layout))
 
 
-def _like(t, fill_zero: bool):
-    """A tensor of the strides of t (a slice's gaps included)."""
-    import torch
-    out = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
-    return out.zero_() if fill_zero else out
-
-
-def _recurrence_desc(x, gate, coupled, out_layout=(0, 0)):
+def _sequences(x):
     if x.dim() != 3:
         _refuse("x has to be [n_seq, n_steps, width]")
-    shape = tuple(x.shape)
-    layout = _layout("x", x, shape, x.dtype)
-    _same_layout("gate", gate, shape, x.dtype, layout)
-    d = RecurrenceDesc(_low_of(x), shape[0], shape[1], shape[2], 1 if coupled else 0, layout[0], layout[1], out_layout[0], out_layout[1])
-    # a dimension of one entry has no stride; the other one's default would not know of a gap
-    if d.in_step_stride == 0:
-        d.in_step_stride = shape[2]
-    if d.in_seq_stride == 0:
-        d.in_seq_stride = max(shape[2], 1)
-    if d.out_step_stride == 0:
-        d.out_step_stride = shape[2]
-    if d.out_seq_stride == 0:
-        d.out_seq_stride = max(shape[2], 1)
-    return d, shape, layout
+    return x.shape
 
 
 def recurrence_forward(x, gate, y0=None, lengths=None, coupled: bool = True, y=None, yT=None):
     """mpode_recurrence_forward on x, gate [n_seq, n_steps, width] (any strides with the channels side by side, the same for both).
     Returns (y, yT): the stored trajectory (zero behind a sequence's length when allocated here, left alone there when given) and the float32 state
     behind the last step.  yT may be y0."""
-    import torch
+    lib, torch = _load()
+    shape = _sequences(x)
+    n, steps, width = shape
+    low, dtype = _low_of(x), x.dtype
+    inner = _layout("x", x, shape, dtype)
+    _same_layout("gate", gate, shape, dtype, inner)
     if y is None:
-        # time-major inputs get a time-major trajectory
-        n, T, w = x.shape if x.dim() == 3 else (0, 0, 0)
-        new = torch.zeros if lengths is not None else torch.empty
-        if n > 1 and T > 1 and x.stride(0) < x.stride(1):
-            y = new((T, n, w), dtype=x.dtype, device=x.device).transpose(0, 1)
-        else:
-            y = new((n, T, w), dtype=x.dtype, device=x.device)
-    d, shape, _ = _recurrence_desc(x, gate, coupled, _layout("y", y, tuple(x.shape), x.dtype) if x.dim() == 3 else (0, 0))
+        y = torch.empty_like(x) if lengths is None else torch.zeros_like(x)       # (time-major inputs get a time-major trajectory)
+    outer = _layout("y", y, shape, dtype)
+    states = (n, width)
     if yT is None:
-        yT = torch.empty((shape[0], shape[2]), dtype=torch.float32, device=x.device)
-    _expect("y0", y0, (shape[0], shape[2]), torch.float32)
-    _expect("yT", yT, (shape[0], shape[2]), torch.float32)
-    _expect("lengths", lengths, (shape[0],), torch.int32)
-    guard, stream = _on_device(x, gate, y0, lengths, y, yT)
-    with guard:
-        _operator_check(load_library().mpode_recurrence_forward(C.byref(d), stream, _ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(yT)))
+        yT = x.new_empty(states, dtype=torch.float32) if y0 is None else torch.empty_like(y0, memory_format=torch.contiguous_format)
+    else:
+        _expect("yT", yT, states, torch.float32)
+    _expect("y0", y0, states, torch.float32)
+    _expect("lengths", lengths, (n,), torch.int32)
+    _run(lib.mpode_recurrence_forward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, *inner, *outer), (x, gate, y0, lengths, y, yT),
+         (_ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(yT)))
     return y, yT
 
 
@@ -480,28 +485,37 @@ def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, c
     """mpode_recurrence_backward from the stored trajectory y.  dL_dy (or None) has the strides of y, dL_dx and dL_dgate those of x.
     Returns (dL_dx, dL_dgate, dL_dy0); the first two are zero behind a sequence's length when allocated here, left alone there when given.
     flag: int32 tensor of one element, set to 1 when a low-format gradient is not finite."""
-    import torch
-    if x.dim() != 3:
-        _refuse("x has to be [n_seq, n_steps, width]")
-    out_layout = _layout("y", y, tuple(x.shape), x.dtype)
-    d, shape, layout = _recurrence_desc(x, gate, coupled, out_layout)
-    _same_layout("dL_dy", dL_dy, shape, x.dtype, out_layout)
+    lib, torch = _load()
+    shape = _sequences(x)
+    n, steps, width = shape
+    low, dtype, device = _low_of(x), x.dtype, x.device
+    inner, outer = _layout("x", x, shape, dtype), _layout("y", y, shape, dtype)
+    _same_layout("gate", gate, shape, dtype, inner)
+    _same_layout("dL_dy", dL_dy, shape, dtype, outer)
     if dL_dx is None:
-        dL_dx = _like(x, lengths is not None)
+        dL_dx = torch.empty_strided(shape, x.stride(), dtype=dtype, device=device)
+        if lengths is not None:
+            dL_dx.zero_()
+    else:
+        _same_layout("dL_dx", dL_dx, shape, dtype, inner)
     if dL_dgate is None:
-        dL_dgate = _like(x, lengths is not None)
+        dL_dgate = torch.empty_strided(shape, x.stride(), dtype=dtype, device=device)
+        if lengths is not None:
+            dL_dgate.zero_()
+    else:
+        _same_layout("dL_dgate", dL_dgate, shape, dtype, inner)
+    states = (n, width)
     if dL_dy0 is None:
-        dL_dy0 = torch.empty((shape[0], shape[2]), dtype=torch.float32, device=x.device)
-    _same_layout("dL_dx", dL_dx, shape, x.dtype, layout)
-    _same_layout("dL_dgate", dL_dgate, shape, x.dtype, layout)
-    for name, t in (("y0", y0), ("dL_dyT", dL_dyT), ("dL_dy0", dL_dy0)):
-        _expect(name, t, (shape[0], shape[2]), torch.float32)
-    _expect("lengths", lengths, (shape[0],), torch.int32)
+        dL_dy0 = torch.empty(states, dtype=torch.float32, device=device)
+    else:
+        _expect("dL_dy0", dL_dy0, states, torch.float32)
+    _expect("y0", y0, states, torch.float32)
+    _expect("dL_dyT", dL_dyT, states, torch.float32)
+    _expect("lengths", lengths, (n,), torch.int32)
     _expect("flag", flag, (1,), torch.int32)
-    guard, stream = _on_device(x, gate, y, dL_dy, dL_dyT, y0, lengths, dL_dx, dL_dgate, dL_dy0, flag)
-    with guard:
-        _operator_check(load_library().mpode_recurrence_backward(C.byref(d), stream, _ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(dL_dy),
-                                                                 _ptr(dL_dyT), _ptr(dL_dx), _ptr(dL_dgate), _ptr(dL_dy0), _ptr(flag)))
+    _run(lib.mpode_recurrence_backward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, *inner, *outer),
+         (x, gate, y, dL_dy, dL_dyT, y0, lengths, dL_dx, dL_dgate, dL_dy0, flag),
+         (_ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(dL_dy), _ptr(dL_dyT), _ptr(dL_dx), _ptr(dL_dgate), _ptr(dL_dy0), _ptr(flag)))
     return dL_dx, dL_dgate, dL_dy0
 
 
@@ -509,22 +523,21 @@ def _rows(name: str, t, shape, dtype) -> int:
     """Row length of a [rows, width] tensor whose columns lie side by side."""
     if t is None:
         return 0
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         _refuse("%s has to be a %s tensor of shape %s, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-    if shape[1] > 1 and t.stride(1) != 1:
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
         _refuse("the columns of %s have to lie side by side" % name)
     if shape[0] <= 1:
         return shape[1]
-    if t.stride(0) < shape[1]:
+    if ld < shape[1]:
         _refuse("the rows of %s overlap" % name)
-    return t.stride(0)
+    return ld
 
 
-def _same_rows(shape, dtype, *named) -> int:
-    lds = {_rows(name, t, shape, dtype) for name, t in named if t is not None}
-    if len(lds) > 1:
-        _refuse("%s have to have the same row length" % ", ".join(name for name, t in named if t is not None))
-    return lds.pop() if lds else 0
+def _same_rows(name: str, t, shape, dtype, ld: int):
+    if t is not None and _rows(name, t, shape, dtype) != ld:
+        _refuse("%s has to have the row length %d" % (name, ld))
 
 
 class ResidualStep:
@@ -533,7 +546,7 @@ class ResidualStep:
 
     def __init__(self, width: int, low: str = "bf16", post_norm: str = "rms", pre_norm: str = "rms", eps: float = 1e-5, h: float = 1.0,
                  p: float = 0.0, site: int = 0):
-        import torch
+        _, torch = _load()
         self.width, self.p, self.h, self.eps, self.site = int(width), float(p), float(h), float(eps), int(site)
         self.low, self.post_norm, self.pre_norm = DTYPES[low], NORMS[post_norm], NORMS[pre_norm]
         self.low_torch = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[low]
@@ -541,31 +554,33 @@ class ResidualStep:
     def _desc(self, ld_y, ld_u, ld_gate, ld_z):
         return ResidualDesc(self.low, self.width, self.post_norm, self.pre_norm, self.eps, self.h, self.p, self.site, ld_y, ld_u, ld_gate, ld_z)
 
-    def _common(self, y, weights, rng):
-        import torch
-        if y.dim() != 2:
-            _refuse("the state has to be [rows, width]")
-        for name, w in weights:
-            _expect(name, w, (self.width,), torch.float32)
-        _expect("rng", rng, (2,), torch.int64)
-        return (y.shape[0], self.width)
+    def _shape(self, y, w_post, scale, w_pre, rng):
+        if y.dim() != 2 or y.shape[1] != self.width:
+            _refuse("the state has to be [rows, %d]" % self.width)
+        one, f32 = (self.width,), _torch.float32
+        _expect("w_post", w_post, one, f32)
+        _expect("scale", scale, one, f32)
+        _expect("w_pre", w_pre, one, f32)
+        _expect("rng", rng, (2,), _torch.int64)
+        return y.shape
 
     def forward(self, y, u=None, gate=None, w_post=None, scale=None, w_pre=None, rng=None, y_out=None, z=None, want_z: bool = True):
         """Returns (y', z, stats): the state behind the step (y itself without u), the next block's input (None with want_z=False) and the statistics
         that backward needs.  y_out may be y."""
-        import torch
-        shape = self._common(y, (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)), rng)
-        if u is not None and y_out is None:
-            y_out = torch.empty_strided(y.shape, y.stride(), dtype=y.dtype, device=y.device)
+        lib, torch = _load()
+        f32, low = torch.float32, self.low_torch
+        shape = self._shape(y, w_post, scale, w_pre, rng)
+        ld_y = _rows("y", y, shape, f32)
+        if y_out is not None:
+            _same_rows("y_out", y_out, shape, f32, ld_y)
+        elif u is not None:
+            y_out = torch.empty_like(y) if y.is_contiguous() else y.new_empty_strided(shape, y.stride())
         if want_z and z is None:
-            z = torch.empty(shape, dtype=self.low_torch, device=y.device)
-        stats = torch.empty((shape[0], 4), dtype=torch.float32, device=y.device)
-        d = self._desc(_same_rows(shape, torch.float32, ("y", y), ("y_out", y_out)), _rows("u", u, shape, self.low_torch),
-                       _rows("gate", gate, shape, self.low_torch), _rows("z", z, shape, self.low_torch))
-        guard, stream = _on_device(y, u, gate, w_post, scale, w_pre, rng, y_out, z)
-        with guard:
-            _operator_check(load_library().mpode_residual_forward(C.byref(d), stream, shape[0], _ptr(y), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale),
-                                                                  _ptr(w_pre), _ptr(rng), _ptr(y_out), _ptr(z), _ptr(stats)))
+            z = y.new_empty(shape, dtype=low)
+        stats = y.new_empty((shape[0], 4))
+        desc = self._desc(ld_y, _rows("u", u, shape, low), _rows("gate", gate, shape, low), _rows("z", z, shape, low))
+        _run(lib.mpode_residual_forward, desc, (y, u, gate, w_post, scale, w_pre, rng, y_out, z),
+             (shape[0], _ptr(y), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(rng), _ptr(y_out), _ptr(z), _ptr(stats)))
         return (y if y_out is None else y_out), z, stats
 
     def backward(self, y_new, u=None, stats=None, dL_dy=None, dL_dz=None, gate=None, w_post=None, scale=None, w_pre=None, rng=None, scale_exp: int = 0,
@@ -573,56 +588,61 @@ class ResidualStep:
         """dL_dy: adjoint of y' (float32), dL_dz: cotangent of z (low format, times 2^scale_exp).  Returns a dict with "dy" (adjoint of y), "du" and "dgate" (low
         format, times 2^scale_exp; None without u, gate) and the gradients "dw_post", "dscale", "dw_pre" of the weights that were given (added to the
         tensors of that name in accumulate_into when given).  flag: int32 tensor of one element, set to 1 when du or dgate is not finite."""
-        import torch
-        shape = self._common(y_new, (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)), rng)
-        _expect("stats", stats, (shape[0], 4), torch.float32)
+        lib, torch = _load()
+        f32, low, device = torch.float32, self.low_torch, y_new.device
+        shape = self._shape(y_new, w_post, scale, w_pre, rng)
+        rows = shape[0]
+        _expect("stats", stats, (rows, 4), f32)
         _expect("flag", flag, (1,), torch.int32)
-        out = dict(dy=torch.empty_strided(y_new.shape, y_new.stride(), dtype=torch.float32, device=y_new.device),
-                   du=None if u is None else torch.empty_strided(u.shape, u.stride(), dtype=u.dtype, device=u.device),
-                   dgate=None if gate is None else torch.empty_strided(gate.shape, gate.stride(), dtype=gate.dtype, device=gate.device))
+        ld_y, ld_u, ld_gate = _rows("y_new", y_new, shape, f32), _rows("u", u, shape, low), _rows("gate", gate, shape, low)
+        _same_rows("dL_dy", dL_dy, shape, f32, ld_y)
+        out = {"dy": torch.empty_strided(shape, y_new.stride(), dtype=f32, device=device), "du": None, "dgate": None}
+        if u is not None:
+            out["du"] = torch.empty_strided(shape, u.stride(), dtype=low, device=device)
+        if gate is not None:
+            out["dgate"] = torch.empty_strided(shape, gate.stride(), dtype=low, device=device)
         for key, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
-            out[key] = None
+            g = None
             if want_weights and w is not None:
-                out[key] = accumulate_into[key] if accumulate_into is not None else torch.empty(self.width, dtype=torch.float32, device=y_new.device)
-                _expect(key, out[key], (self.width,), torch.float32)
-        grads = [out[k] for k in ("dw_post", "dscale", "dw_pre")]
-        d = self._desc(_same_rows(shape, torch.float32, ("y_new", y_new), ("dL_dy", dL_dy), ("dy", out["dy"])),
-                       _same_rows(shape, self.low_torch, ("u", u), ("du", out["du"])), _same_rows(shape, self.low_torch, ("gate", gate), ("dgate", out["dgate"])),
-                       _rows("dL_dz", dL_dz, shape, self.low_torch))
-        lib = load_library()
-        guard, stream = _on_device(y_new, u, stats, dL_dy, dL_dz, gate, w_post, scale, w_pre, rng, flag, *grads)
-        with guard:
-            ws, nbytes = None, 0
-            if any(g is not None for g in grads) and shape[0] > 0:
-                nbytes = int(lib.mpode_residual_workspace_bytes(C.byref(d), shape[0]))
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=y_new.device)
-            _operator_check(lib.mpode_residual_backward(C.byref(d), stream, shape[0], _ptr(y_new), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre),
-                                                        _ptr(rng), _ptr(stats), _ptr(dL_dy), _ptr(dL_dz), int(scale_exp), _ptr(out["dy"]), _ptr(out["du"]),
-                                                        _ptr(out["dgate"]), *[_ptr(g) for g in grads], 1 if accumulate_into is not None else 0, _ptr(flag),
-                                                        _ptr(ws), nbytes))
+                if accumulate_into is None:
+                    g = torch.empty(self.width, dtype=f32, device=device)
+                else:
+                    g = accumulate_into[key]
+                    _expect(key, g, (self.width,), f32)
+            out[key] = g
+        grads = (out["dw_post"], out["dscale"], out["dw_pre"])
+        desc = self._desc(ld_y, ld_u, ld_gate, _rows("dL_dz", dL_dz, shape, low))
+        ws, nbytes = None, 0
+        if rows > 0 and grads != (None, None, None):
+            nbytes = lib.mpode_residual_workspace_bytes(desc, rows)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _run(lib.mpode_residual_backward, desc, (y_new, u, stats, dL_dy, dL_dz, gate, w_post, scale, w_pre, rng, flag) + grads,
+             (rows, _ptr(y_new), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(rng), _ptr(stats), _ptr(dL_dy), _ptr(dL_dz),
+              int(scale_exp), _ptr(out["dy"]), _ptr(out["du"]), _ptr(out["dgate"]), _ptr(grads[0]), _ptr(grads[1]), _ptr(grads[2]),
+              0 if accumulate_into is None else 1, _ptr(flag), _ptr(ws), nbytes))
         return out
 
 
 def dropout(x, p: float, rng, site: int = 0, out=None, flag=None):
     """mpode_dropout on the rows of x [..., width] (2-D with any row length, or contiguous); on a cotangent it is the backward pass.
     rng: int64 tensor {seed, step} on the device.  out may be x."""
-    import torch
-    if x.dim() == 0:
+    lib, torch = _load()
+    low, dim = _low_of(x), x.dim()
+    if dim == 0:
         _refuse("x has to have rows")
-    shape = (x.numel() // max(x.shape[-1], 1), x.shape[-1])
-    if x.dim() != 2 and not x.is_contiguous():
-        _refuse("x has to be contiguous, or 2-D with its columns side by side")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if tuple(out.shape) != tuple(x.shape) or (out.dim() != 2 and not out.is_contiguous()):
-        _refuse("out has to have the shape of x, and be contiguous or 2-D")
-    low = _low_of(x)
+        out = torch.empty_like(x)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        _refuse("out has to be of the shape and type of x")
+    if dim == 2:
+        shape = x.shape
+        ld_x, ld_out = _rows("x", x, shape, x.dtype), _rows("out", out, shape, x.dtype)
+    else:
+        if not x.is_contiguous() or not out.is_contiguous():
+            _refuse("x and out have to be contiguous, or 2-D with their columns side by side")
+        shape = (x.numel() // max(x.shape[-1], 1), x.shape[-1])
+        ld_x = ld_out = shape[1]
     _expect("rng", rng, (2,), torch.int64)
     _expect("flag", flag, (1,), torch.int32)
-    rows_x = _rows("x", x if x.dim() == 2 else x.view(shape), shape, x.dtype)
-    rows_out = _rows("out", out if out.dim() == 2 else out.view(shape), shape, x.dtype)
-    guard, stream = _on_device(x, rng, out, flag)
-    with guard:
-        _operator_check(load_library().mpode_dropout(low, stream, shape[0], shape[1], _ptr(x), rows_x, _ptr(out), rows_out, float(p), _ptr(rng), int(site),
-                                                     _ptr(flag)))
+    _run(lib.mpode_dropout, low, (x, rng, out, flag), (shape[0], shape[1], _ptr(x), ld_x, _ptr(out), ld_out, p, _ptr(rng), site, _ptr(flag)))
     return out

@@ -15,21 +15,37 @@ struct DropArgs {
     unsigned* flag;
 };
 
-// One thread, one group of eight columns at a time: 16-byte loads where the layout allows, bound by those bytes and the generator alike
-template <typename T, bool VEC> __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs p) {
+// One thread, one group of eight columns at a time: 16-byte accesses where the layout allows.  FLAT: rows of whole groups one behind the other, where a
+// group's place needs no division.
+template <typename T, bool VEC, bool FLAT> __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs p) {
     const uint64_t seed = p.d.rng[0], step = p.d.rng[1];
-    bool bad = false;
+    Largest<T> largest;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < p.groups; i += (long long)gridDim.x * 256) {
-        const long long row = i / p.groups_row;
-        const int col = (int)(i - row * p.groups_row) * 8, n = min(8, p.width - col);
-        float f[8];
-        load8<T, VEC>((const T*)p.x + row * p.ld_x + col, n, f);
-        const uint32_t keep = keep_bits((uint64_t)i, seed, step, p.d.site, p.d.threshold);
+        long long from = i * 8, to = i * 8;
+        int n = 8;
+        if (!FLAT) {
+            const long long row = i / p.groups_row;
+            const int col = (int)(i - row * p.groups_row) * 8;
+            n = min(8, p.width - col);
+            from = row * p.ld_x + col;
+            to = row * p.ld_out + col;
+        }
+        Oct o;
+        load8<T, VEC>((const T*)p.x + from, n, o);
+        const Kept keep(p.d, (uint64_t)i, seed, step);
+        const float2 s = make_float2(p.d.scale, p.d.scale);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = (keep >> j) & 1u ? f[j] * p.d.scale : 0.f;
-        bad |= store8<T, VEC>((T*)p.out + row * p.ld_out + col, n, f);
+        for (int j = 0; j < 4; ++j) {
+            o.v[j] = __fmul2_rn(o.v[j], s);
+            if (p.d.on && !keep[2 * j]) o.v[j].x = 0.f;
+            if (p.d.on && !keep[2 * j + 1]) o.v[j].y = 0.f;
+        }
+        Raw8<T> r;
+        pack<T>(o, r);
+        store_raw<T, VEC>((T*)p.out + to, n, r);
+        if (p.flag != nullptr) largest.see(r, n);
     }
-    warp_flag_or(p.flag, bad);
+    warp_flag_or(p.flag, largest.nonfinite());
 }
 
 }  // namespace
@@ -58,8 +74,9 @@ extern "C" mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long l
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
     with_low(low, [&](auto t) {
         using T = decltype(t);
-        if (vec) dropout_kernel<T, true><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-        else dropout_kernel<T, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+        if (vec && ld_x == width && ld_out == width) dropout_kernel<T, true, true><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+        else if (vec) dropout_kernel<T, true, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+        else dropout_kernel<T, false, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
         return cudaSuccess;
     });
     return operator_launched(cudaGetLastError(), "mpode_dropout");

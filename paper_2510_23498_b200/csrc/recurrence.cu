@@ -17,6 +17,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "operators.h"
 #include "rows.cuh"
 
@@ -73,63 +75,81 @@ template <typename T, int V> __device__ __forceinline__ typename Word<T, V>::typ
     for (int i = 0; i < V; ++i) f[i] = v;
     return Word<T, V>::put(f);
 }
-template <typename T, int V> __device__ __forceinline__ bool word_nonfinite(typename Word<T, V>::type w) {
-    float f[V];
-    Word<T, V>::get(w, f);
-    bool bad = false;
+template <typename T, int V> __device__ __forceinline__ void see(Largest<T>& m, const typename Word<T, V>::type& w) {
+    if constexpr (sizeof(T) == 2 && V == 2) m.see(w);
+    else if constexpr (sizeof(T) == 2) m.see((uint32_t)*reinterpret_cast<const uint16_t*>(&w));
+    else {
+        float f[V];
+        Word<T, V>::get(w, f);
 #pragma unroll
-    for (int v = 0; v < V; ++v) bad |= Low<float>::nonfinite(f[v]);
-    return bad;
+        for (int v = 0; v < V; ++v) m.see(__float_as_uint(f[v]));
+    }
 }
 
-// a b + c and a + b on all channels of a lane; two of them are one instruction
+// a b + c, a + b and a b on all channels of a lane; two of them are one instruction
 template <int V> struct Ops {
     static __device__ __forceinline__ void fma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
         if constexpr (V == 2) {
-            asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]), "f"(c[0]), "f"(c[1]));
+            const float2 r = __ffma2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]), make_float2(c[0], c[1]));
+            d[0] = r.x; d[1] = r.y;
         } else d[0] = fmaf(a[0], b[0], c[0]);
     }
     static __device__ __forceinline__ void add(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
         if constexpr (V == 2) {
-            asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+            const float2 r = __fadd2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+            d[0] = r.x; d[1] = r.y;
         } else d[0] = a[0] + b[0];
     }
     static __device__ __forceinline__ void mul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
         if constexpr (V == 2) {
-            asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-                : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]));
+            const float2 r = __fmul2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+            d[0] = r.x; d[1] = r.y;
         } else d[0] = a[0] * b[0];
     }
 };
 
-// -sigmoid(g) = -b and the slope b (1 - b), which is e b^2 with e = exp(-g).  16-bit gates: the device's approximate power and quotient (2^-22
-// relative, and the argument's rounding adds |g| 2^-24), which cost 5 instructions where the accurate ones of float32 cost 15; the exponent is
-// kept below 2^126, so that e b^2 is finite: b is 1e-38 instead of less, which no float32 state feels.
-template <typename T> __device__ __forceinline__ void negated_gate(float g, float& nb, float& slope) {
-    float e;
+// -sigmoid(g) = -b, and the slope b (1 - b), which is e b^2 with e = exp(-g).  16-bit gates: the device's approximate power and quotient (2^-22
+// relative, and the argument's rounding adds |g| 2^-24), which cost 3 instructions a channel where the accurate ones of float32 cost 15; for the slope
+// the exponent is kept below 2^126, so that e b^2 is finite: b is 1e-38 instead of less, which no float32 state feels.
+template <typename T, int V, bool SLOPE> __device__ __forceinline__ void negated_gate(const float (&g)[V], float (&nb)[V], float (&slope)[V]) {
+    float e[V];
     if constexpr (sizeof(T) == 4) {
-        e = expf(-g);
-        const float b = __fdividef(1.f, 1.f + e);
-        nb = -b;
-        slope = b * (e > 1.f ? 1.f - b : e * b);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            e[v] = expf(-g[v]);
+            const float b = __fdividef(1.f, 1.f + e[v]);
+            nb[v] = -b;
+            if (SLOPE) slope[v] = b * (e[v] > 1.f ? 1.f - b : e[v] * b);
+        }
     } else {
-        asm("min.NaN.f32 %0, %1, %2;" : "=f"(e) : "f"(g * -1.4426950408889634f), "f"(126.f));
-        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb) : "f"(-1.f - e));
-        slope = e * nb * nb;
+        float k[V], d[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) k[v] = -1.4426950408889634f;
+        Ops<V>::mul(e, g, k);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (SLOPE) asm("min.NaN.f32 %0, %0, %1;" : "+f"(e[v]) : "f"(126.f));
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[v]));
+            k[v] = -1.f;
+        }
+        Ops<V>::fma(d, e, k, k);
+#pragma unroll
+        for (int v = 0; v < V; ++v) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb[v]) : "f"(d[v]));
+        if (SLOPE) {
+            Ops<V>::mul(slope, nb, nb);
+            Ops<V>::mul(slope, slope, e);
+        }
     }
 }
 
-// one step, nb = -b; x is negated when coupled
-template <bool COUPLED, int V> __device__ __forceinline__ void step_forward(float (&y)[V], const float (&nb)[V], const float (&x)[V]) {
+// One step of the state s, nb = -b.  The coupled forward pass runs on s = -y, where b x is taken away without a change of sign: s - b s - b x.
+template <bool COUPLED, int V> __device__ __forceinline__ void step_forward(float (&s)[V], const float (&nb)[V], const float (&x)[V]) {
     float kept[V];
-    Ops<V>::fma(kept, nb, y, y);
-    if constexpr (COUPLED) Ops<V>::fma(y, nb, x, kept);
-    else Ops<V>::add(y, kept, x);
+    Ops<V>::fma(kept, nb, s, s);
+    if constexpr (COUPLED) Ops<V>::fma(s, nb, x, kept);
+    else Ops<V>::add(s, kept, x);
 }
-// The composed map y -> A y + u of some steps, C = 1 - A: A exact to its last bits where it is small (a reset leaves A = 0), C where the steps
+// The composed map s -> A s + u of some steps, C = 1 - A: A exact to its last bits where it is small (a reset leaves A = 0), C where the steps
 // forget little.  Kept per lane as A, -C and u.
 template <int V> struct Map {
     float A[V], nC[V], u[V];
@@ -146,322 +166,586 @@ template <int V> struct Map {
         Ops<V>::fma(nC, nb, left, nC);
     }
 };
-struct Affine { float A, C, u; };
-__device__ __forceinline__ float apply(const Affine& m, float y) { return (m.A < 0.5f ? m.A * y : fmaf(-m.C, y, y)) + m.u; }
-// first m, then n
-__device__ __forceinline__ Affine compose(const Affine& m, const Affine& n) {
-    return {m.A * n.A, fmaf(n.C, 1.f - m.C, m.C), apply(n, m.u)};
-}
+// As the warps and blocks exchange it: s -> m s + (k s + u), with (m, k) = (A, 0) or (-C, 1), whichever is the smaller one
+template <int V> struct Affine {
+    float m[V], k[V], u[V];
+    __device__ __forceinline__ void from(const Map<V>& p) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const bool fast = p.A[v] < 0.5f;
+            m[v] = fast ? p.A[v] : p.nC[v]; k[v] = fast ? 0.f : 1.f; u[v] = p.u[v];
+        }
+    }
+    __device__ __forceinline__ void apply(float (&s)[V]) const {
+        float t[V];
+        Ops<V>::fma(t, k, s, u);
+        Ops<V>::fma(s, m, s, t);
+    }
+    // p, then this map
+    __device__ __forceinline__ void follow(Map<V>& p) const {
+        float t[V], one[V], k1[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) { one[v] = 1.f; k1[v] = k[v] - 1.f; }
+        Ops<V>::mul(t, k, p.A);
+        Ops<V>::fma(p.A, m, p.A, t);
+        Ops<V>::add(t, one, p.nC);
+        Ops<V>::fma(p.nC, k, p.nC, k1);              // -C - c (1 - C) with c = -m, or 1 - m: -1 + m (1 - C)
+        Ops<V>::fma(p.nC, m, t, p.nC);
+        apply(p.u);
+    }
+};
 
+constexpr int kMaxWarps = 8, kMaxCluster = 16;
+constexpr unsigned long long kWaitNs = 2000000000ull;
+
+// Shared memory of the exchange: maps of the block's warps and of the cluster's blocks, two sets used in turn.  Places of warps and blocks
+// that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
+template <int V> struct __align__(16) Exchange {
+    float warp[2][kMaxWarps][3][32 * V];
+    float block[2][kMaxCluster][3][32 * V];
+    unsigned long long bar[2];                  // counts the bytes of a set's block maps
+};
 __device__ __forceinline__ unsigned smem_of(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ unsigned peer_of(unsigned local, unsigned rank) {
     unsigned r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void peer_store(unsigned at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-constexpr int kMaxWarps = 8, kMaxCluster = 8;
+template <int V> __device__ __forceinline__ void lds(float (&f)[V], const float* p) {
+    if constexpr (V == 2) {
+        const float2 t = *reinterpret_cast<const float2*>(p);
+        f[0] = t.x; f[1] = t.y;
+    } else f[0] = *p;
+}
+template <int V> __device__ __forceinline__ void sts(float* p, const float (&f)[V]) {
+    if constexpr (V == 2) *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
+    else *p = f[0];
+}
+template <int V> __device__ __forceinline__ void fetch(Affine<V>& a, const float (&t)[3][32 * V]) {
+    lds<V>(a.m, &t[0][threadIdx.x * V]); lds<V>(a.k, &t[1][threadIdx.x * V]); lds<V>(a.u, &t[2][threadIdx.x * V]);
+}
+template <int V> __device__ __forceinline__ void put(float (&t)[3][32 * V], const Affine<V>& a) {
+    sts<V>(&t[0][threadIdx.x * V], a.m); sts<V>(&t[1][threadIdx.x * V], a.k); sts<V>(&t[2][threadIdx.x * V], a.u);
+}
+// into another block's shared memory; the bytes count on that block's barrier, so that neither side needs a fence (one that made this block's
+// stores visible first would wait for its trajectory on the way to memory: 1 us a round)
+template <int V> __device__ __forceinline__ void send(unsigned at, const float (&f)[V], unsigned bar) {
+    if constexpr (V == 2)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(f[0]), "f"(f[1]), "r"(bar) : "memory");
+    else asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(at), "f"(f[0]), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool set_arrived(unsigned bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0u;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// The blocks of a cluster run at the same time, so this wait ends; should it not within two seconds, the results become NaN and the kernel ends
+__device__ __noinline__ bool await_set(unsigned bar, unsigned parity) {
+    const unsigned long long t0 = now_ns();
+    while (!set_arrived(bar, parity))
+        if (now_ns() - t0 > kWaitNs) return false;
+    return true;
+}
 
-// Shared memory of the exchange: products of the block's warps and of the cluster's blocks, two sets used in turn (a set is written again
-// only behind the next barrier, which nobody passes before the set has been read)
-template <int V> struct Exchange {
-    float warp[2][kMaxWarps][3][32 * V];
-    float block[2][kMaxCluster][3][32 * V];
-};
-template <int V> __device__ __forceinline__ Affine fetch(const float (&t)[3][32 * V], int i) { return {t[0][i], t[1][i], t[2][i]}; }
+template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex, int blocks) {
+    Affine<V> id;
+#pragma unroll
+    for (int v = 0; v < V; ++v) { id.m[v] = id.u[v] = 0.f; id.k[v] = 1.f; }
+    for (int set = 0; set < 2; ++set) {
+        for (int w = blockDim.y + threadIdx.y; w < kMaxWarps; w += blockDim.y) put<V>(ex.warp[set][w], id);
+        if (blocks > 1)
+            for (int r = blocks + threadIdx.y; r < kMaxCluster; r += blockDim.y) put<V>(ex.block[set][r], id);
+    }
+    if (blocks == 1) return;
+    if (threadIdx.x == 0 && threadIdx.y == 0) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&ex.bar[0])) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&ex.bar[1])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_arrive();                       // nobody writes into a block that has not started
+}
 
 // The state in front of this warp's steps, from the state in front of all of this round's steps (`carry`, replaced by the one behind them).
-// Called by all threads of the cluster with the same number of blocks.
-template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, int set, const Map<V>& own, float (&carry)[V], float (&start)[V],
-                                                          int blocks, int rank) {
-    const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        ex.warp[set][warp][0][v * 32 + lane] = own.A[v];
-        ex.warp[set][warp][1][v * 32 + lane] = -own.nC[v];
-        ex.warp[set][warp][2][v * 32 + lane] = own.u[v];
-    }
+// Called by all threads of the cluster in the same rounds.  A set is written again two rounds later: a block sends the maps of the round between
+// only when its warps have read this one's, and a block that receives all of those has finished the round before.
+template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsigned round, const Map<V>& own, float (&carry)[V], float (&start)[V],
+                                                          int blocks, int rank, bool& broken) {
+    const int warp = threadIdx.y, set = round & 1;
+    Affine<V> a;
+    a.from(own);
+    put<V>(ex.warp[set][warp], a);
     __syncthreads();
     if (blocks == 1) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float y = carry[v];
-            for (int w = 0; w < warps; ++w) {
-                if (w == warp) start[v] = y;
-                y = apply(fetch<V>(ex.warp[set][w], v * 32 + lane), y);
+        for (int w = 0; w < kMaxWarps; ++w) {
+            if (w == warp) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) start[v] = carry[v];
             }
-            carry[v] = y;
+            fetch<V>(a, ex.warp[set][w]);
+            a.apply(carry);
         }
         return;
     }
-    if (warp < blocks) {                                                    // this block's product goes to every block, one warp to each
+    const unsigned bar = smem_of(&ex.bar[set]);
+    if (warp == 0 && threadIdx.x == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(blocks * 3 * 32 * V * 4) : "memory");
+    Map<V> all;
+    Affine<V> before;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            Affine m = fetch<V>(ex.warp[set][0], v * 32 + lane);
-            for (int w = 1; w < warps; ++w) m = compose(m, fetch<V>(ex.warp[set][w], v * 32 + lane));
-            for (int to = warp; to < blocks; to += warps) {
-                peer_store(peer_of(smem_of(&ex.block[set][rank][0][v * 32 + lane]), to), m.A);
-                peer_store(peer_of(smem_of(&ex.block[set][rank][1][v * 32 + lane]), to), m.C);
-                peer_store(peer_of(smem_of(&ex.block[set][rank][2][v * 32 + lane]), to), m.u);
+    for (int w = 0; w < kMaxWarps; ++w) {
+        if (w == warp) before.from(all);
+        fetch<V>(a, ex.warp[set][w]);
+        a.follow(all);
+    }
+    a.from(all);
+    const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]);
+    for (int to = warp; to < blocks; to += (int)blockDim.y) {               // this block's map to every block, a warp to each
+        const unsigned there = peer_of(at, to), count = peer_of(bar, to);
+        send<V>(there, a.m, count);
+        send<V>(there + 32 * V * 4, a.k, count);
+        send<V>(there + 64 * V * 4, a.u, count);
+    }
+    const unsigned parity = (round >> 1) & 1;
+    if (!broken && !set_arrived(bar, parity)) broken = !await_set(bar, parity);
+    __syncwarp();
+    if (broken) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) carry[v] = __int_as_float(0x7fffffff);
+    }
+    for (int r0 = 0; r0 < blocks; r0 += 4) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (r0 + r == rank) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) start[v] = carry[v];
             }
+            fetch<V>(a, ex.block[set][r0 + r]);
+            a.apply(carry);
         }
     }
-    cluster_arrive();
-    cluster_wait();
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        float y = carry[v];
-        for (int r = 0; r < blocks; ++r) {
-            if (r == rank) start[v] = y;
-            y = apply(fetch<V>(ex.block[set][r], v * 32 + lane), y);
-        }
-        carry[v] = y;
-        y = start[v];
-        for (int w = 0; w < warp; ++w) y = apply(fetch<V>(ex.warp[set][w], v * 32 + lane), y);
-        start[v] = y;
-    }
+    before.apply(start);
 }
 
-// which channels and steps a thread works on
-struct Place { int seq, col, len, rank; bool on; };
+// Which channels and steps a thread works on.  Lanes behind the last channel do what the last one does, and write the same values to the same
+// places: a condition at each store costs more than the rest of the second run (1320 cycles a round of 16 steps instead of 520).
+struct Place { int seq, tile, col, lane, len, rank; unsigned slot; };      // tile: the first channel of the warp
 template <int V> __device__ __forceinline__ Place place(const RecArgs& p, int blocks) {
     const int tiles = (p.width + 32 * V - 1) / (32 * V), tile = blockIdx.x / blocks;
     Place q;
     q.rank = blockIdx.x - tile * blocks;
     q.seq = tile / tiles;
-    q.col = (tile - q.seq * tiles) * 32 * V + threadIdx.x * V;
-    q.on = q.col < p.width;
+    q.tile = (tile - q.seq * tiles) * 32 * V;
+    q.lane = min((int)threadIdx.x, (p.width - q.tile) / V - 1);
+    q.col = q.tile + q.lane * V;
     q.len = p.n_steps;
     if (p.lengths != nullptr) q.len = min(max(p.lengths[q.seq], 0), p.n_steps);
+    q.slot = q.rank * blockDim.y + threadIdx.y;
     return q;
 }
 
-// A warp's tile of one array: L steps of V channels a lane, from step t0 on (step: the stride; negative backwards in time), `n` of which exist; the
-// others hold `fill`
-template <typename T, int V, int L> __device__ __forceinline__ void load_tile(typename Word<T, V>::type (&w)[L], const T* p, long long step, int n, float fill) {
+template <bool B> struct Flag { static constexpr bool value = B; };
+
+// Where a warp finds its steps: a tile of N arrays, L steps of V channels a lane.
+//   STAGED: copied to shared memory 16 bytes at a time by asynchronous copies that run two rounds ahead (each warp its own two stages, so that
+//           no other warp has to be waited for), read from there as often as needed.  Rows of all arrays are multiples of 16 bytes from aligned pointers.
+//   else:   loaded into registers when the round starts.  For any alignment (V = 1), and for sequences of a round or two, where nothing runs ahead.
+// Step i of array k lies at base + off + i * step bytes: 32-bit offsets from an address that is the same for the whole block.
+template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
+constexpr int kStages = 2;
+template <typename T, int V, int L, int N, bool STAGED> struct Tile;
+template <typename T, int V, int L, int N> struct Tile<T, V, L, N, false> {
     using word = typename Word<T, V>::type;
-    if (n >= L) {
+    word w[N][L];
+    unsigned lane;
+    __device__ __forceinline__ void bind(char*, int l) { lane = l * (unsigned)sizeof(word); }
+    template <bool FULL> __device__ __forceinline__ void request(int, int k, const char* base, unsigned off, unsigned step, int lo, int hi, int) {
+        off += lane;
 #pragma unroll
-        for (int i = 0; i < L; ++i, p += step) w[i] = *(const word*)p;
-    } else {
-        const word none = word_of<T, V>(fill);
-#pragma unroll
-        for (int i = 0; i < L; ++i, p += step) {
-            w[i] = none;
-            if (i < n) w[i] = *(const word*)p;
+        for (int i = 0; i < L; ++i, off += step) {
+            w[k][i] = word_of<T, V>(0.f);
+            if (i >= lo && i < hi) w[k][i] = *(const word*)(base + off);
         }
     }
-}
+    __device__ __forceinline__ void commit() {}
+    __device__ __forceinline__ void wait() {}
+    __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
+};
+template <typename T, int V, int L, int N> struct Tile<T, V, L, N, true> {
+    using word = typename Word<T, V>::type;
+    static constexpr int kRow = kRowBytes<T, V>, kPieces = kRow / 16, kRows = 32 / kPieces;
+    static_assert(L % kRows == 0, "whole rows a copy");
+    char* at;
+    unsigned lane;
+    __device__ __forceinline__ void bind(char* smem, int l) {
+        at = smem + threadIdx.y * (kStages * N * L * kRow);
+        lane = l * (unsigned)sizeof(word);
+    }
+    // steps lo .. hi - 1 and `bytes` of a row exist; FULL: all of them
+    template <bool FULL> __device__ __forceinline__ void request(int stage, int k, const char* base, unsigned off, unsigned step, int lo, int hi, int bytes) {
+        const int piece = (threadIdx.x % kPieces) * 16;
+        int row = threadIdx.x / kPieces;
+        off += piece + row * step;
+        unsigned to = smem_of(at) + ((stage * N + k) * L + row) * kRow + piece;
+#pragma unroll
+        for (int j = 0; j < L / kRows; ++j, row += kRows, off += step * kRows, to += kRow * kRows)
+            if (FULL || (row >= lo && row < hi && piece < bytes)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(base + off) : "memory");
+    }
+    __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ void wait() {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+    }
+    __device__ __forceinline__ word get(int stage, int k, int i) const {
+        return *(const word*)(at + ((stage * N + k) * L + i) * kRow + lane);
+    }
+};
 
-template <typename T, int V, bool COUPLED, int L>
+template <typename T, int V, bool COUPLED, int L, bool STAGED>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const int blocks) {
     using W = Word<T, V>;
     using word = typename W::type;
+    extern __shared__ __align__(16) char staged[];
     __shared__ Exchange<V> ex;
     const Place q = place<V>(p, blocks);
-    if (blocks > 1) cluster_arrive();                       // nobody writes into a block that has not started
-    const T* x = (const T*)p.x + q.seq * p.in_seq + q.col;
-    const T* g = (const T*)p.gate + q.seq * p.in_seq + q.col;
-    T* out = (T*)p.out + q.seq * p.out_seq + q.col;
     const bool alone = blocks == 1 && blockDim.y == 1;
-    const int stride = blocks * (int)blockDim.y * L;
-    float carry[V];
+    if (!alone) exchange_begin<V>(ex, blocks);
+    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
+    const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es;
+    const unsigned in_at = q.tile * es + q.slot * L * in_step, out_at = q.col * es + q.slot * L * out_step;
+    const int row_bytes = (p.width - q.tile) * (int)es;
+    const char* x = (const char*)p.x + q.seq * p.in_seq * es;
+    const char* g = (const char*)p.gate + q.seq * p.in_seq * es;
+    char* out = (char*)p.out + q.seq * p.out_seq * es;
+    const long long in_round = (long long)stride * in_step, out_round = (long long)stride * out_step;
+    const long long state = (long long)q.seq * p.width + q.col;
+    float carry[V];                                         // -y when coupled
+    bool broken = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = p.y0 != nullptr && q.on ? p.y0[(long long)q.seq * p.width + q.col + v] : 0.f;
-    long long t0 = (q.rank * (int)blockDim.y + (int)threadIdx.y) * L;
-    // steps that do not exist keep the state: x = 0, gate = -inf
-    int n = q.on ? (int)max(0ll, min((long long)L, q.len - t0)) : 0;
-    word xw[L], gw[L];
-    load_tile<T, V, L>(xw, x + t0 * p.in_step, p.in_step, n, 0.f);
-    load_tile<T, V, L>(gw, g + t0 * p.in_step, p.in_step, n, -INFINITY);
+    for (int v = 0; v < V; ++v) {
+        carry[v] = p.y0 != nullptr ? p.y0[state + v] : 0.f;
+        if (COUPLED) carry[v] = -carry[v];
+    }
+    Tile<T, V, L, 2, STAGED> tile;
+    tile.bind(staged, q.lane);
+    // steps of this warp's tile that exist
+    auto count = [&](unsigned base) {
+        const unsigned t0 = base + q.slot * L;
+        return t0 < (unsigned)q.len ? (int)min((unsigned)L, (unsigned)q.len - t0) : 0;
+    };
+    auto request = [&](auto full, unsigned base, int stage) {
+        const int n = count(base);
+        tile.template request<full.value>(stage, 0, x, in_at, in_step, 0, n, row_bytes);
+        tile.template request<full.value>(stage, 1, g, in_at, in_step, 0, n, row_bytes);
+        tile.commit();
+        x += in_round; g += in_round;
+    };
+    if (STAGED)
+        for (int k = 0; k < kStages; ++k) request(Flag<false>(), k * stride, k);
     if (blocks > 1) cluster_wait();
-    int set = 0;
-    for (long long base = 0; base < q.len; base += stride, set ^= 1) {
+    unsigned round = 0;
+    // full: every step of the round exists; next: so does everything of the round that is requested
+    auto body = [&](auto full, auto next, unsigned base) {
         float nb[L][V], start[V];
-        word now[L];
+        const int stage = round % kStages, n = count(base);
+        if (!STAGED) request(Flag<false>(), base, 0);
+        tile.wait();
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            float f[V], slope;
-            W::get(gw[i], f);
+            float f[V], none[V];
+            W::get(tile.get(stage, 1, i), f);
+            negated_gate<T, V, false>(f, nb[i], none);
+            if (!full.value && i >= n) {                    // a step that does not exist keeps the state
 #pragma unroll
-            for (int v = 0; v < V; ++v) negated_gate<T>(f[v], nb[i][v], slope);
-            now[i] = COUPLED ? W::negate(xw[i]) : xw[i];
+                for (int v = 0; v < V; ++v) nb[i][v] = 0.f;
+            }
         }
-        // the next round's steps are on their way while this one's are summed
-        const int m = n;
-        T* const o = out + t0 * p.out_step;
-        t0 += stride;
-        n = q.on ? (int)max(0ll, min((long long)L, q.len - t0)) : 0;
-        load_tile<T, V, L>(xw, x + t0 * p.in_step, p.in_step, n, 0.f);
-        load_tile<T, V, L>(gw, g + t0 * p.in_step, p.in_step, n, -INFINITY);
+        auto x_of = [&](int i, float (&xs)[V]) {
+            W::get(tile.get(stage, 0, i), xs);
+            if (!full.value && i >= n) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) start[v] = carry[v];
+                for (int v = 0; v < V; ++v) xs[v] = 0.f;
+            }
+        };
         if (!alone) {
             Map<V> own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float xs[V];
-                W::get(now[i], xs);
+                x_of(i, xs);
                 own.decay(nb[i]);
                 step_forward<COUPLED, V>(own.u, nb[i], xs);
             }
-            exchange<V>(ex, set, own, carry, start, blocks, q.rank);
-        }
-        T* to = o;
+            exchange<V>(ex, round, own, carry, start, blocks, q.rank, broken);
+        } else {
 #pragma unroll
-        for (int i = 0; i < L; ++i, to += p.out_step) {
-            float xs[V];
-            W::get(now[i], xs);
-            step_forward<COUPLED, V>(start, nb[i], xs);
-            if (i < m) *(word*)to = W::put(start);
+            for (int v = 0; v < V; ++v) start[v] = carry[v];
         }
+        unsigned at = out_at;
+#pragma unroll
+        for (int i = 0; i < L; ++i, at += out_step) {
+            float xs[V];
+            x_of(i, xs);
+            step_forward<COUPLED, V>(start, nb[i], xs);
+            if (full.value || i < n) *(word*)(out + at) = COUPLED ? W::negate(W::put(start)) : W::put(start);
+        }
+        out += out_round;
         if (alone) {
 #pragma unroll
             for (int v = 0; v < V; ++v) carry[v] = start[v];
         }
+        if (STAGED) {
+            __syncwarp();                                   // all lanes have read this stage
+            request(next, base + kStages * stride, stage);
+        }
+        ++round;
+    };
+    unsigned base = 0;
+    if (STAGED) {
+        if (row_bytes >= kRowBytes<T, V>)
+            for (; (unsigned long long)base + (kStages + 1) * stride <= (unsigned)q.len; base += stride) body(Flag<true>(), Flag<true>(), base);
+        for (; (unsigned long long)base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), Flag<false>(), base);
     }
-    if (p.last != nullptr && q.on && q.rank == 0 && threadIdx.y == 0) {
+    for (; base < (unsigned)q.len; base += stride) body(Flag<false>(), Flag<false>(), base);
+    if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) p.last[(long long)q.seq * p.width + q.col + v] = carry[v];
+        for (int v = 0; v < V; ++v) p.last[state + v] = COUPLED ? -carry[v] : carry[v];
     }
+    if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written
 }
 
-// Steps counted from the end: step i of a warp is time t0 - i
-template <typename T, int V, bool COUPLED, int L>
+// Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
+// Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
+template <typename T, int V, bool COUPLED, int L, bool STAGED>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const int blocks) {
     using W = Word<T, V>;
     using word = typename W::type;
+    extern __shared__ __align__(16) char staged[];
     __shared__ Exchange<V> ex;
     const Place q = place<V>(p, blocks);
-    if (blocks > 1) cluster_arrive();
-    const long long in0 = q.seq * p.in_seq + q.col, out0 = q.seq * p.out_seq + q.col, w0 = (long long)q.seq * p.width + q.col;
-    const T *x = (const T*)p.x + in0, *g = (const T*)p.gate + in0, *y = (const T*)p.y + out0, *dy = (const T*)p.dy + out0;
-    T *dx = (T*)p.out + in0, *dg = (T*)p.out2 + in0;
     const bool alone = blocks == 1 && blockDim.y == 1;
-    const int stride = blocks * (int)blockDim.y * L;
+    if (!alone) exchange_begin<V>(ex, blocks);
+    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
+    // offsets count down from the last time of the round
+    const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es, back = (stride - 1) - q.slot * L;
+    const unsigned in_at = q.tile * es + back * in_step, out_at = q.tile * es + back * out_step, to_at = q.col * es + back * in_step;
+    const int row_bytes = (p.width - q.tile) * (int)es;
+    const unsigned skipped = p.n_steps - q.len;             // steps at the start of the count that do not exist
+    unsigned base = skipped / stride * stride;              // rounds that lie behind the sequence are passed over
+    const long long in_round = (long long)stride * in_step, out_round = (long long)stride * out_step;
+    const long long first_in = q.seq * p.in_seq * es + ((long long)p.n_steps - stride - base) * in_step;
+    const long long first_out = q.seq * p.out_seq * es + ((long long)p.n_steps - stride - base) * out_step;
+    const char *x = (const char*)p.x + first_in, *g = (const char*)p.gate + first_in, *y = (const char*)p.y + first_out - out_step, *dy = (const char*)p.dy + first_out;
+    char *dx = (char*)p.out + first_in, *dg = (char*)p.out2 + first_in;
+    const long long state = (long long)q.seq * p.width + q.col;
     float carry[V];
-    bool bad = false;
+    bool broken = false;
+    Largest<T> largest;
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr && q.on ? p.dyT[w0 + v] : 0.f;
-    long long t0 = (long long)q.len - 1 - (q.rank * (int)blockDim.y + (int)threadIdx.y) * L;
-    int n = q.on ? (int)max(0ll, min((long long)L, t0 + 1)) : 0;
-    word xw[L], gw[L], dw[L], yw[L];
-    auto load = [&]() {
-        load_tile<T, V, L>(gw, g + t0 * p.in_step, -p.in_step, n, -INFINITY);
-        load_tile<T, V, L>(dw, dy + t0 * p.out_step, -p.out_step, p.dy != nullptr ? n : 0, 0.f);
-        if (COUPLED) load_tile<T, V, L>(xw, x + t0 * p.in_step, -p.in_step, n, 0.f);
-        load_tile<T, V, L>(yw, y + (t0 - 1) * p.out_step, -p.out_step, (int)min((long long)n, t0), 0.f);      // the states in front of the steps
+    for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr ? p.dyT[state + v] : 0.f;
+    Tile<T, V, L, COUPLED ? 4 : 3, STAGED> tile;
+    tile.bind(staged, q.lane);
+    // the tile's steps lo .. hi - 1 exist
+    auto range = [&](unsigned base, int& lo, int& hi) {
+        const unsigned first = base + q.slot * L;
+        lo = first < skipped ? (int)min((unsigned)L, skipped - first) : 0;
+        hi = first < (unsigned)p.n_steps ? (int)min((unsigned)L, p.n_steps - first) : 0;
     };
-    load();
+    auto request = [&](auto full, unsigned base, int stage) {
+        int lo, hi;
+        range(base, lo, hi);
+        const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;         // time 0 has no stored state in front of it
+        tile.template request<full.value>(stage, 0, g, in_at, 0u - in_step, lo, hi, row_bytes);
+        if (p.dy != nullptr) tile.template request<full.value>(stage, 1, dy, out_at, 0u - out_step, lo, hi, row_bytes);
+        tile.template request<full.value>(stage, 2, y, out_at, 0u - out_step, lo, before, row_bytes);
+        if constexpr (COUPLED) tile.template request<full.value>(stage, 3, x, in_at, 0u - in_step, lo, hi, row_bytes);
+        tile.commit();
+        x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
+    };
+    if (STAGED)
+        for (int k = 0; k < kStages; ++k) request(Flag<false>(), base + k * stride, k);
     if (blocks > 1) cluster_wait();
-    int set = 0;
-    for (long long base = 0; base < q.len; base += stride, set ^= 1) {
+    unsigned round = 0;
+    const bool no_dy = p.dy == nullptr;
+    auto body = [&](auto full, auto next) {
         float nb[L][V], slope[L][V], start[V];
-        word now[L], before[L], given[L];
+        const int stage = round % kStages;
+        int lo, hi;
+        range(base, lo, hi);
+        const int zero = (int)(p.n_steps - 1 - (base + q.slot * L));                            // index of time 0
+        if (!STAGED) request(Flag<false>(), base, 0);
+        tile.wait();
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             float f[V];
-            W::get(gw[i], f);
+            W::get(tile.get(stage, 0, i), f);
+            negated_gate<T, V, true>(f, nb[i], slope[i]);
+            if (!full.value && (i < lo || i >= hi)) {                                           // a step that does not exist keeps the adjoint
 #pragma unroll
-            for (int v = 0; v < V; ++v) negated_gate<T>(f[v], nb[i][v], slope[i][v]);
-            now[i] = xw[i]; before[i] = yw[i]; given[i] = dw[i];
+                for (int v = 0; v < V; ++v) nb[i][v] = 0.f;
+            }
         }
-        const int m = n, first = t0 < L ? (int)t0 : L;                       // index of time 0
-        const long long at = t0 * p.in_step;
-        t0 -= stride;
-        n = q.on ? (int)max(0ll, min((long long)L, t0 + 1)) : 0;
-        load();
+        auto dy_of = [&](int i, float (&d)[V]) {
+            W::get(tile.get(stage, 1, i), d);
+            if (no_dy || (!full.value && (i < lo || i >= hi))) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) start[v] = carry[v];
+                for (int v = 0; v < V; ++v) d[v] = 0.f;
+            }
+        };
         if (!alone) {
             Map<V> own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float d[V], l[V];
-                W::get(given[i], d);
+                dy_of(i, d);
                 own.decay(nb[i]);
                 Ops<V>::add(l, own.u, d);
                 Ops<V>::fma(own.u, nb[i], l, l);
             }
-            exchange<V>(ex, set, own, carry, start, blocks, q.rank);
+            exchange<V>(ex, round, own, carry, start, blocks, q.rank, broken);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) start[v] = carry[v];
         }
-        T *ox = dx + at, *og = dg + at;
+        unsigned at = to_at;
 #pragma unroll
-        for (int i = 0; i < L; ++i, ox -= p.in_step, og -= p.in_step) {
-            float xs[V], ys[V], d[V], l[V], gx[V], gg[V];
-            W::get(given[i], d);
-            W::get(before[i], ys);
-            if (i == first && p.y0 != nullptr && q.on) {
+        for (int i = 0; i < L; ++i, at -= in_step) {
+            float ys[V], d[V], l[V], gx[V], gg[V];
+            dy_of(i, d);
+            W::get(tile.get(stage, 2, i), ys);
+            if (!full.value && i == zero) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) ys[v] = p.y0[w0 + v];
+                for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[state + v] : 0.f;
             }
             Ops<V>::add(l, start, d);
             Ops<V>::fma(start, nb[i], l, l);
-            if (COUPLED) W::get(now[i], xs);
+            Ops<V>::mul(gg, slope[i], l);
+            if constexpr (COUPLED) {
+                float xs[V], minus[V];
+                W::get(tile.get(stage, 3, i), xs);
+                Ops<V>::mul(gx, nb[i], l);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                gx[v] = COUPLED ? -nb[i][v] * l[v] : l[v];
-                gg[v] = slope[i][v] * l[v] * (COUPLED ? xs[v] - ys[v] : -ys[v]);
+                for (int v = 0; v < V; ++v) minus[v] = -1.f;
+                Ops<V>::fma(ys, ys, minus, xs);
             }
-            if (i < m) {
-                const word wx = W::put(gx), wg = W::put(gg);
-                bad |= word_nonfinite<T, V>(wx) || word_nonfinite<T, V>(wg);
-                *(word*)ox = wx;
-                *(word*)og = wg;
+            Ops<V>::mul(gg, gg, ys);
+            if (full.value || (i >= lo && i < hi)) {
+                const word wx = COUPLED ? W::negate(W::put(gx)) : W::put(l), wg = COUPLED ? W::put(gg) : W::negate(W::put(gg));
+                if (p.flag != nullptr) { see<T, V>(largest, wx); see<T, V>(largest, wg); }
+                *(word*)(dx + at) = wx;
+                *(word*)(dg + at) = wg;
             }
         }
         if (alone) {
 #pragma unroll
             for (int v = 0; v < V; ++v) carry[v] = start[v];
         }
+        dx -= in_round; dg -= in_round;
+        if (STAGED) {
+            __syncwarp();
+            request(next, base + kStages * stride, stage);
+        }
+        base += stride;
+        ++round;
+    };
+    // (a full round does not hold time 0)
+    if (STAGED) {
+        if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>(), Flag<false>());
+        if (row_bytes >= kRowBytes<T, V>)
+            while ((unsigned long long)base + (kStages + 1) * stride < (unsigned)p.n_steps) body(Flag<true>(), Flag<true>());
+        while ((unsigned long long)base + stride < (unsigned)p.n_steps) body(Flag<true>(), Flag<false>());
     }
-    if (p.last != nullptr && q.on && q.rank == 0 && threadIdx.y == 0) {
+    while (base < (unsigned)p.n_steps) body(Flag<false>(), Flag<false>());
+    if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) p.last[w0 + v] = carry[v];
+        for (int v = 0; v < V; ++v) p.last[state + v] = carry[v];
     }
-    warp_flag_or(p.flag, bad);
+    warp_flag_or(p.flag, largest.nonfinite());
+    if (blocks > 1) { cluster_arrive(); cluster_wait(); }
 }
 
 // How a call is spread over the GPU: warps along the time axis of a block, then blocks of a cluster, until every SM has its warps or no steps are left
 struct Shape { int warps, blocks; long long tiles; };
-Shape shape_of(const mpode_recurrence_desc& d, int lanes_width, int steps_of_warp) {
+// a round's bytes have to stay within 32-bit offsets
+bool round_fits(const RecArgs& a, long long steps, int es) {
+    const long long step = a.in_step > a.out_step ? a.in_step : a.out_step;
+    return step < (1ll << 32) && (steps * step + a.width) * es < (1ll << 32);
+}
+Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int lanes_width, int steps_of_warp) {
     Shape s;
     s.tiles = (long long)d.n_seq * ((d.width + lanes_width - 1) / lanes_width);
     s.warps = s.blocks = 1;
     while (s.warps < kMaxWarps && (long long)s.warps * steps_of_warp < d.n_steps) s.warps *= 2;
     while (s.blocks < kMaxCluster && s.tiles * s.blocks < 148 && (long long)s.blocks * s.warps * steps_of_warp < d.n_steps) s.blocks *= 2;
+    while (s.blocks > 1 && !round_fits(a, (long long)s.blocks * s.warps * steps_of_warp, (int)low_size(d.low))) s.blocks /= 2;
+    while (s.warps > 1 && !round_fits(a, (long long)s.warps * steps_of_warp, (int)low_size(d.low))) s.warps /= 2;
     return s;
 }
 
-cudaError_t launch(void (*kernel)(const RecArgs, const int), const RecArgs& a, const Shape& s, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(const RecArgs, const int), const RecArgs& a, const Shape& s, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.tiles * s.blocks));
     cfg.blockDim = dim3(32, s.warps);
     cfg.stream = st;
+    cfg.dynamicSmemBytes = smem;
+    if (smem > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)s.blocks;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = s.blocks > 1 ? 1 : 0;
+    if (s.blocks > 8) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     return cudaLaunchKernelEx(&cfg, kernel, a, s.blocks);
 }
 
 template <typename T, int V> constexpr int kForwardSteps = sizeof(T) * V > 4 ? 8 : 16;
 template <typename T, int V> constexpr int kBackwardSteps = sizeof(T) * V > 4 ? 4 : 8;
 
-template <typename T, int V> cudaError_t run_forward(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
-    constexpr int L = kForwardSteps<T, V>;
-    const Shape s = shape_of(d, 32 * V, L);
-    return d.coupled ? launch(recurrence_forward_kernel<T, V, true, L>, a, s, st) : launch(recurrence_forward_kernel<T, V, false, L>, a, s, st);
+// rows of multiples of 16 bytes from aligned pointers everywhere
+bool pieces_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
+    const long long es = (long long)low_size(d.low);
+    if (((a.in_step | a.in_seq | a.out_step | a.out_seq | d.width) * es) & 15) return false;
+    const void* const all[] = {a.x, a.gate, a.y, a.dy};
+    for (const void* q : all)
+        if (misaligned(q, 16)) return false;
+    return true;
 }
-template <typename T, int V> cudaError_t run_backward(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
-    constexpr int L = kBackwardSteps<T, V>;
-    const Shape s = shape_of(d, 32 * V, L);
-    return d.coupled ? launch(recurrence_backward_kernel<T, V, true, L>, a, s, st) : launch(recurrence_backward_kernel<T, V, false, L>, a, s, st);
+template <typename T, int V, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
+    constexpr int L = BACKWARD ? kBackwardSteps<T, V> : kForwardSteps<T, V>;
+    const Shape s = shape_of(d, a, 32 * V, L);
+    if constexpr (V == 2) {
+        if (d.n_steps > 2 * s.warps * s.blocks * L && pieces_fit(d, a)) {
+            constexpr int arrays = BACKWARD ? (COUPLED ? 4 : 3) : 2;
+            const size_t smem = (size_t)s.warps * kStages * arrays * L * kRowBytes<T, V>;
+            if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, true>, a, s, smem, st);
+            else return launch(recurrence_forward_kernel<T, V, COUPLED, L, true>, a, s, smem, st);
+        }
+    }
+    if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, false>, a, s, 0, st);
+    else return launch(recurrence_forward_kernel<T, V, COUPLED, L, false>, a, s, 0, st);
+}
+template <bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, bool two, cudaStream_t st) {
+    return with_low(d.low, [&](auto t) {
+        using T = decltype(t);
+        if (two) return d.coupled ? run<T, 2, true, BACKWARD>(d, a, st) : run<T, 2, false, BACKWARD>(d, a, st);
+        return d.coupled ? run<T, 1, true, BACKWARD>(d, a, st) : run<T, 1, false, BACKWARD>(d, a, st);
+    });
 }
 
 // the checks that both directions share; fills in strides that are zero
@@ -485,6 +769,9 @@ mpode_status check(const mpode_recurrence_desc* d, RecArgs& a) {
                            (a.out_seq <= N * a.out_step + lo - 1 && a.out_step <= S * a.out_seq + lo - 1)))
         return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: the strides make rows overlap");
     a.n_seq = d->n_seq; a.n_steps = d->n_steps; a.width = d->width;
+    if (d->n_steps <= 1) a.in_step = a.out_step = lo;
+    if (!round_fits(a, 16, (int)low_size(d->low)))
+        return operator_fail(MPODE_ERR_UNSUPPORTED, "recurrence: step strides %lld and %lld (16 steps have to lie within 4 GB)", a.in_step, a.out_step);
     return MPODE_OK;
 }
 // two channels an access need even widths and strides and rows aligned to two elements
@@ -541,12 +828,7 @@ mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* c
     if (desc->n_steps > 0 && (!x_dev || !gate_dev || !y_dev)) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_recurrence_forward: null pointer argument");
     const mpode_status off = check_pointers(*desc, a);
     if (off != MPODE_OK) return off;
-    const cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e;
-    if (desc->low == MPODE_F32) e = words_fit(*desc, a) ? run_forward<float, 2>(*desc, a, st) : run_forward<float, 1>(*desc, a, st);
-    else if (desc->low == MPODE_BF16) e = words_fit(*desc, a) ? run_forward<__nv_bfloat16, 2>(*desc, a, st) : run_forward<__nv_bfloat16, 1>(*desc, a, st);
-    else e = words_fit(*desc, a) ? run_forward<__half, 2>(*desc, a, st) : run_forward<__half, 1>(*desc, a, st);
-    return operator_launched(e, "mpode_recurrence_forward");
+    return operator_launched(run<false>(*desc, a, words_fit(*desc, a), (cudaStream_t)cuda_stream), "mpode_recurrence_forward");
 }
 
 mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
@@ -562,12 +844,7 @@ mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* 
         return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_recurrence_backward: null pointer argument");
     const mpode_status off = check_pointers(*desc, a);
     if (off != MPODE_OK) return off;
-    const cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e;
-    if (desc->low == MPODE_F32) e = words_fit(*desc, a) ? run_backward<float, 2>(*desc, a, st) : run_backward<float, 1>(*desc, a, st);
-    else if (desc->low == MPODE_BF16) e = words_fit(*desc, a) ? run_backward<__nv_bfloat16, 2>(*desc, a, st) : run_backward<__nv_bfloat16, 1>(*desc, a, st);
-    else e = words_fit(*desc, a) ? run_backward<__half, 2>(*desc, a, st) : run_backward<__half, 1>(*desc, a, st);
-    return operator_launched(e, "mpode_recurrence_backward");
+    return operator_launched(run<true>(*desc, a, words_fit(*desc, a), (cudaStream_t)cuda_stream), "mpode_recurrence_backward");
 }
 
 }  // extern "C"

@@ -49,241 +49,340 @@ __device__ __forceinline__ Lane lane_of(int width, int blocks) {
 
 // Sums over a row's threads, the same bits in all of them.  One warp: shuffles.  One block: partial sums of its warps in shared memory.
 // A cluster: every warp's into every block's shared memory.  Two sets of partial sums in turn, so that one barrier a sum does.
+constexpr int kSlots = kMaxBlocks * (kMaxThreads / 32);
 template <int N> struct RowSum {
-    float part[2][kMaxBlocks * (kMaxThreads / 32)][N];
+    float part[2][N][kSlots];
 };
 template <int N> __device__ __forceinline__ void row_sum(float (&v)[N], const Lane& q, RowSum<N>& s, int& set) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (N == 1) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+        for (int o = 16; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    } else {
+        // both at once: the lower lanes take over the first sum, the upper ones the second
+        const float give = lane < 16 ? v[1] : v[0];
+        float mine = lane < 16 ? v[0] : v[1];
+        mine += __shfl_xor_sync(0xffffffffu, give, 16);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        const float other = __shfl_xor_sync(0xffffffffu, mine, 16);
+        v[0] = lane < 16 ? mine : other;
+        v[1] = lane < 16 ? other : mine;
+    }
     if (q.warps * q.blocks == 1) return;
-    const int lane = threadIdx.x & 31, slot = q.rank * q.warps + q.warp, slots = q.blocks * q.warps;
+    const int slot = q.rank * q.warps + q.warp, slots = q.blocks * q.warps;
     if (q.blocks == 1) {
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) s.part[set][slot][i] = v[i];
-        }
+        if (lane < N) s.part[set][lane][slot] = N == 1 ? v[0] : lane == 0 ? v[0] : v[N - 1];
         __syncthreads();
     } else {
         if (lane < q.blocks) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 unsigned at;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_of(&s.part[set][slot][i])), "r"(lane));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_of(&s.part[set][i][slot])), "r"(lane));
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v[i]) : "memory");
             }
         }
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
+    // four at a time (the number of warps of a block is a power of two; a pair of them fills a half)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = lane < slots ? s.part[set][lane][i] : 0.f;
-        if (lane + 32 < slots) v[i] += s.part[set][lane + 32][i];
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    if (slots < 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = s.part[set][i][0] + s.part[set][i][1];
+    } else {
+#pragma unroll 4
+        for (int k = 0; k < slots; k += 4)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float4 f = *reinterpret_cast<const float4*>(&s.part[set][i][k]);
+                v[i] += (f.x + f.y) + (f.z + f.w);
+            }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     set ^= 1;
 }
 
-template <bool VEC> __device__ __forceinline__ void load_weights(const float* w, int col, int n, float (&f)[8]) {
-    if (w == nullptr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 1.f;
-    } else load8<float, VEC>(w + col, n, f);
+template <bool VEC> __device__ __forceinline__ void load_weights(const float* w, const Lane& q, Oct& o) {
+    if (w == nullptr) o.fill(1.f);
+    else load8<float, VEC>(w + q.col, q.n, o);
 }
+__device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
 
 // mean and 1 / deviation of a row whose elements lie in the threads' registers (zero where none exist)
-__device__ __forceinline__ void row_stats(const float (&f)[8], int kind, float eps, const Lane& q, int width, RowSum<1>& s, int& set, float& mean, float& rstd) {
+template <bool CENTER> __device__ __forceinline__ void row_stats(const Oct& f, int kind, float eps, const Lane& q, int width, RowSum<1>& s, int& set, float& mean,
+                                                                 float& rstd) {
     mean = 0.f;
     rstd = 1.f;
     if (kind == MPODE_NORM_NONE) return;
     const float inv = 1.f / (float)width;
-    if (kind == MPODE_NORM_MEANVAR) {
-        float v[1] = {0.f};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[0] += f[i];
+    if (CENTER && kind == MPODE_NORM_MEANVAR) {
+        float v[1] = {f.sum()};
         row_sum<1>(v, q, s, set);
         mean = v[0] * inv;
     }
-    float v[1] = {0.f};
+    float2 sq = pair(0.f);
+    const float2 less = pair(-mean);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float d = i < q.n ? f[i] - mean : 0.f;
-        v[0] = fmaf(d, d, v[0]);
+    for (int j = 0; j < 4; ++j) {
+        float2 d = f.v[j];
+        if (CENTER) {
+            d = __fadd2_rn(d, less);
+            if (2 * j >= q.n) d.x = 0.f;
+            if (2 * j + 1 >= q.n) d.y = 0.f;
+        }
+        sq = __ffma2_rn(d, d, sq);
     }
+    float v[1] = {sq.x + sq.y};
     row_sum<1>(v, q, s, set);
     rstd = rsqrtf(fmaf(v[0], inv, eps));
 }
 
-// sigmoid and its slope, both without cancellation
-__device__ __forceinline__ float gate_of(float g, float& slope) {
-    const float e = expf(-fabsf(g)), big = __fdividef(1.f, 1.f + e), small = e * big;
-    slope = small * big;
-    return g < 0.f ? small : big;
+// sigmoid and its slope sig (1 - sig) = e sig^2 with e = exp(-g).  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the
+// argument's rounding adds |g| 2^-24); the exponent is kept below 2^126, so that e sig^2 is finite.
+template <typename T, bool SLOPE> __device__ __forceinline__ float2 gate_of(float2 g, float2& slope) {
+    float2 e, s;
+    if constexpr (sizeof(T) == 4) {
+        e = make_float2(expf(-g.x), expf(-g.y));
+        s = make_float2(__fdividef(1.f, 1.f + e.x), __fdividef(1.f, 1.f + e.y));
+        if (SLOPE) slope = make_float2(s.x * (e.x > 1.f ? 1.f - s.x : e.x * s.x), s.y * (e.y > 1.f ? 1.f - s.y : e.y * s.y));
+    } else {
+        e = __fmul2_rn(g, pair(-1.4426950408889634f));
+        if (SLOPE) {
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(126.f));
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(126.f));
+        }
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+        const float2 d = __fadd2_rn(e, pair(1.f));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
+        if (SLOPE) slope = __fmul2_rn(__fmul2_rn(s, s), e);
+    }
+    return s;
 }
 
-template <typename T, bool VEC> __global__ void __launch_bounds__(kMaxThreads) residual_forward_kernel(const ResArgs p, const int blocks) {
-    __shared__ RowSum<1> sums;
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// CENTER: one of the norms takes the mean away
+template <typename T, bool VEC, bool CENTER> __global__ void __launch_bounds__(kMaxThreads) residual_forward_kernel(const ResArgs p, const int blocks) {
+    __shared__ __align__(16) RowSum<1> sums;
     const Lane q = lane_of(p.width, blocks);
     int set = 0;
-    if (blocks > 1) {                                       // nobody writes into a block that has not started
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (blocks > 1) cluster_sync();                         // nobody writes into a block that has not started
     const long long step_rows = (long long)(gridDim.x / blocks) * q.groups;
-    const uint64_t seed = p.drop.threshold ? p.drop.rng[0] : 0, step = p.drop.threshold ? p.drop.rng[1] : 0;
+    const uint64_t seed = p.drop.on ? p.drop.rng[0] : 0, step = p.drop.on ? p.drop.rng[1] : 0;
     const int groups_row = (p.width + 7) / 8;
-    for (long long row = (long long)(blockIdx.x / blocks) * q.groups + q.group; row < p.rows; row += step_rows) {
-        float y[8], mean_u = 0.f, rstd_u = 1.f, mean_y, rstd_y;
-        load8<float, VEC>(p.y + row * p.ld_y + q.col, q.n, y);
+    long long row = (long long)(blockIdx.x / blocks) * q.groups + q.group;
+    // the next row is on its way while this one's sums meet
+    Raw8<float> yr;
+    Raw8<T> ur, gr;
+    auto request = [&](long long r) {
+        load_raw<float, VEC>(p.y + r * p.ld_y + q.col, q.n, yr);
+        if (p.u != nullptr) load_raw<T, VEC>((const T*)p.u + r * p.ld_u + q.col, q.n, ur);
+        if (p.gate != nullptr) load_raw<T, VEC>((const T*)p.gate + r * p.ld_gate + q.col, q.n, gr);
+    };
+    if (row < p.rows) request(row);
+    for (; row < p.rows; row += step_rows) {
+        float mean_u = 0.f, rstd_u = 1.f, mean_y = 0.f, rstd_y = 1.f;
+        Oct y, u, g;
+        unpack<float>(yr, y);
+        if (p.u != nullptr) unpack<T>(ur, u);
+        if (p.gate != nullptr) unpack<T>(gr, g);
+        if (row + step_rows < p.rows) request(row + step_rows);
         if (p.u != nullptr) {
-            float u[8], w[8], c[8];
-            load8<T, VEC>((const T*)p.u + row * p.ld_u + q.col, q.n, u);
-            float g[8];
-            if (p.gate != nullptr) load8<T, VEC>((const T*)p.gate + row * p.ld_gate + q.col, q.n, g);
-            row_stats(u, p.post, p.eps, q, p.width, sums, set, mean_u, rstd_u);
-            load_weights<VEC>(p.w_post, q.col, q.n, w);
-            load_weights<VEC>(p.scale, q.col, q.n, c);
-            uint32_t keep = 0xffu;
-            if (p.drop.threshold) keep = keep_bits((uint64_t)row * groups_row + q.col / 8, seed, step, p.drop.site, p.drop.threshold);
+            Oct w, c;
+            Kept keep;
+            if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
+            row_stats<CENTER>(u, p.post, p.eps, q, p.width, sums, set, mean_u, rstd_u);
+            load_weights<VEC>(p.w_post, q, w);
+            load_weights<VEC>(p.scale, q, c);
+            const float2 less = pair(-mean_u), r = pair(rstd_u), h = pair(p.h * p.drop.scale);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v = (u[i] - mean_u) * rstd_u * w[i], slope;
-                if (p.gate != nullptr) v *= gate_of(g[i], slope);
-                v *= p.h * p.drop.scale * c[i];
-                if ((keep >> i) & 1u) y[i] += v;
+            for (int j = 0; j < 4; ++j) {
+                float2 v = u.v[j], slope;
+                if (CENTER) v = __fadd2_rn(v, less);
+                v = __fmul2_rn(__fmul2_rn(v, r), w.v[j]);
+                if (p.gate != nullptr) v = __fmul2_rn(v, gate_of<T, false>(g.v[j], slope));
+                const float2 k = __fmul2_rn(h, c.v[j]);
+                if (p.drop.on) {
+                    v = __fmul2_rn(v, k);
+                    if (!keep[2 * j]) v.x = 0.f;
+                    if (!keep[2 * j + 1]) v.y = 0.f;
+                    y.v[j] = __fadd2_rn(y.v[j], v);
+                } else y.v[j] = __ffma2_rn(v, k, y.v[j]);
             }
+            if (!VEC) {                                      // columns that do not exist stay zero in the sums below
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (2 * j >= q.n) y.v[j].x = 0.f;
+                    if (2 * j + 1 >= q.n) y.v[j].y = 0.f;
+                }
+            } else if (q.n <= 0) y.fill(0.f);
         }
         if (p.y_out != nullptr) store8<float, VEC>(p.y_out + row * p.ld_y + q.col, q.n, y);
-        mean_y = 0.f; rstd_y = 1.f;
         if (p.z != nullptr) {
-            float w[8];
-            row_stats(y, p.pre, p.eps, q, p.width, sums, set, mean_y, rstd_y);
-            load_weights<VEC>(p.w_pre, q.col, q.n, w);
+            Oct w;
+            row_stats<CENTER>(y, p.pre, p.eps, q, p.width, sums, set, mean_y, rstd_y);
+            load_weights<VEC>(p.w_pre, q, w);
+            const float2 less = pair(-mean_y), r = pair(rstd_y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = (y[i] - mean_y) * rstd_y * w[i];
+            for (int j = 0; j < 4; ++j) {
+                if (CENTER) y.v[j] = __fadd2_rn(y.v[j], less);
+                y.v[j] = __fmul2_rn(__fmul2_rn(y.v[j], r), w.v[j]);
+            }
             store8<T, VEC>((T*)p.z + row * p.ld_z + q.col, q.n, y);
         }
         if (p.stats != nullptr && q.rank == 0 && threadIdx.x == 0)
             reinterpret_cast<float4*>(p.stats)[row] = make_float4(mean_u, rstd_u, mean_y, rstd_y);
     }
-    if (blocks > 1) {                                       // nobody leaves while its shared memory may be written
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (blocks > 1) cluster_sync();                         // nobody leaves while its shared memory may be written
 }
 
 // With n' the normalised y', n that of u, and t the cotangent of the step's term:
 //   a = dy' + r' (w dz - n' mean(w dz n') - mean(w dz)),  dw_pre += dz n';   t = drop(a), dscale += h t v sig, with v = w_post n;
 //   t <- h scale t, dgate = t v sig', t <- t sig, dw_post += t n, du = r (w t - n mean(w t n) - mean(w t)); the means of w dz and w t only for MEANVAR
-template <typename T, bool VEC> __global__ void __launch_bounds__(kMaxThreads, 1) residual_backward_kernel(const ResArgs p, const int blocks) {
-    __shared__ RowSum<2> sums;
+template <typename T, bool VEC, bool CENTER> __global__ void __launch_bounds__(kMaxThreads, 1) residual_backward_kernel(const ResArgs p, const int blocks) {
+    constexpr int N = CENTER ? 2 : 1;
+    __shared__ __align__(16) RowSum<N> sums;
     const Lane q = lane_of(p.width, blocks);
     int set = 0;
-    if (blocks > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (blocks > 1) cluster_sync();
     const long long step_rows = (long long)(gridDim.x / blocks) * q.groups;
-    const uint64_t seed = p.drop.threshold ? p.drop.rng[0] : 0, step = p.drop.threshold ? p.drop.rng[1] : 0;
+    const uint64_t seed = p.drop.on ? p.drop.rng[0] : 0, step = p.drop.on ? p.drop.rng[1] : 0;
     const int groups_row = (p.width + 7) / 8;
     const float inv = 1.f / (float)p.width;
-    float gw_post[8], gscale[8], gw_pre[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) gw_post[i] = gscale[i] = gw_pre[i] = 0.f;
-    bool bad = false;
-    for (long long row = (long long)(blockIdx.x / blocks) * q.groups + q.group; row < p.rows; row += step_rows) {
-        float a[8], w[8], st[4] = {0.f, 1.f, 0.f, 1.f};
-        if (p.stats != nullptr) {
-            const float4 f = reinterpret_cast<const float4*>(p.stats)[row];
-            st[0] = f.x; st[1] = f.y; st[2] = f.z; st[3] = f.w;
-        }
-        float u[8], g[8];
-        if (p.u != nullptr) {
-            load8<T, VEC>((const T*)p.u + row * p.ld_u + q.col, q.n, u);
-            if (p.gate != nullptr) load8<T, VEC>((const T*)p.gate + row * p.ld_gate + q.col, q.n, g);
-        }
-        if (p.dy != nullptr) load8<float, VEC>(p.dy + row * p.ld_y + q.col, q.n, a);
-        else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = 0.f;
-        }
+    const bool exists = q.n > 0;
+    Oct gw_post, gscale, gw_pre;
+    gw_post.fill(0.f); gscale.fill(0.f); gw_pre.fill(0.f);
+    Largest<T> largest;
+    long long row = (long long)(blockIdx.x / blocks) * q.groups + q.group;
+    Raw8<float> yr, ar;
+    Raw8<T> ur, gr, dr;
+    float4 stats = make_float4(0.f, 1.f, 0.f, 1.f);
+    auto request = [&](long long r) {
+        if (p.stats != nullptr) stats = reinterpret_cast<const float4*>(p.stats)[r];
         if (p.dz != nullptr) {
-            float y[8], d[8], m[2] = {0.f, 0.f};
-            load8<float, VEC>(p.y + row * p.ld_y + q.col, q.n, y);
-            load8<T, VEC>((const T*)p.dz + row * p.ld_z + q.col, q.n, d);
-            load_weights<VEC>(p.w_pre, q.col, q.n, w);
+            load_raw<float, VEC>(p.y + r * p.ld_y + q.col, q.n, yr);
+            load_raw<T, VEC>((const T*)p.dz + r * p.ld_z + q.col, q.n, dr);
+        }
+        if (p.dy != nullptr) load_raw<float, VEC>(p.dy + r * p.ld_y + q.col, q.n, ar);
+        if (p.u != nullptr) load_raw<T, VEC>((const T*)p.u + r * p.ld_u + q.col, q.n, ur);
+        if (p.gate != nullptr) load_raw<T, VEC>((const T*)p.gate + r * p.ld_gate + q.col, q.n, gr);
+    };
+    if (row < p.rows) request(row);
+    for (; row < p.rows; row += step_rows) {
+        const float4 st = stats;
+        Oct a, w;
+        Raw8<T> un = ur, gn = gr;                           // unpacked where they are used
+        if (p.dy != nullptr) unpack<float>(ar, a);
+        else a.fill(0.f);
+        Oct y, d;
+        if (p.dz != nullptr) {
+            unpack<float>(yr, y);
+            unpack<T>(dr, d);
+        }
+        if (row + step_rows < p.rows) request(row + step_rows);
+        if (p.dz != nullptr) {
+            load_weights<VEC>(p.w_pre, q, w);
+            float2 m0 = pair(0.f), m1 = pair(0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[i] = (y[i] - st[2]) * st[3];
-                d[i] *= p.cot_in;
-                gw_pre[i] = fmaf(d[i], y[i], gw_pre[i]);
-                d[i] *= w[i];
-                m[0] = fmaf(d[i], y[i], m[0]);
-                m[1] += d[i];
+            for (int j = 0; j < 4; ++j) {
+                if (CENTER) y.v[j] = __fadd2_rn(y.v[j], pair(-st.z));
+                y.v[j] = __fmul2_rn(y.v[j], pair(st.w));
+                d.v[j] = __fmul2_rn(d.v[j], pair(p.cot_in));
+                gw_pre.v[j] = __ffma2_rn(d.v[j], y.v[j], gw_pre.v[j]);
+                d.v[j] = __fmul2_rn(d.v[j], w.v[j]);
+                m0 = __ffma2_rn(d.v[j], y.v[j], m0);
+                if (CENTER) m1 = __fadd2_rn(m1, d.v[j]);
             }
             if (p.pre != MPODE_NORM_NONE) {
-                row_sum<2>(m, q, sums, set);
-                m[0] *= inv;
-                m[1] = p.pre == MPODE_NORM_MEANVAR ? m[1] * inv : 0.f;
-            } else m[0] = m[1] = 0.f;
+                float m[N];
+                m[0] = m0.x + m0.y;
+                if (CENTER) m[N - 1] = m1.x + m1.y;
+                row_sum<N>(m, q, sums, set);
+                m0 = pair(-m[0] * inv);
+                m1 = pair(CENTER && p.pre == MPODE_NORM_MEANVAR ? -m[N - 1] * inv : 0.f);
+            } else m0 = m1 = pair(0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] += st[3] * (d[i] - y[i] * m[0] - m[1]);
+            for (int j = 0; j < 4; ++j) {
+                if (CENTER) d.v[j] = __fadd2_rn(d.v[j], m1);
+                a.v[j] = __ffma2_rn(__ffma2_rn(y.v[j], m0, d.v[j]), pair(st.w), a.v[j]);
+            }
         }
         store8<float, VEC>(p.dy_out + row * p.ld_y + q.col, q.n, a);
-        if (p.u != nullptr) {
-            float c[8], m[2] = {0.f, 0.f};
-            load_weights<VEC>(p.w_post, q.col, q.n, w);
-            load_weights<VEC>(p.scale, q.col, q.n, c);
-            uint32_t keep = 0xffu;
-            if (p.drop.threshold) keep = keep_bits((uint64_t)row * groups_row + q.col / 8, seed, step, p.drop.site, p.drop.threshold);
-            if (q.n < 8) keep &= (1u << max(q.n, 0)) - 1u;          // (columns that do not exist add nothing to the sums)
+        if (p.u == nullptr) continue;
+        Oct u, g, c;
+        unpack<T>(un, u);
+        if (p.gate != nullptr) unpack<T>(gn, g);
+        Kept keep;
+        if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
+        load_weights<VEC>(p.w_post, q, w);
+        load_weights<VEC>(p.scale, q, c);
+        float2 m0 = pair(0.f), m1 = pair(0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[i] = (u[i] - st[0]) * st[1];
-                float slope = 0.f, sig = 1.f;
-                if (p.gate != nullptr) sig = gate_of(g[i], slope);
-                float t = (keep >> i) & 1u ? a[i] * (p.h * p.drop.scale) : 0.f;
-                const float v = u[i] * w[i];
-                gscale[i] = fmaf(t, v * sig, gscale[i]);
-                t *= c[i];
-                g[i] = t * v * slope * p.cot_out;
-                t *= sig;
-                gw_post[i] = fmaf(t, u[i], gw_post[i]);
-                a[i] = t * w[i];
-                m[0] = fmaf(a[i], u[i], m[0]);
-                m[1] += a[i];
+        for (int j = 0; j < 4; ++j) {
+            if (CENTER) u.v[j] = __fadd2_rn(u.v[j], pair(-st.x));
+            u.v[j] = __fmul2_rn(u.v[j], pair(st.y));
+            float2 t = __fmul2_rn(a.v[j], pair(p.h * p.drop.scale));
+            if (p.drop.on) {
+                if (!keep[2 * j]) t.x = 0.f;
+                if (!keep[2 * j + 1]) t.y = 0.f;
             }
-            if (p.dgate != nullptr) bad |= store8<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col, q.n, g);
-            if (p.post != MPODE_NORM_NONE) {
-                row_sum<2>(m, q, sums, set);
-                m[0] *= inv;
-                m[1] = p.post == MPODE_NORM_MEANVAR ? m[1] * inv : 0.f;
-            } else m[0] = m[1] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = st[1] * (a[i] - u[i] * m[0] - m[1]) * p.cot_out;
-            bad |= store8<T, VEC>((T*)p.du + row * p.ld_u + q.col, q.n, a);
+            if (VEC ? !exists : 2 * j >= q.n) t.x = 0.f;    // columns that do not exist add nothing to the sums
+            if (VEC ? !exists : 2 * j + 1 >= q.n) t.y = 0.f;
+            const float2 v = __fmul2_rn(u.v[j], w.v[j]);
+            if (p.gate != nullptr) {
+                float2 slope;
+                const float2 sig = gate_of<T, true>(g.v[j], slope);
+                gscale.v[j] = __ffma2_rn(t, __fmul2_rn(v, sig), gscale.v[j]);
+                t = __fmul2_rn(t, c.v[j]);
+                g.v[j] = __fmul2_rn(__fmul2_rn(t, v), __fmul2_rn(slope, pair(p.cot_out)));
+                t = __fmul2_rn(t, sig);
+            } else {
+                gscale.v[j] = __ffma2_rn(t, v, gscale.v[j]);
+                t = __fmul2_rn(t, c.v[j]);
+            }
+            gw_post.v[j] = __ffma2_rn(t, u.v[j], gw_post.v[j]);
+            a.v[j] = __fmul2_rn(t, w.v[j]);
+            m0 = __ffma2_rn(a.v[j], u.v[j], m0);
+            if (CENTER) m1 = __fadd2_rn(m1, a.v[j]);
         }
+        Raw8<T> out;
+        if (p.dgate != nullptr) {
+            pack<T>(g, out);
+            if (p.flag != nullptr) largest.see(out, q.n);
+            store_raw<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col, q.n, out);
+        }
+        if (p.post != MPODE_NORM_NONE) {
+            float m[N];
+            m[0] = m0.x + m0.y;
+            if (CENTER) m[N - 1] = m1.x + m1.y;
+            row_sum<N>(m, q, sums, set);
+            m0 = pair(-m[0] * inv);
+            m1 = pair(CENTER && p.post == MPODE_NORM_MEANVAR ? -m[N - 1] * inv : 0.f);
+        } else m0 = m1 = pair(0.f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (CENTER) a.v[j] = __fadd2_rn(a.v[j], m1);
+            a.v[j] = __fmul2_rn(__fmul2_rn(__ffma2_rn(u.v[j], m0, a.v[j]), pair(st.y)), pair(p.cot_out));
+        }
+        pack<T>(a, out);
+        if (p.flag != nullptr) largest.see(out, q.n);
+        store_raw<T, VEC>((T*)p.du + row * p.ld_u + q.col, q.n, out);
     }
-    warp_flag_or(p.flag, bad);
+    warp_flag_or(p.flag, largest.nonfinite());
     if (p.partial != nullptr) {
         float* out = p.partial + ((long long)(blockIdx.x / blocks) * q.groups + q.group) * 3 * p.width + q.col;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < q.n) {
-                out[i] = gw_post[i];
-                out[p.width + i] = gscale[i];
-                out[2 * p.width + i] = gw_pre[i];
-            }
+        store8<float, VEC>(out, q.n, gw_post);
+        store8<float, VEC>(out + p.width, q.n, gscale);
+        store8<float, VEC>(out + 2 * p.width, q.n, gw_pre);
     }
-    if (blocks > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (blocks > 1) cluster_sync();
 }
 
 // out_k[c] (+)= sum over the partial rows, in a fixed order: 32 columns and 16 slices of the rows a block
@@ -376,6 +475,8 @@ bool vectors_fit(const mpode_residual_desc& d, const ResArgs& a, bool& torn) {
     return fit;
 }
 
+bool center(const mpode_residual_desc& d) { return d.post_norm == MPODE_NORM_MEANVAR || d.pre_norm == MPODE_NORM_MEANVAR; }
+
 size_t partial_rows(int rows, int width) {
     const Shape s = shape_of(rows, width, kBackwardBlocks);
     return (size_t)s.clusters * s.groups;
@@ -400,20 +501,21 @@ mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_
     if (bad != MPODE_OK) return bad;
     if (rows == 0) return MPODE_OK;
     ResArgs a = base_args(*desc, rows, rng_dev);
-    if (u_dev == nullptr) a.drop.threshold = 0;
+    if (u_dev == nullptr) a.drop.on = false;
     if (!y_dev || (u_dev && !y_out_dev) || (!u_dev && !z_dev)) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: null pointer argument");
     if (gate_dev && !u_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: a gate without a block output");
-    if (a.drop.threshold != 0 && !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: dropout without its {seed, step}");
+    if (a.drop.on && !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: dropout without its {seed, step}");
     a.y = y_dev; a.u = u_dev; a.gate = gate_dev; a.w_post = w_post_dev; a.scale = scale_dev; a.w_pre = w_pre_dev;
     a.y_out = y_out_dev; a.z = z_dev; a.stats = stats_dev;
     bool torn;
     const bool vec = vectors_fit(*desc, a, torn);
     if (torn) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: a pointer is not aligned to its elements (stats_dev: 16 bytes)");
     const Shape s = shape_of(rows, desc->width, kForwardBlocks);
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
     return operator_launched(with_low(desc->low, [&](auto t) {
         using T = decltype(t);
-        return vec ? launch(residual_forward_kernel<T, true>, a, s, (cudaStream_t)cuda_stream)
-                   : launch(residual_forward_kernel<T, false>, a, s, (cudaStream_t)cuda_stream);
+        if (center(*desc)) return vec ? launch(residual_forward_kernel<T, true, true>, a, s, st) : launch(residual_forward_kernel<T, false, true>, a, s, st);
+        return vec ? launch(residual_forward_kernel<T, true, false>, a, s, st) : launch(residual_forward_kernel<T, false, false>, a, s, st);
     }), "mpode_residual_forward");
 }
 
@@ -427,7 +529,7 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
     if (bad != MPODE_OK) return bad;
     if (scale_exp < -100 || scale_exp > 100) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: scale exponent %d", who, scale_exp);
     ResArgs a = base_args(*desc, rows, rng_dev);
-    if (u_dev == nullptr) a.drop.threshold = 0;
+    if (u_dev == nullptr) a.drop.on = false;
     a.y = y_new_dev; a.u = u_dev; a.gate = gate_dev; a.w_post = w_post_dev; a.scale = scale_dev; a.w_pre = w_pre_dev;
     a.stats = const_cast<float*>(stats_dev);
     a.dy = dL_dy_new_dev; a.dz = dL_dz_dev; a.dy_out = dL_dy_dev; a.du = dL_du_dev; a.dgate = dL_dgate_dev;
@@ -442,7 +544,7 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
         if (dL_dgate_dev && !gate_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: a cotangent for a gate that is not there", who);
         if (!stats_dev && ((u_dev && desc->post_norm != MPODE_NORM_NONE) || (dL_dz_dev && desc->pre_norm != MPODE_NORM_NONE)))
             return operator_fail(MPODE_ERR_INVALID_ARG, "%s: norms need the forward pass's statistics", who);
-        if (a.drop.threshold != 0 && !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: dropout without its {seed, step}", who);
+        if (a.drop.on && !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: dropout without its {seed, step}", who);
         bool torn;
         const bool vec = vectors_fit(*desc, a, torn);
         torn = torn || misaligned(dL_dw_post_dev, 4) || misaligned(dL_dscale_dev, 4) || misaligned(dL_dw_pre_dev, 4);
@@ -456,7 +558,8 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
         const Shape s = shape_of(rows, desc->width, kBackwardBlocks);
         const mpode_status ran = operator_launched(with_low(desc->low, [&](auto t) {
             using T = decltype(t);
-            return vec ? launch(residual_backward_kernel<T, true>, a, s, st) : launch(residual_backward_kernel<T, false>, a, s, st);
+            if (center(*desc)) return vec ? launch(residual_backward_kernel<T, true, true>, a, s, st) : launch(residual_backward_kernel<T, false, true>, a, s, st);
+            return vec ? launch(residual_backward_kernel<T, true, false>, a, s, st) : launch(residual_backward_kernel<T, false, false>, a, s, st);
         }), who);
         if (ran != MPODE_OK || !weights) return ran;
     }

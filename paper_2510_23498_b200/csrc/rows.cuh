@@ -1,5 +1,4 @@
-// Eight neighbouring elements of a row at a time, as float32: 16-byte accesses (VEC: the caller has checked alignment, and all eight exist or
-// none does) or single elements, of which the first n exist.
+// Eight neighbouring elements of a row at a time: as they lie in memory (Raw8), and as four pairs of float32 (Oct), on which one instruction works on two.
 #pragma once
 #include <type_traits>
 
@@ -9,13 +8,12 @@ namespace mpode {
 
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
-    static __device__ __forceinline__ float2 get(uint32_t w) {
-        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-    }
+    static __device__ __forceinline__ float2 get(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
     static __device__ __forceinline__ uint32_t put(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
+    static constexpr uint32_t infinity = 0x7F80u;
 };
 template <> struct Pair<__half> {
     static __device__ __forceinline__ float2 get(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
@@ -23,64 +21,106 @@ template <> struct Pair<__half> {
         const __half2 h = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
+    static constexpr uint32_t infinity = 0x7C00u;
 };
 
-template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p, int n, float (&f)[8]) {
-    if constexpr (VEC) {
-        if (n <= 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = 0.f;
-            return;
-        }
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-            f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4*>(p);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 t = Pair<T>::get(w[i]);
-                f[2 * i] = t.x; f[2 * i + 1] = t.y;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < n ? Low<T>::to_f(p[i]) : 0.f;
+struct Oct {
+    float2 v[4];
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? v[i >> 1].y : v[i >> 1].x; }
+    __device__ __forceinline__ float sum() const {
+        const float2 s = __fadd2_rn(__fadd2_rn(v[0], v[1]), __fadd2_rn(v[2], v[3]));
+        return s.x + s.y;
     }
-}
+    __device__ __forceinline__ void fill(float f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = make_float2(f, f);
+    }
+};
 
-// returns whether a value that was written is not finite
-template <typename T, bool VEC> __device__ __forceinline__ bool store8(T* p, int n, const float (&f)[8]) {
-    bool bad = false;
+// VEC: 16-byte accesses, for which the caller has checked alignment, and all eight elements exist or none does; else single elements of which the first n
+// exist.  Elements that do not exist read as zero.
+template <typename T> struct Raw8 { uint32_t w[sizeof(T) * 2]; };
+template <typename T, bool VEC> __device__ __forceinline__ void load_raw(const T* p, int n, Raw8<T>& r) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) * 2; ++j) r.w[j] = 0u;
     if constexpr (VEC) {
-        if (n <= 0) return false;
-        if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+        if (n <= 0) return;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) bad |= Low<float>::nonfinite(f[i]);
-        } else {
-            uint32_t w[4];
-            const uint32_t lo = sizeof(T) == 2 && std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u, hi = lo << 16;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = Pair<T>::put(f[2 * i], f[2 * i + 1]);
-                bad |= (w[i] & lo) == lo || (w[i] & hi) == hi;
-            }
-            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+            const uint4 a = reinterpret_cast<const uint4*>(p)[j];
+            r.w[4 * j] = a.x; r.w[4 * j + 1] = a.y; r.w[4 * j + 2] = a.z; r.w[4 * j + 3] = a.w;
         }
-    } else {
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) {
-                const T t = Low<T>::from_f(f[i]);
-                bad |= Low<T>::nonfinite(t);
-                p[i] = t;
+            if (i < n) r.w[i] = __float_as_uint(p[i]);
+    } else {
+        const uint16_t* const h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) r.w[i / 2] |= (uint32_t)h[i] << (16 * (i & 1));
+    }
+}
+template <typename T> __device__ __forceinline__ void unpack(const Raw8<T>& r, Oct& o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) o.v[j] = make_float2(__uint_as_float(r.w[2 * j]), __uint_as_float(r.w[2 * j + 1]));
+        else o.v[j] = Pair<T>::get(r.w[j]);
+    }
+}
+template <typename T> __device__ __forceinline__ void pack(const Oct& o, Raw8<T>& r) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) { r.w[2 * j] = __float_as_uint(o.v[j].x); r.w[2 * j + 1] = __float_as_uint(o.v[j].y); }
+        else r.w[j] = Pair<T>::put(o.v[j].x, o.v[j].y);
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void load8(const T* p, int n, Oct& o) {
+    Raw8<T> r;
+    load_raw<T, VEC>(p, n, r);
+    unpack<T>(r, o);
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store_raw(T* p, int n, const Raw8<T>& r) {
+    if constexpr (VEC) {
+        if (n <= 0) return;
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(p)[j] = make_uint4(r.w[4 * j], r.w[4 * j + 1], r.w[4 * j + 2], r.w[4 * j + 3]);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = __uint_as_float(r.w[i]);
+    } else {
+        uint16_t* const h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) h[i] = (uint16_t)(r.w[i / 2] >> (16 * (i & 1)));
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int n, const Oct& o) {
+    Raw8<T> r;
+    pack<T>(o, r);
+    store_raw<T, VEC>(p, n, r);
+}
+
+// Largest magnitude of the low-format values seen, as bits (infinities and NaN above every number): two instructions a word
+template <typename T> struct Largest {
+    uint32_t m = 0;
+    __device__ __forceinline__ void see(uint32_t w) {
+        if constexpr (sizeof(T) == 4) m = max(m, w & 0x7fffffffu);
+        else m = __vmaxu2(m, w & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ void see(const Raw8<T>& r, int n) {
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) * 2; ++j)
+            if (j * 4 < n * (int)sizeof(T)) {
+                const bool half = sizeof(T) == 2 && j * 2 + 1 == n;          // an odd row's last word holds one element
+                see(half ? r.w[j] & 0xffffu : r.w[j]);
             }
     }
-    return bad;
-}
+    __device__ __forceinline__ bool nonfinite() const {
+        if constexpr (sizeof(T) == 4) return m >= 0x7f800000u;
+        else return (m & 0xffffu) >= Pair<T>::infinity || (m >> 16) >= Pair<T>::infinity;
+    }
+};
 
 }  // namespace mpode
