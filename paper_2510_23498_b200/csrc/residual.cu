@@ -243,11 +243,72 @@ template <typename T, bool VEC, bool CENTER> __global__ void __launch_bounds__(k
     if (blocks > 1) cluster_sync();                         // nobody leaves while its shared memory may be written
 }
 
+// A thread's own pieces of the rows y', dy', dz, u and gate (0 .. 4).  VEC: copied to shared memory by asynchronous copies some rows ahead; a thread reads
+// what it has copied itself, so that nothing has to be waited for but its own copies.  Else loaded into registers when the row starts.
+template <typename T, bool VEC> struct Rows;
+template <typename T> struct Rows<T, true> {
+    static constexpr int kStages = sizeof(T) == 4 ? 2 : 3, kLow = sizeof(T) / 2, kPieces = 4 + 3 * kLow;
+    uint4* at;
+    int threads;
+    __device__ __forceinline__ void bind(char* smem, int n) {
+        threads = blockDim.x * blockDim.y;
+        at = reinterpret_cast<uint4*>(smem) + threadIdx.y * blockDim.x + threadIdx.x;
+        if (n <= 0)                                         // columns that do not exist are zero
+            for (int i = 0; i < kStages * kPieces; ++i) at[i * threads] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    static __device__ __forceinline__ constexpr int first(int k) { return k < 2 ? 2 * k : 4 + (k - 2) * kLow; }
+    template <typename E> __device__ __forceinline__ void request(int stage, int k, const E* from, int n) {
+        if (n <= 0) return;
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(E) / 2; ++j)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_of(at + (stage * kPieces + first(k) + j) * threads)), "l"(reinterpret_cast<const uint4*>(from) + j) : "memory");
+    }
+    __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
+    template <typename E> __device__ __forceinline__ void raw(int stage, int k, Raw8<E>& r) const {
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(E) / 2; ++j) {
+            const uint4 v = at[(stage * kPieces + first(k) + j) * threads];
+            r.w[4 * j] = v.x; r.w[4 * j + 1] = v.y; r.w[4 * j + 2] = v.z; r.w[4 * j + 3] = v.w;
+        }
+    }
+    __device__ __forceinline__ void get(int stage, int k, Oct& o) const {
+        if (k < 2) {
+            Raw8<float> r;
+            raw<float>(stage, k, r);
+            unpack<float>(r, o);
+        } else {
+            Raw8<T> r;
+            raw<T>(stage, k, r);
+            unpack<T>(r, o);
+        }
+    }
+};
+template <typename T> struct Rows<T, false> {
+    static constexpr int kStages = 1;
+    Raw8<float> wide[2];
+    Raw8<T> low[3];
+    __device__ __forceinline__ void bind(char*, int) {}
+    template <typename E> __device__ __forceinline__ void request(int, int k, const E* from, int n) {
+        if constexpr (std::is_same<E, T>::value && !std::is_same<T, float>::value) load_raw<T, false>(from, n, low[k - 2]);
+        else if (k < 2) load_raw<float, false>((const float*)from, n, wide[k]);
+        else load_raw<T, false>((const T*)from, n, low[k - 2]);
+    }
+    __device__ __forceinline__ void commit() {}
+    __device__ __forceinline__ void wait() {}
+    __device__ __forceinline__ void raw(int, int k, Raw8<T>& r) const { r = low[k - 2]; }
+    __device__ __forceinline__ void get(int, int k, Oct& o) const {
+        if (k < 2) unpack<float>(wide[k], o);
+        else unpack<T>(low[k - 2], o);
+    }
+};
+
 // With n' the normalised y', n that of u, and t the cotangent of the step's term:
 //   a = dy' + r' (w dz - n' mean(w dz n') - mean(w dz)),  dw_pre += dz n';   t = drop(a), dscale += h t v sig, with v = w_post n;
 //   t <- h scale t, dgate = t v sig', t <- t sig, dw_post += t n, du = r (w t - n mean(w t n) - mean(w t)); the means of w dz and w t only for MEANVAR
 template <typename T, bool VEC, bool CENTER> __global__ void __launch_bounds__(kMaxThreads, 1) residual_backward_kernel(const ResArgs p, const int blocks) {
     constexpr int N = CENTER ? 2 : 1;
+    extern __shared__ __align__(16) char staged[];
     __shared__ __align__(16) RowSum<N> sums;
     const Lane q = lane_of(p.width, blocks);
     int set = 0;
@@ -261,32 +322,45 @@ template <typename T, bool VEC, bool CENTER> __global__ void __launch_bounds__(k
     gw_post.fill(0.f); gscale.fill(0.f); gw_pre.fill(0.f);
     Largest<T> largest;
     long long row = (long long)(blockIdx.x / blocks) * q.groups + q.group;
-    Raw8<float> yr, ar;
-    Raw8<T> ur, gr, dr;
+    Rows<T, VEC> in;
+    in.bind(staged, q.n);
     float4 stats = make_float4(0.f, 1.f, 0.f, 1.f);
-    auto request = [&](long long r) {
-        if (p.stats != nullptr) stats = reinterpret_cast<const float4*>(p.stats)[r];
-        if (p.dz != nullptr) {
-            load_raw<float, VEC>(p.y + r * p.ld_y + q.col, q.n, yr);
-            load_raw<T, VEC>((const T*)p.dz + r * p.ld_z + q.col, q.n, dr);
+    auto request = [&](long long r, int stage) {
+        if (r < p.rows) {
+            if (p.dz != nullptr) {
+                in.request(stage, 0, p.y + r * p.ld_y + q.col, q.n);
+                in.request(stage, 2, (const T*)p.dz + r * p.ld_z + q.col, q.n);
+            }
+            if (p.dy != nullptr) in.request(stage, 1, p.dy + r * p.ld_y + q.col, q.n);
+            if (p.u != nullptr) in.request(stage, 3, (const T*)p.u + r * p.ld_u + q.col, q.n);
+            if (p.gate != nullptr) in.request(stage, 4, (const T*)p.gate + r * p.ld_gate + q.col, q.n);
         }
-        if (p.dy != nullptr) load_raw<float, VEC>(p.dy + r * p.ld_y + q.col, q.n, ar);
-        if (p.u != nullptr) load_raw<T, VEC>((const T*)p.u + r * p.ld_u + q.col, q.n, ur);
-        if (p.gate != nullptr) load_raw<T, VEC>((const T*)p.gate + r * p.ld_gate + q.col, q.n, gr);
+        in.commit();
     };
-    if (row < p.rows) request(row);
-    for (; row < p.rows; row += step_rows) {
+    if (VEC)
+        for (int k = 0; k < in.kStages; ++k) request(row + k * step_rows, k);
+    if (p.stats != nullptr && row < p.rows) stats = reinterpret_cast<const float4*>(p.stats)[row];
+    int stage = 0;
+    auto advance = [&]() {                                  // this row's pieces have been used: its stage is free
+        if (VEC) request(row + in.kStages * step_rows, stage);
+        row += step_rows;
+        stage = stage + 1 < in.kStages ? stage + 1 : 0;
+    };
+    for (; row < p.rows; advance()) {
         const float4 st = stats;
-        Oct a, w;
-        Raw8<T> un = ur, gn = gr;                           // unpacked where they are used
-        if (p.dy != nullptr) unpack<float>(ar, a);
+        if (p.stats != nullptr && row + step_rows < p.rows) stats = reinterpret_cast<const float4*>(p.stats)[row + step_rows];
+        if (!VEC) request(row, 0);
+        in.wait();
+        Oct a, y, d, w;
+        Raw8<T> un, gn;                                     // unpacked where they are used
+        if (p.dy != nullptr) in.get(stage, 1, a);
         else a.fill(0.f);
-        Oct y, d;
         if (p.dz != nullptr) {
-            unpack<float>(yr, y);
-            unpack<T>(dr, d);
+            in.get(stage, 0, y);
+            in.get(stage, 2, d);
         }
-        if (row + step_rows < p.rows) request(row + step_rows);
+        if (p.u != nullptr) in.raw(stage, 3, un);
+        if (p.gate != nullptr) in.raw(stage, 4, gn);
         if (p.dz != nullptr) {
             load_weights<VEC>(p.w_pre, q, w);
             float2 m0 = pair(0.f), m1 = pair(0.f);
@@ -423,11 +497,16 @@ Shape shape_of(int rows, int width, int clusters_at_once) {
 }
 constexpr int kForwardBlocks = 148 * 4, kBackwardBlocks = 148 * 2;
 
-cudaError_t launch(void (*kernel)(const ResArgs, const int), const ResArgs& a, const Shape& s, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(const ResArgs, const int), const ResArgs& a, const Shape& s, cudaStream_t st, size_t smem = 0) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.clusters * s.blocks));
     cfg.blockDim = dim3(s.threads, s.groups);
     cfg.stream = st;
+    cfg.dynamicSmemBytes = smem;
+    if (smem > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)s.blocks;
@@ -558,8 +637,10 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
         const Shape s = shape_of(rows, desc->width, kBackwardBlocks);
         const mpode_status ran = operator_launched(with_low(desc->low, [&](auto t) {
             using T = decltype(t);
-            if (center(*desc)) return vec ? launch(residual_backward_kernel<T, true, true>, a, s, st) : launch(residual_backward_kernel<T, false, true>, a, s, st);
-            return vec ? launch(residual_backward_kernel<T, true, false>, a, s, st) : launch(residual_backward_kernel<T, false, false>, a, s, st);
+            using R = Rows<T, true>;
+            const size_t smem = (size_t)s.threads * s.groups * R::kStages * R::kPieces * 16;
+            if (center(*desc)) return vec ? launch(residual_backward_kernel<T, true, true>, a, s, st, smem) : launch(residual_backward_kernel<T, false, true>, a, s, st);
+            return vec ? launch(residual_backward_kernel<T, true, false>, a, s, st, smem) : launch(residual_backward_kernel<T, false, false>, a, s, st);
         }), who);
         if (ran != MPODE_OK || !weights) return ran;
     }
