@@ -1,0 +1,57 @@
+// Exchange between the blocks of a cluster through distributed shared memory: asynchronous stores whose bytes count on the receiver's barrier, so
+// that neither side needs a fence (one that made a block's stores visible first would wait for its results on the way to memory, about 1 us).
+#pragma once
+#include "common.cuh"
+
+namespace mpode {
+
+__device__ __forceinline__ unsigned smem_of(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ unsigned peer_of(unsigned local, unsigned rank) {
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void send(unsigned at, float f, unsigned bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(at), "f"(f), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void send(unsigned at, float f, float g, unsigned bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(f), "f"(g), "r"(bar) : "memory");
+}
+
+// Two barriers used in turn.  A set of places is written again two rounds later: a round is complete only when every sender of the cluster has sent, and each of them
+// sends behind its own reads of the round before.
+__device__ __forceinline__ void sets_begin(unsigned long long* bar) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&bar[0])) : "memory");
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&bar[1])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+// one thread a block and round: the bytes that will come
+__device__ __forceinline__ void set_expects(unsigned bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool set_arrived(unsigned bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0u;
+}
+// The blocks of a cluster run at the same time, so this wait ends; should it not within two seconds, the caller makes its results NaN and goes on
+// without waiting again, so that the kernel ends.
+static __device__ __noinline__ bool await_set(unsigned bar, unsigned parity) {
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+    while (!set_arrived(bar, parity)) {
+        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+        if (t - t0 > 2000000000ull) return false;
+    }
+    return true;
+}
+__device__ __forceinline__ void wait_set(unsigned bar, unsigned parity, bool& broken) {
+    if (!broken && !set_arrived(bar, parity)) broken = !await_set(bar, parity);
+    __syncwarp();
+}
+
+}  // namespace mpode

@@ -19,6 +19,7 @@
 
 #include <type_traits>
 
+#include "cluster.cuh"
 #include "operators.h"
 #include "rows.cuh"
 
@@ -196,7 +197,6 @@ template <int V> struct Affine {
 };
 
 constexpr int kMaxWarps = 8, kMaxCluster = 16;
-constexpr unsigned long long kWaitNs = 2000000000ull;
 
 // Shared memory of the exchange: maps of the block's warps and of the cluster's blocks, two sets used in turn.  Places of warps and blocks
 // that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
@@ -205,15 +205,6 @@ template <int V> struct __align__(16) Exchange {
     float block[2][kMaxCluster][3][32 * V];
     unsigned long long bar[2];                  // counts the bytes of a set's block maps
 };
-__device__ __forceinline__ unsigned smem_of(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ unsigned peer_of(unsigned local, unsigned rank) {
-    unsigned r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 template <int V> __device__ __forceinline__ void lds(float (&f)[V], const float* p) {
     if constexpr (V == 2) {
         const float2 t = *reinterpret_cast<const float2*>(p);
@@ -230,30 +221,9 @@ template <int V> __device__ __forceinline__ void fetch(Affine<V>& a, const float
 template <int V> __device__ __forceinline__ void put(float (&t)[3][32 * V], const Affine<V>& a) {
     sts<V>(&t[0][threadIdx.x * V], a.m); sts<V>(&t[1][threadIdx.x * V], a.k); sts<V>(&t[2][threadIdx.x * V], a.u);
 }
-// into another block's shared memory; the bytes count on that block's barrier, so that neither side needs a fence (one that made this block's
-// stores visible first would wait for its trajectory on the way to memory: 1 us a round)
-template <int V> __device__ __forceinline__ void send(unsigned at, const float (&f)[V], unsigned bar) {
-    if constexpr (V == 2)
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(f[0]), "f"(f[1]), "r"(bar) : "memory");
-    else asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(at), "f"(f[0]), "r"(bar) : "memory");
-}
-__device__ __forceinline__ bool set_arrived(unsigned bar, unsigned parity) {
-    unsigned ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0u;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-// The blocks of a cluster run at the same time, so this wait ends; should it not within two seconds, the results become NaN and the kernel ends
-__device__ __noinline__ bool await_set(unsigned bar, unsigned parity) {
-    const unsigned long long t0 = now_ns();
-    while (!set_arrived(bar, parity))
-        if (now_ns() - t0 > kWaitNs) return false;
-    return true;
+template <int V> __device__ __forceinline__ void send_all(unsigned at, const float (&f)[V], unsigned bar) {
+    if constexpr (V == 2) send(at, f[0], f[1], bar);
+    else send(at, f[0], bar);
 }
 
 template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex, int blocks) {
@@ -266,17 +236,12 @@ template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex,
             for (int r = blocks + threadIdx.y; r < kMaxCluster; r += blockDim.y) put<V>(ex.block[set][r], id);
     }
     if (blocks == 1) return;
-    if (threadIdx.x == 0 && threadIdx.y == 0) {
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&ex.bar[0])) : "memory");
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&ex.bar[1])) : "memory");
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+    if (threadIdx.x == 0 && threadIdx.y == 0) sets_begin(ex.bar);
     cluster_arrive();                       // nobody writes into a block that has not started
 }
 
 // The state in front of this warp's steps, from the state in front of all of this round's steps (`carry`, replaced by the one behind them).
-// Called by all threads of the cluster in the same rounds.  A set is written again two rounds later: a block sends the maps of the round between
-// only when its warps have read this one's, and a block that receives all of those has finished the round before.
+// Called by all threads of the cluster in the same rounds.
 template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsigned round, const Map<V>& own, float (&carry)[V], float (&start)[V],
                                                           int blocks, int rank, bool& broken) {
     const int warp = threadIdx.y, set = round & 1;
@@ -297,8 +262,7 @@ template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsig
         return;
     }
     const unsigned bar = smem_of(&ex.bar[set]);
-    if (warp == 0 && threadIdx.x == 0)
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(blocks * 3 * 32 * V * 4) : "memory");
+    if (warp == 0 && threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
     Map<V> all;
     Affine<V> before;
 #pragma unroll
@@ -311,13 +275,11 @@ template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsig
     const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]);
     for (int to = warp; to < blocks; to += (int)blockDim.y) {               // this block's map to every block, a warp to each
         const unsigned there = peer_of(at, to), count = peer_of(bar, to);
-        send<V>(there, a.m, count);
-        send<V>(there + 32 * V * 4, a.k, count);
-        send<V>(there + 64 * V * 4, a.u, count);
+        send_all<V>(there, a.m, count);
+        send_all<V>(there + 32 * V * 4, a.k, count);
+        send_all<V>(there + 64 * V * 4, a.u, count);
     }
-    const unsigned parity = (round >> 1) & 1;
-    if (!broken && !set_arrived(bar, parity)) broken = !await_set(bar, parity);
-    __syncwarp();
+    wait_set(bar, (round >> 1) & 1, broken);
     if (broken) {
 #pragma unroll
         for (int v = 0; v < V; ++v) carry[v] = __int_as_float(0x7fffffff);

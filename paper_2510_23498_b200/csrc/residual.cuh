@@ -1,0 +1,190 @@
+// What the two directions of the residual step share: arguments, how rows lie on threads, row sums.
+#pragma once
+#include "cluster.cuh"
+#include "operators.h"
+#include "philox.cuh"
+#include "rows.cuh"
+
+namespace mpode {
+
+struct ResArgs {
+    const float *y, *w_post, *scale, *w_pre;      // y: forward the state before the step, backward the one behind it
+    const void *u, *gate;
+    float *y_out, *stats;                         // stats [rows][4]: mean and 1 / deviation of u, then of y'
+    void* z;
+    // backward
+    const float* dy; const void* dz;
+    float* dy_out; void *du, *dgate;
+    float* partial;                               // [blocks * groups][3][width]: dw_post, dscale, dw_pre, or null when no weight gradient is asked for
+    float cot_in, cot_out;                        // 2^-e, 2^e
+    unsigned* flag;
+    long long ld_y, ld_u, ld_gate, ld_z;
+    int rows, width, post, pre;
+    float eps, h;
+    Dropout drop;
+};
+
+// How rows are spread: warps of a row in a block, rows in a block, blocks of a row (a cluster), clusters
+struct ResShape { int warps, groups, blocks, clusters; };
+constexpr int kResWarps = 16, kResBlocks = 4, kResMaxWidth = kResWarps * 256 * kResBlocks, kResGroups = 8;
+
+cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
+cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
+
+#ifdef __CUDACC__
+// Where a thread stands.  WARPS warps a row; one warp: eight rows a block.  CLUSTER: the row goes on in the other blocks of the cluster.
+template <int WARPS, bool CLUSTER> struct Lane {
+    static constexpr int kGroups = WARPS == 1 ? kResGroups : 1, kThreads = 32 * WARPS * kGroups;
+    int group, warp, blocks, rank, col, n, first, step;      // column and how many columns exist; first row and distance of the rows
+    __device__ __forceinline__ Lane(int width, int blocks_) {
+        const int t = threadIdx.x;
+        group = WARPS == 1 ? t >> 5 : 0;
+        warp = WARPS == 1 ? 0 : t >> 5;
+        blocks = CLUSTER ? blocks_ : 1;
+        const int cluster = CLUSTER ? (int)(blockIdx.x / blocks) : (int)blockIdx.x;
+        rank = CLUSTER ? (int)(blockIdx.x - cluster * blocks) : 0;
+        col = (rank * 32 * WARPS + (WARPS == 1 ? t & 31 : t)) * 8;
+        n = min(8, width - col);
+        first = cluster * kGroups + group;
+        step = (CLUSTER ? (int)(gridDim.x / blocks) : (int)gridDim.x) * kGroups;
+    }
+};
+
+// Sums over a row's threads, the same bits in all of them.  One warp: shuffles.  One block: partial sums of its warps in shared memory.  A cluster: every
+// warp's into every block's shared memory.  Two sets of partial sums in turn, so that one barrier a sum does.
+template <int N, int WARPS, bool CLUSTER> struct RowSum {
+    static constexpr int kSlots = WARPS * (CLUSTER ? kResBlocks : 1);
+    struct __align__(16) Shared {
+        float part[2][N][kSlots];
+        unsigned long long bar[2];
+    };
+    Shared& s;
+    unsigned round = 0;
+    bool broken = false;
+    __device__ __forceinline__ RowSum(Shared& shared, int blocks) : s(shared) {
+        if (!CLUSTER) return;
+        for (int i = threadIdx.x; i < 2 * N * kSlots; i += blockDim.x) (&s.part[0][0][0])[i] = 0.f;      // (places of blocks that do not exist)
+        if (threadIdx.x == 0) sets_begin(s.bar);
+        cluster_arrive();                                    // nobody writes into a block that has not started
+        cluster_wait();
+    }
+    __device__ __forceinline__ void end() {
+        if (!CLUSTER) return;
+        cluster_arrive();                                    // nobody leaves while its shared memory may be written
+        cluster_wait();
+    }
+    template <int W, bool C> __device__ __forceinline__ void operator()(float (&v)[N], const Lane<W, C>& q) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (N == 1) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        } else {
+            // both at once: the lower lanes take over the first sum, the upper ones the second
+            float mine = lane < 16 ? v[0] : v[1];
+            mine += __shfl_xor_sync(0xffffffffu, lane < 16 ? v[1] : v[0], 16);
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            const float other = __shfl_xor_sync(0xffffffffu, mine, 16);
+            v[0] = lane < 16 ? mine : other;
+            v[1] = lane < 16 ? other : mine;
+        }
+        if constexpr (kSlots > 1) {
+            const int set = round & 1;
+            if constexpr (!CLUSTER) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (lane == i) s.part[set][i][q.warp] = v[i];
+                __syncthreads();
+            } else {
+                const unsigned bar = smem_of(&s.bar[set]);
+                if (threadIdx.x == 0) set_expects(bar, q.blocks * WARPS * N * 4);
+                if (lane < q.blocks) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) send(peer_of(smem_of(&s.part[set][i][q.rank * WARPS + q.warp]), lane), v[i], peer_of(bar, lane));
+                }
+                __syncwarp();
+                wait_set(bar, (round >> 1) & 1, broken);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float* const f = s.part[set][i];
+                if constexpr (kSlots == 2) v[i] = f[0] + f[1];
+                else {
+                    float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int k = 0; k < kSlots; k += 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(f + k);
+                        t = __fadd2_rn(t, __fadd2_rn(make_float2(x.x, x.y), make_float2(x.z, x.w)));
+                    }
+                    v[i] = t.x + t.y;
+                }
+                if (CLUSTER && broken) v[i] = __int_as_float(0x7fffffff);
+            }
+            ++round;
+        }
+    }
+};
+
+__device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
+template <bool VEC> __device__ __forceinline__ void load_weights(const float* w, int col, int n, Oct& o) {
+    if (w == nullptr) o.fill(1.f);
+    else load8<float, VEC>(w + col, n, o);
+}
+
+// sigmoid and its slope sig (1 - sig) = e sig^2 with e = exp(-g).  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the
+// argument's rounding adds |g| 2^-24); the exponent is kept below 2^126, so that e sig^2 is finite.
+template <typename T, bool SLOPE> __device__ __forceinline__ float2 gate_of(float2 g, float2& slope) {
+    float2 e, s;
+    if constexpr (sizeof(T) == 4) {
+        e = make_float2(expf(-g.x), expf(-g.y));
+        s = make_float2(__fdividef(1.f, 1.f + e.x), __fdividef(1.f, 1.f + e.y));
+        if (SLOPE) slope = make_float2(s.x * (e.x > 1.f ? 1.f - s.x : e.x * s.x), s.y * (e.y > 1.f ? 1.f - s.y : e.y * s.y));
+    } else {
+        e = __fmul2_rn(g, pair(-1.4426950408889634f));
+        if (SLOPE) {
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(126.f));
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(126.f));
+        }
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+        const float2 d = __fadd2_rn(e, pair(1.f));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
+        if (SLOPE) slope = __fmul2_rn(__fmul2_rn(s, s), e);
+    }
+    return s;
+}
+
+#endif
+
+inline cudaError_t launch_rows(void (*kernel)(const ResArgs, const int), const ResArgs& a, const ResShape& s, size_t smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(s.clusters * s.blocks));
+    cfg.blockDim = dim3(32 * s.warps * s.groups);
+    cfg.stream = st;
+    cfg.dynamicSmemBytes = smem;
+    if (smem > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)s.blocks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = s.blocks > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a, s.blocks);
+}
+// Calls f with the shape as types: f(WARPS, CLUSTER).  Rows without 16-byte accesses take fewer shapes (more idle lanes in narrow rows).
+template <int N> struct Int { static constexpr int value = N; };
+template <bool B> struct Bool { static constexpr bool value = B; };
+template <typename F> cudaError_t with_shape(const ResShape& s, F&& f) {
+    if (s.blocks > 1) return f(Int<16>(), Bool<true>());
+    if (s.warps == 16) return f(Int<16>(), Bool<false>());
+    if (s.warps == 8) return f(Int<8>(), Bool<false>());
+    if (s.warps == 4) return f(Int<4>(), Bool<false>());
+    if (s.warps == 2) return f(Int<2>(), Bool<false>());
+    return f(Int<1>(), Bool<false>());
+}
+
+}  // namespace mpode
