@@ -2,52 +2,56 @@
 //     n = N_post(u),  y' = y + h scale * drop(sigmoid(gate) * w_post n),  z = Q16(w_pre N_pre(y')),
 // u the block's output and z the next block's input, and the step's backward pass.  N: none, v / sqrt(mean(v^2) + eps), or the same of v - mean(v).
 //
-// Bound by the bytes of its rows (16-bit formats: 14 an element forward, 22 backward): a row is read once, stays in registers while its sums are
-// formed, and is written once.  Eight neighbouring columns a thread (16-byte accesses, one counter of the generator); a row takes one warp up to
-// 256 columns and a block of up to 512 threads up to 4096, wider rows a cluster of up to four blocks whose partial sums meet in distributed
-// shared memory.  All sums, statistics, gates and gradients are float32; what is stored in the low format is rounded once, when it is written.
+// This file: argument checks, how rows are spread over the GPU, and the weights' gradients' last sums; the passes are in residual_forward.cu and
+// residual_backward.cu.  Bound by the bytes of its rows (16-bit formats: 14 an element forward, 22 backward): a row is read once from memory and
+// written once.  Eight neighbouring columns a thread (16-byte accesses, one counter of the generator); a row takes one warp up to 256 columns, a block of
+// up to 8 warps up to 2048, and a cluster of up to 8 blocks beyond that, whose partial sums meet in distributed shared memory.  All sums, statistics,
+// gates and gradients are float32; what is stored in the low format is rounded once, when it is written.
 #include "residual.cuh"
 
 namespace mpode {
 namespace {
 
-// out_k[c] (+)= sum over the partial rows, in a fixed order: 32 columns and 16 slices of the rows a block
-struct FinishArgs { const float* partial; float* out[3]; int rows, width, accumulate; };
+// The weights' gradients from the partial rows [rows][2][width], summed in a fixed order: 32 columns and 16 slices of the rows a block.
+// dw_post = scale S, dscale = w_post S, dw_pre.
+struct FinishArgs { const float *partial, *w_post, *scale; float *dw_post, *dscale, *dw_pre; int rows, width, accumulate; };
 __global__ void __launch_bounds__(512) residual_finish_kernel(const FinishArgs p) {
     __shared__ float part[16][33];
-    const int i = blockIdx.x * 32 + threadIdx.x;         // column of the three gradients side by side
+    const int i = blockIdx.x * 32 + threadIdx.x;            // column of the two sums side by side
     float s = 0.f;
-    if (i < 3 * p.width)
-        for (int r = threadIdx.y; r < p.rows; r += 16) s += p.partial[(long long)r * 3 * p.width + i];
+    if (i < 2 * p.width)
+        for (int r = threadIdx.y; r < p.rows; r += 16) s += p.partial[(long long)r * 2 * p.width + i];
     part[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
-    if (threadIdx.y != 0 || i >= 3 * p.width) return;
+    if (threadIdx.y != 0 || i >= 2 * p.width) return;
     s = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s += part[r][threadIdx.x];
-    const int k = i / p.width;
-    float* out = p.out[k];
-    if (out == nullptr) return;
-    out += i - k * p.width;
-    *out = (p.accumulate ? *out : 0.f) + s;
+    auto put = [&](float* out, float v) {
+        if (out != nullptr) *out = (p.accumulate ? *out : 0.f) + v;
+    };
+    if (i >= p.width) put(p.dw_pre == nullptr ? nullptr : p.dw_pre + (i - p.width), s);
+    else {
+        put(p.dw_post == nullptr ? nullptr : p.dw_post + i, p.scale == nullptr ? s : s * p.scale[i]);
+        put(p.dscale == nullptr ? nullptr : p.dscale + i, p.w_post == nullptr ? s : s * p.w_post[i]);
+    }
 }
 
 // at_once: clusters (of one warp row each) that the GPU is to hold
 ResShape shape_of(int rows, int width, bool vec, int at_once) {
     ResShape s;
-    s.blocks = 1;
-    while (s.blocks * kResWarps * 256 < width) s.blocks *= 2;
+    s.blocks = (width + kResWarps * 256 - 1) / (kResWarps * 256);
     s.warps = 1;
     while (s.warps * 256 < width && s.warps < kResWarps) s.warps *= 2;
     if (!vec && (s.warps == 2 || s.warps == 4)) s.warps = 8;
     s.groups = s.warps == 1 ? kResGroups : 1;
     const int need = (rows + s.groups - 1) / s.groups;
     int most = at_once * (s.warps >= 8 || s.warps == 1 ? 1 : 8 / s.warps);
-    if (s.warps == 16) most /= 2 * s.blocks;
+    most = most / s.blocks > 0 ? most / s.blocks : 1;
     s.clusters = need < most ? need : most;
     return s;
 }
-constexpr int kForwardBlocks = 148 * 4, kBackwardBlocks = 148 * 2;      // blocks of 8 warps
+constexpr int kForwardBlocks = 148 * 4, kBackwardBlocks = 148 * 3;      // blocks of 8 warps
 
 mpode_status check(const mpode_residual_desc* d, int rows, const char* who) {
     if (d == nullptr) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: null descriptor", who);
@@ -105,7 +109,7 @@ extern "C" {
 size_t mpode_residual_workspace_bytes(const mpode_residual_desc* desc, int rows) {
     if (check(desc, rows, "mpode_residual_workspace_bytes") != MPODE_OK || rows == 0) return 0;
     const size_t a = partial_rows(rows, desc->width, true), b = partial_rows(rows, desc->width, false);
-    return (a > b ? a : b) * 3 * desc->width * sizeof(float);
+    return (a > b ? a : b) * 2 * desc->width * sizeof(float);
 }
 
 mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_stream, int rows, const float* y_dev, const void* u_dev,
@@ -170,8 +174,8 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
         if (ran != MPODE_OK || !weights) return ran;
     }
     if (!weights) return MPODE_OK;
-    FinishArgs f{a.partial, {dL_dw_post_dev, dL_dscale_dev, dL_dw_pre_dev}, partials, desc->width, accumulate};
-    residual_finish_kernel<<<(3 * desc->width + 31) / 32, dim3(32, 16), 0, st>>>(f);
+    FinishArgs f{a.partial, w_post_dev, scale_dev, dL_dw_post_dev, dL_dscale_dev, dL_dw_pre_dev, partials, desc->width, accumulate};
+    residual_finish_kernel<<<(2 * desc->width + 31) / 32, dim3(32, 16), 0, st>>>(f);
     return operator_launched(cudaGetLastError(), who);
 }
 

@@ -15,7 +15,7 @@ struct ResArgs {
     // backward
     const float* dy; const void* dz;
     float* dy_out; void *du, *dgate;
-    float* partial;                               // [blocks * groups][3][width]: dw_post, dscale, dw_pre, or null when no weight gradient is asked for
+    float* partial;                               // [rows of blocks][2][width]: see residual_backward.cu; null when no weight gradient is asked for
     float cot_in, cot_out;                        // 2^-e, 2^e
     unsigned* flag;
     long long ld_y, ld_u, ld_gate, ld_z;
@@ -26,16 +26,19 @@ struct ResArgs {
 
 // How rows are spread: warps of a row in a block, rows in a block, blocks of a row (a cluster), clusters
 struct ResShape { int warps, groups, blocks, clusters; };
-constexpr int kResWarps = 16, kResBlocks = 4, kResMaxWidth = kResWarps * 256 * kResBlocks, kResGroups = 8;
+constexpr int kResWarps = 8, kResBlocks = 8, kResMaxWidth = kResWarps * 256 * kResBlocks, kResGroups = 8;
 
 cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
 cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
 
 #ifdef __CUDACC__
+__device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
+
 // Where a thread stands.  WARPS warps a row; one warp: eight rows a block.  CLUSTER: the row goes on in the other blocks of the cluster.
 template <int WARPS, bool CLUSTER> struct Lane {
     static constexpr int kGroups = WARPS == 1 ? kResGroups : 1, kThreads = 32 * WARPS * kGroups;
-    int group, warp, blocks, rank, col, n, first, step;      // column and how many columns exist; first row and distance of the rows
+    // base, cols: the block's part of a row; col, n: the thread's first column and how many exist; first row and distance of the rows
+    int group, warp, blocks, rank, base, cols, col, n, first, step;
     __device__ __forceinline__ Lane(int width, int blocks_) {
         const int t = threadIdx.x;
         group = WARPS == 1 ? t >> 5 : 0;
@@ -43,8 +46,11 @@ template <int WARPS, bool CLUSTER> struct Lane {
         blocks = CLUSTER ? blocks_ : 1;
         const int cluster = CLUSTER ? (int)(blockIdx.x / blocks) : (int)blockIdx.x;
         rank = CLUSTER ? (int)(blockIdx.x - cluster * blocks) : 0;
-        col = (rank * 32 * WARPS + (WARPS == 1 ? t & 31 : t)) * 8;
-        n = min(8, width - col);
+        const int part = CLUSTER ? (width + 8 * blocks - 1) / (8 * blocks) * 8 : width;
+        base = rank * part;
+        cols = max(0, min(part, width - base));
+        col = base + (WARPS == 1 ? t & 31 : t) * 8;
+        n = min(8, base + cols - col);
         first = cluster * kGroups + group;
         step = (CLUSTER ? (int)(gridDim.x / blocks) : (int)gridDim.x) * kGroups;
     }
@@ -125,10 +131,91 @@ template <int N, int WARPS, bool CLUSTER> struct RowSum {
     }
 };
 
-__device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
-template <bool VEC> __device__ __forceinline__ void load_weights(const float* w, int col, int n, Oct& o) {
+// Where a thread reads its rows (arrays 0 .. N - 1: WIDE float32 ones, then low ones), four columns at a time and as often as it needs them.
+//   VEC:  whole rows are copied to shared memory by bulk copies, kStages rows ahead; one thread of the row asks for them.
+//   else: from global memory.
+template <typename T, bool VEC, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows;
+template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T, true, WARPS, CLUSTER, WIDE, LOW> {
+    using L = Lane<WARPS, CLUSTER>;
+    static constexpr int kStages = 2, kCols = WARPS * 256, kWide = kCols * 4, kLow = kCols * (int)sizeof(T), kStage = WIDE * kWide + LOW * kLow;
+    static constexpr size_t kBytes = (size_t)L::kGroups * (kStages * kStage + 16);
+    char* mine;              // this row's stages
+    unsigned bar, bytes_wide, bytes_low, parity = 0;
+    int stage = 0, at;       // column of the thread in the block's part of the row
+    bool broken = false, leader;
+    __device__ __forceinline__ Rows(char* smem, const L& q) {
+        mine = smem + q.group * kStages * kStage;
+        bar = smem_of(smem + L::kGroups * kStages * kStage) + q.group * 16;
+        bytes_wide = q.cols * 4; bytes_low = q.cols * (unsigned)sizeof(T);
+        at = q.col - q.base;
+        leader = WARPS == 1 ? (threadIdx.x & 31) == 0 : threadIdx.x == 0;
+        if (q.n <= 0)        // columns that do not exist are zero
+            for (int s = 0; s < kStages; ++s) {
+                for (int k = 0; k < WIDE; ++k)
+                    for (int h = 0; h < 8; ++h) reinterpret_cast<float*>(mine + s * kStage + k * kWide)[at + h] = 0.f;
+                for (int k = 0; k < LOW; ++k)
+                    for (int h = 0; h < 8; ++h) reinterpret_cast<T*>(mine + s * kStage + WIDE * kWide + k * kLow)[at + h] = Low<T>::from_f(0.f);
+            }
+        if (leader)
+            for (int s = 0; s < kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        sync();
+    }
+    __device__ __forceinline__ void sync() const {
+        if (WARPS == 1) __syncwarp();
+        else __syncthreads();
+    }
+    // by the leader, for the arrays that are there: from[k] is the row's first column of this block, or null
+    __device__ __forceinline__ void request(int s, const void* const (&from)[WIDE + LOW]) {
+        unsigned bytes = 0;
+#pragma unroll
+        for (int k = 0; k < WIDE + LOW; ++k)
+            if (from[k] != nullptr) bytes += k < WIDE ? bytes_wide : bytes_low;          // (none in a block without columns)
+        set_expects(bar + 8 * s, bytes);
+#pragma unroll
+        for (int k = 0; k < WIDE + LOW; ++k)
+            if (from[k] != nullptr && bytes > 0)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(smem_of(mine + s * kStage + (k < WIDE ? k * kWide : WIDE * kWide + (k - WIDE) * kLow))), "l"(from[k]),
+                               "r"(k < WIDE ? bytes_wide : bytes_low), "r"(bar + 8 * s) : "memory");
+    }
+    __device__ __forceinline__ void wait() { wait_set(bar + 8 * stage, parity, broken); }
+    __device__ __forceinline__ int slot() const { return stage; }
+    __device__ __forceinline__ void done() {
+        if (++stage == kStages) { stage = 0; parity ^= 1; }
+    }
+    template <int K> __device__ __forceinline__ Quad get(int h) const {
+        if constexpr (K < WIDE) return load4<float, true>(reinterpret_cast<const float*>(mine + stage * kStage + K * kWide) + at + 4 * h, 4);
+        else return load4<T, true>(reinterpret_cast<const T*>(mine + stage * kStage + WIDE * kWide + (K - WIDE) * kLow) + at + 4 * h, 4);
+    }
+};
+template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T, false, WARPS, CLUSTER, WIDE, LOW> {
+    using L = Lane<WARPS, CLUSTER>;
+    static constexpr int kStages = 0;
+    static constexpr size_t kBytes = 0;
+    const void* row[WIDE + LOW];
+    int at, n;
+    bool broken = false, leader = false;
+    __device__ __forceinline__ Rows(char*, const L& q) : at(q.col - q.base), n(q.n) {}
+    __device__ __forceinline__ void sync() const {}
+    __device__ __forceinline__ void request(int, const void* const (&from)[WIDE + LOW]) {
+#pragma unroll
+        for (int k = 0; k < WIDE + LOW; ++k) row[k] = from[k];
+    }
+    __device__ __forceinline__ void wait() {}
+    __device__ __forceinline__ int slot() const { return 0; }
+    __device__ __forceinline__ void done() {}
+    template <int K> __device__ __forceinline__ Quad get(int h) const {
+        if constexpr (K < WIDE) return load4<float, false>((const float*)row[K] + at + 4 * h, n - 4 * h);
+        else return load4<T, false>((const T*)row[K] + at + 4 * h, n - 4 * h);
+    }
+};
+
+template <bool VEC> __device__ __forceinline__ Oct weights_of(const float* w, int col, int n) {
+    Oct o;
     if (w == nullptr) o.fill(1.f);
     else load8<float, VEC>(w + col, n, o);
+    return o;
 }
 
 // sigmoid and its slope sig (1 - sig) = e sig^2 with e = exp(-g).  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the
@@ -179,8 +266,7 @@ inline cudaError_t launch_rows(void (*kernel)(const ResArgs, const int), const R
 template <int N> struct Int { static constexpr int value = N; };
 template <bool B> struct Bool { static constexpr bool value = B; };
 template <typename F> cudaError_t with_shape(const ResShape& s, F&& f) {
-    if (s.blocks > 1) return f(Int<16>(), Bool<true>());
-    if (s.warps == 16) return f(Int<16>(), Bool<false>());
+    if (s.blocks > 1) return f(Int<8>(), Bool<true>());
     if (s.warps == 8) return f(Int<8>(), Bool<false>());
     if (s.warps == 4) return f(Int<4>(), Bool<false>());
     if (s.warps == 2) return f(Int<2>(), Bool<false>());

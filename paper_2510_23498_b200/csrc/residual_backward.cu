@@ -1,221 +1,178 @@
 // Backward pass of the residual step: adjoint, cotangents and the weights' gradients of a row in one pass.
+//
+// With y, u the rows (less their means), r, s their reciprocal deviations, c = scale w_post, and drop() for the mask with the kept elements' factor:
+//   e = r dz,  dw_pre += e y,  a = dy' + w_pre e - y r^2 mean(w_pre e y) - mean(w_pre e)
+//   t = h s drop(a),  q = t u,  S += q sig,  dgate = c q sig',  du = c t sig - u s^2 mean(c q sig) - mean(c t sig)
+// where the last means are taken only with MEANVAR; dw_post = scale S and dscale = w_post S come from one sum over the rows, formed behind the last one.
+//
+// A row goes through three phases with a sum over the row between them.  Its inputs lie in shared memory and are read again in the next phase: what a
+// thread keeps of its eight columns are two gradients and two weights (32 registers) and one product, so that three blocks of 8 warps fit an SM and one's
+// sums are hidden behind another's arithmetic.
 #include "residual.cuh"
 
 namespace mpode {
 namespace {
 
-// A thread's own pieces of the rows y', dy', dz, u and gate (0 .. 4).  VEC: copied to shared memory by asynchronous copies some rows ahead; a thread reads
-// what it has copied itself, so that nothing has to be waited for but its own copies.  Else loaded into registers when the row starts.
-template <typename T, bool VEC, int threads> struct Rows;
-template <typename T, int threads> struct Rows<T, true, threads> {
-    static constexpr int kStages = sizeof(T) == 4 ? 2 : 3, kLow = sizeof(T) / 2, kPieces = 4 + 3 * kLow;
-    uint4* at;
-    __device__ __forceinline__ void bind(char* smem, int n) {
-        at = reinterpret_cast<uint4*>(smem) + threadIdx.x;
-        if (n <= 0)                                         // columns that do not exist are zero
-            for (int i = 0; i < kStages * kPieces; ++i) at[i * threads] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    static __device__ __forceinline__ constexpr int first(int k) { return k < 2 ? 2 * k : 4 + (k - 2) * kLow; }
-    template <typename E> __device__ __forceinline__ void request(int stage, int k, const E* from, int n) {
-        if (n <= 0) return;
-#pragma unroll
-        for (int j = 0; j < (int)sizeof(E) / 2; ++j)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_of(at + (stage * kPieces + first(k) + j) * threads)), "l"(reinterpret_cast<const uint4*>(from) + j) : "memory");
-    }
-    __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
-    template <typename E> __device__ __forceinline__ void raw(int stage, int k, Raw8<E>& r) const {
-#pragma unroll
-        for (int j = 0; j < (int)sizeof(E) / 2; ++j) {
-            const uint4 v = at[(stage * kPieces + first(k) + j) * threads];
-            r.w[4 * j] = v.x; r.w[4 * j + 1] = v.y; r.w[4 * j + 2] = v.z; r.w[4 * j + 3] = v.w;
-        }
-    }
-    __device__ __forceinline__ void get(int stage, int k, Oct& o) const {
-        if (k < 2) {
-            Raw8<float> r;
-            raw<float>(stage, k, r);
-            unpack<float>(r, o);
-        } else {
-            Raw8<T> r;
-            raw<T>(stage, k, r);
-            unpack<T>(r, o);
-        }
-    }
-};
-template <typename T, int threads> struct Rows<T, false, threads> {
-    static constexpr int kStages = 1;
-    Raw8<float> wide[2];
-    Raw8<T> low[3];
-    __device__ __forceinline__ void bind(char*, int) {}
-    template <typename E> __device__ __forceinline__ void request(int, int k, const E* from, int n) {
-        if constexpr (std::is_same<E, T>::value && !std::is_same<T, float>::value) load_raw<T, false>(from, n, low[k - 2]);
-        else if (k < 2) load_raw<float, false>((const float*)from, n, wide[k]);
-        else load_raw<T, false>((const T*)from, n, low[k - 2]);
-    }
-    __device__ __forceinline__ void commit() {}
-    __device__ __forceinline__ void wait() {}
-    __device__ __forceinline__ void raw(int, int k, Raw8<T>& r) const { r = low[k - 2]; }
-    __device__ __forceinline__ void get(int, int k, Oct& o) const {
-        if (k < 2) unpack<float>(wide[k], o);
-        else unpack<T>(low[k - 2], o);
-    }
-};
-
-// With n' the normalised y', n that of u, and t the cotangent of the step's term:
-//   a = dy' + r' (w dz - n' mean(w dz n') - mean(w dz)),  dw_pre += dz n';   t = drop(a), dscale += h t v sig, with v = w_post n;
-//   t <- h scale t, dgate = t v sig', t <- t sig, dw_post += t n, du = r (w t - n mean(w t n) - mean(w t)); the means of w dz and w t only for MEANVAR
 template <typename T, bool VEC, bool CENTER, int WARPS, bool CLUSTER>
-__global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, WARPS == 16 ? 1 : 512 / Lane<WARPS, CLUSTER>::kThreads) residual_backward_kernel(const ResArgs p, const int blocks) {
+__global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, WARPS == 1 ? 2 : 768 / Lane<WARPS, CLUSTER>::kThreads)
+residual_backward_kernel(const ResArgs p, const int blocks) {
     constexpr int N = CENTER ? 2 : 1;
     using Sum = RowSum<N, WARPS, CLUSTER>;
+    using In = Rows<T, VEC, WARPS, CLUSTER, 2, 3>;          // y', dy', dz, u, gate
     extern __shared__ __align__(16) char staged[];
     __shared__ typename Sum::Shared shared;
     const Lane<WARPS, CLUSTER> q(p.width, blocks);
     Sum sum(shared, blocks);
+    In in(staged, q);
     const uint64_t seed = p.drop.on ? p.drop.rng[0] : 0, step = p.drop.on ? p.drop.rng[1] : 0;
     const int groups_row = (p.width + 7) / 8;
     const float inv = 1.f / (float)p.width;
-    const bool exists = q.n > 0;
-    Oct gw_post, gscale, gw_pre;
-    gw_post.fill(0.f); gscale.fill(0.f); gw_pre.fill(0.f);
-    Largest<T> largest;
-    int row = q.first;
-    Rows<T, VEC, Lane<WARPS, CLUSTER>::kThreads> in;
-    in.bind(staged, q.n);
-    float4 stats = make_float4(0.f, 1.f, 0.f, 1.f);
+    const bool has_dz = p.dz != nullptr, has_dy = p.dy != nullptr, has_u = p.u != nullptr, has_gate = p.gate != nullptr;
     auto request = [&](long long r, int stage) {
-        if (r < p.rows) {
-            if (p.dz != nullptr) {
-                in.request(stage, 0, p.y + r * p.ld_y + q.col, q.n);
-                in.request(stage, 2, (const T*)p.dz + r * p.ld_z + q.col, q.n);
-            }
-            if (p.dy != nullptr) in.request(stage, 1, p.dy + r * p.ld_y + q.col, q.n);
-            if (p.u != nullptr) in.request(stage, 3, (const T*)p.u + r * p.ld_u + q.col, q.n);
-            if (p.gate != nullptr) in.request(stage, 4, (const T*)p.gate + r * p.ld_gate + q.col, q.n);
-        }
-        in.commit();
+        const int c = q.base;
+        const void* const from[5] = {has_dz ? p.y + r * p.ld_y + c : nullptr, has_dy ? p.dy + r * p.ld_y + c : nullptr,
+                                     has_dz ? (const T*)p.dz + r * p.ld_z + c : nullptr, has_u ? (const T*)p.u + r * p.ld_u + c : nullptr,
+                                     has_gate ? (const T*)p.gate + r * p.ld_gate + c : nullptr};
+        in.request(stage, from);
     };
-    if (VEC)
-        for (int k = 0; k < in.kStages; ++k) request(row + (long long)k * q.step, k);
+    if (in.leader)
+        for (int k = 0; k < in.kStages; ++k)
+            if (q.first + (long long)k * q.step < p.rows) request(q.first + (long long)k * q.step, k);
+    Oct S, gw_pre, w_pre = weights_of<VEC>(p.w_pre, q.col, q.n), c = weights_of<VEC>(p.scale, q.col, q.n);
+    {
+        const Oct w_post = weights_of<VEC>(p.w_post, q.col, q.n);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c.v[k] = __fmul2_rn(c.v[k], w_post.v[k]);
+    }
+    S.fill(0.f); gw_pre.fill(0.f);
+    Largest<T> largest;
+    float4 stats = make_float4(0.f, 1.f, 0.f, 1.f);
+    int row = q.first;
     if (p.stats != nullptr && row < p.rows) stats = reinterpret_cast<const float4*>(p.stats)[row];
-    int stage = 0;
+    // the row's means, negative; the first one times `factor`
+    auto means = [&](float2 m0, float2 m1, int kind, float factor, float2& n0, float2& n1) {
+        n0 = n1 = pair(0.f);
+        if (kind == MPODE_NORM_NONE) return;
+        float m[N];
+        m[0] = m0.x + m0.y;
+        if (CENTER) m[N - 1] = m1.x + m1.y;
+        sum(m, q);
+        n0 = pair(-m[0] * inv * factor);
+        if (CENTER && kind == MPODE_NORM_MEANVAR) n1 = pair(-m[N - 1] * inv);
+    };
+    auto less = [&](Quad v, float2 mean) {
+        if (CENTER) { v.v[0] = __fadd2_rn(v.v[0], mean); v.v[1] = __fadd2_rn(v.v[1], mean); }
+        return v;
+    };
     while (row < p.rows) {
         const int next = q.step < p.rows - row ? row + q.step : p.rows;
         const float4 st = stats;
         if (p.stats != nullptr && next < p.rows) stats = reinterpret_cast<const float4*>(p.stats)[next];
         if (!VEC) request(row, 0);
         in.wait();
-        Oct a, y, d, w;
-        Raw8<T> un, gn;                                     // unpacked where they are used
-        if (p.dy != nullptr) in.get(stage, 1, a);
-        else a.fill(0.f);
-        if (p.dz != nullptr) {
-            in.get(stage, 0, y);
-            in.get(stage, 2, d);
-        }
-        if (p.u != nullptr) in.raw(stage, 3, un);
-        if (p.gate != nullptr) in.raw(stage, 4, gn);
-        if (p.dz != nullptr) {
-            load_weights<VEC>(p.w_pre, q.col, q.n, w);
-            float2 m0 = pair(0.f), m1 = pair(0.f);
+        const float s_u = st.y, r_y = in.broken ? __int_as_float(0x7fffffff) : st.w;
+        float2 m0 = pair(0.f), m1 = pair(0.f), n0, n1;
+        Oct kept;                                           // w_pre e, then c t sig
+        kept.fill(0.f);
+        if (has_dz) {
+            const float2 k = pair(p.cot_in * r_y);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (CENTER) y.v[j] = __fadd2_rn(y.v[j], pair(-st.z));
-                y.v[j] = __fmul2_rn(y.v[j], pair(st.w));
-                d.v[j] = __fmul2_rn(d.v[j], pair(p.cot_in));
-                gw_pre.v[j] = __ffma2_rn(d.v[j], y.v[j], gw_pre.v[j]);
-                d.v[j] = __fmul2_rn(d.v[j], w.v[j]);
-                m0 = __ffma2_rn(d.v[j], y.v[j], m0);
-                if (CENTER) m1 = __fadd2_rn(m1, d.v[j]);
-            }
-            if (p.pre != MPODE_NORM_NONE) {
-                float m[N];
-                m[0] = m0.x + m0.y;
-                if (CENTER) m[N - 1] = m1.x + m1.y;
-                sum(m, q);
-                m0 = pair(-m[0] * inv);
-                m1 = pair(CENTER && p.pre == MPODE_NORM_MEANVAR ? -m[N - 1] * inv : 0.f);
-            } else m0 = m1 = pair(0.f);
+            for (int h = 0; h < 2; ++h) {
+                const Quad y = less(in.template get<0>(h), pair(-st.z)), dz = in.template get<2>(h);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (CENTER) d.v[j] = __fadd2_rn(d.v[j], m1);
-                a.v[j] = __ffma2_rn(__ffma2_rn(y.v[j], m0, d.v[j]), pair(st.w), a.v[j]);
+                for (int j = 0; j < 2; ++j) {
+                    const int i = 2 * h + j;
+                    const float2 e = __fmul2_rn(dz.v[j], k);
+                    gw_pre.v[i] = __ffma2_rn(e, y.v[j], gw_pre.v[i]);
+                    kept.v[i] = __fmul2_rn(e, w_pre.v[i]);
+                    m0 = __ffma2_rn(kept.v[i], y.v[j], m0);
+                    if (CENTER) m1 = __fadd2_rn(m1, kept.v[i]);
+                }
             }
+            means(m0, m1, p.pre, r_y * r_y, n0, n1);
         }
-        store8<float, VEC>(p.dy_out + row * p.ld_y + q.col, q.n, a);
-        if (p.u != nullptr) {
-        Oct u, g, c;
-        unpack<T>(un, u);
-        if (p.gate != nullptr) unpack<T>(gn, g);
         Kept keep;
         if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
-        load_weights<VEC>(p.w_post, q.col, q.n, w);
-        load_weights<VEC>(p.scale, q.col, q.n, c);
-        float2 m0 = pair(0.f), m1 = pair(0.f);
+        m0 = m1 = pair(0.f);
+        const float2 hs = pair(p.h * p.drop.scale * s_u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (CENTER) u.v[j] = __fadd2_rn(u.v[j], pair(-st.x));
-            u.v[j] = __fmul2_rn(u.v[j], pair(st.y));
-            float2 t = __fmul2_rn(a.v[j], pair(p.h * p.drop.scale));
-            if (p.drop.on) {
-                if (!keep[2 * j]) t.x = 0.f;
-                if (!keep[2 * j + 1]) t.y = 0.f;
+        for (int h = 0; h < 2; ++h) {
+            Quad a;
+            a.v[0] = kept.v[2 * h]; a.v[1] = kept.v[2 * h + 1];
+            if (has_dy) {
+                const Quad dy = in.template get<1>(h);
+                a.v[0] = __fadd2_rn(a.v[0], dy.v[0]); a.v[1] = __fadd2_rn(a.v[1], dy.v[1]);
             }
-            if (VEC ? !exists : 2 * j >= q.n) t.x = 0.f;    // columns that do not exist add nothing to the sums
-            if (VEC ? !exists : 2 * j + 1 >= q.n) t.y = 0.f;
-            const float2 v = __fmul2_rn(u.v[j], w.v[j]);
-            if (p.gate != nullptr) {
-                float2 slope;
-                const float2 sig = gate_of<T, true>(g.v[j], slope);
-                gscale.v[j] = __ffma2_rn(t, __fmul2_rn(v, sig), gscale.v[j]);
-                t = __fmul2_rn(t, c.v[j]);
-                g.v[j] = __fmul2_rn(__fmul2_rn(t, v), __fmul2_rn(slope, pair(p.cot_out)));
-                t = __fmul2_rn(t, sig);
-            } else {
-                gscale.v[j] = __ffma2_rn(t, v, gscale.v[j]);
-                t = __fmul2_rn(t, c.v[j]);
-            }
-            gw_post.v[j] = __ffma2_rn(t, u.v[j], gw_post.v[j]);
-            a.v[j] = __fmul2_rn(t, w.v[j]);
-            m0 = __ffma2_rn(a.v[j], u.v[j], m0);
-            if (CENTER) m1 = __fadd2_rn(m1, a.v[j]);
-        }
-        Raw8<T> out;
-        if (p.dgate != nullptr) {
-            pack<T>(g, out);
-            if (p.flag != nullptr) largest.see(out, q.n);
-            store_raw<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col, q.n, out);
-        }
-        if (p.post != MPODE_NORM_NONE) {
-            float m[N];
-            m[0] = m0.x + m0.y;
-            if (CENTER) m[N - 1] = m1.x + m1.y;
-            sum(m, q);
-            m0 = pair(-m[0] * inv);
-            m1 = pair(CENTER && p.post == MPODE_NORM_MEANVAR ? -m[N - 1] * inv : 0.f);
-        } else m0 = m1 = pair(0.f);
+            if (has_dz) {
+                const Quad y = less(in.template get<0>(h), pair(-st.z));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (CENTER) a.v[j] = __fadd2_rn(a.v[j], m1);
-            a.v[j] = __fmul2_rn(__fmul2_rn(__ffma2_rn(u.v[j], m0, a.v[j]), pair(st.y)), pair(p.cot_out));
+                for (int j = 0; j < 2; ++j) {
+                    if (CENTER) a.v[j] = __fadd2_rn(a.v[j], n1);
+                    a.v[j] = __ffma2_rn(y.v[j], n0, a.v[j]);
+                }
+            }
+            if (!VEC || q.n > 0) store4<float, VEC>(p.dy_out + row * p.ld_y + q.col + 4 * h, q.n - 4 * h, a);
+            if (!has_u) continue;
+            const Quad u = less(in.template get<3>(h), pair(-st.x));
+            Quad g;
+            if (has_gate) g = in.template get<4>(h);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = 2 * h + j;
+                float2 t = __fmul2_rn(a.v[j], hs);
+                if (p.drop.on) {
+                    if (!keep[2 * i]) t.x = 0.f;
+                    if (!keep[2 * i + 1]) t.y = 0.f;
+                }
+                if (CENTER) {                               // columns that do not exist, which the means would fill
+                    if (2 * i >= q.n) t.x = 0.f;
+                    if (2 * i + 1 >= q.n) t.y = 0.f;
+                }
+                float2 x = __fmul2_rn(t, u.v[j]);
+                if (has_gate) {
+                    float2 slope;
+                    const float2 sig = gate_of<T, true>(g.v[j], slope);
+                    g.v[j] = __fmul2_rn(__fmul2_rn(x, slope), __fmul2_rn(c.v[i], pair(p.cot_out)));
+                    x = __fmul2_rn(x, sig);
+                    t = __fmul2_rn(t, sig);
+                }
+                S.v[i] = __fadd2_rn(S.v[i], x);
+                m0 = __ffma2_rn(x, c.v[i], m0);
+                kept.v[i] = __fmul2_rn(t, c.v[i]);
+                if (CENTER) m1 = __fadd2_rn(m1, kept.v[i]);
+            }
+            if (has_gate && (!VEC || q.n > 0)) {
+                if (p.flag != nullptr) largest.see(g, q.n - 4 * h);
+                store4<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col + 4 * h, q.n - 4 * h, g);
+            }
         }
-        pack<T>(a, out);
-        if (p.flag != nullptr) largest.see(out, q.n);
-        store_raw<T, VEC>((T*)p.du + row * p.ld_u + q.col, q.n, out);
+        if (has_u) {
+            means(m0, m1, p.post, s_u * s_u, n0, n1);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                Quad u = less(in.template get<3>(h), pair(-st.x));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float2 t = kept.v[2 * h + j];
+                    if (CENTER) t = __fadd2_rn(t, n1);
+                    u.v[j] = __fmul2_rn(__ffma2_rn(u.v[j], n0, t), pair(p.cot_out));
+                }
+                if (!VEC || q.n > 0) {
+                    if (p.flag != nullptr) largest.see(u, q.n - 4 * h);
+                    store4<T, VEC>((T*)p.du + row * p.ld_u + q.col + 4 * h, q.n - 4 * h, u);
+                }
+            }
         }
-        if (VEC) {                                          // this row's pieces have been used: its stage is free
-            request(row + (long long)in.kStages * q.step, stage);
-            stage = stage + 1 < in.kStages ? stage + 1 : 0;
-        }
+        in.sync();                                          // everyone has read this stage
+        if (in.leader && row + (long long)in.kStages * q.step < p.rows) request(row + (long long)in.kStages * q.step, in.slot());
+        in.done();
         row = next;
     }
     warp_flag_or(p.flag, largest.nonfinite());
     if (p.partial != nullptr) {
-        float* out = p.partial + (long long)q.first * 3 * p.width + q.col;
-        store8<float, VEC>(out, q.n, gw_post);
-        store8<float, VEC>(out + p.width, q.n, gscale);
-        store8<float, VEC>(out + 2 * p.width, q.n, gw_pre);
+        float* out = p.partial + (long long)q.first * 2 * p.width + q.col;
+        store8<float, VEC>(out, q.n, S);
+        store8<float, VEC>(out + p.width, q.n, gw_pre);
     }
     sum.end();
 }
@@ -228,8 +185,7 @@ cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const Res
         return with_shape(s, [&](auto warps, auto cluster) {
             constexpr int W = warps.value;
             constexpr bool C = cluster.value;
-            using R = Rows<T, true, Lane<W, C>::kThreads>;
-            const size_t smem = (size_t)Lane<W, C>::kThreads * R::kStages * R::kPieces * 16;
+            constexpr size_t smem = Rows<T, true, W, C, 2, 3>::kBytes;
             if (!vec) {
                 if constexpr (W == 2 || W == 4) return cudaErrorInvalidValue;
                 else return launch_rows(residual_backward_kernel<T, false, true, W, C>, a, s, 0, st);

@@ -1,4 +1,5 @@
-// Forward pass of the residual step: z and y' of a row in one pass, the row in registers while its sums meet.
+// Forward pass of the residual step: z and y' of a row in one pass.  The row's inputs lie in shared memory, where the sum over u and the step read them; y' stays
+// in registers while its sum meets.  Four blocks of 8 warps an SM hide one's sums behind another's arithmetic.
 #include "residual.cuh"
 
 namespace mpode {
@@ -6,93 +7,121 @@ namespace {
 
 // CENTER: one of the norms takes the mean away
 template <typename T, bool VEC, bool CENTER, int WARPS, bool CLUSTER>
-__global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 768 / Lane<WARPS, CLUSTER>::kThreads) residual_forward_kernel(const ResArgs p, const int blocks) {
+__global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WARPS, CLUSTER>::kThreads) residual_forward_kernel(const ResArgs p, const int blocks) {
     using Sum = RowSum<1, WARPS, CLUSTER>;
+    using In = Rows<T, VEC, WARPS, CLUSTER, 1, 2>;          // y, u, gate
+    extern __shared__ __align__(16) char staged[];
     __shared__ typename Sum::Shared shared;
     const Lane<WARPS, CLUSTER> q(p.width, blocks);
     Sum sum(shared, blocks);
+    In in(staged, q);
     const uint64_t seed = p.drop.on ? p.drop.rng[0] : 0, step = p.drop.on ? p.drop.rng[1] : 0;
     const int groups_row = (p.width + 7) / 8;
     const float inv = 1.f / (float)p.width;
-    // mean and 1 / deviation of the row (zero where no elements exist)
-    auto stats_of = [&](const Oct& f, int kind, float& mean, float& rstd) {
-        mean = 0.f;
-        rstd = 1.f;
-        if (kind == MPODE_NORM_NONE) return;
-        if (CENTER && kind == MPODE_NORM_MEANVAR) {
-            float v[1] = {f.sum()};
-            sum(v, q);
-            mean = v[0] * inv;
-        }
-        float2 sq = pair(0.f);
-        const float2 less = pair(-mean);
+    const bool has_u = p.u != nullptr, has_gate = p.gate != nullptr;
+    auto request = [&](long long r, int stage) {
+        const void* const from[3] = {p.y + r * p.ld_y + q.base, has_u ? (const T*)p.u + r * p.ld_u + q.base : nullptr,
+                                     has_gate ? (const T*)p.gate + r * p.ld_gate + q.base : nullptr};
+        in.request(stage, from);
+    };
+    if (in.leader)
+        for (int k = 0; k < in.kStages; ++k)
+            if (q.first + (long long)k * q.step < p.rows) request(q.first + (long long)k * q.step, k);
+    Oct w_pre = weights_of<VEC>(p.w_pre, q.col, q.n), c = weights_of<VEC>(p.scale, q.col, q.n);        // c = scale w_post
+    {
+        const Oct w_post = weights_of<VEC>(p.w_post, q.col, q.n);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float2 d = f.v[j];
-            if (CENTER) {
-                d = __fadd2_rn(d, less);
-                if (2 * j >= q.n) d.x = 0.f;
-                if (2 * j + 1 >= q.n) d.y = 0.f;
-            }
-            sq = __ffma2_rn(d, d, sq);
-        }
-        float v[1] = {sq.x + sq.y};
+        for (int k = 0; k < 4; ++k) c.v[k] = __fmul2_rn(c.v[k], w_post.v[k]);
+    }
+    // less the mean, zero where no columns exist
+    auto less = [&](float2 v, float mean, int i) {
+        v = __fadd2_rn(v, pair(-mean));
+        if (2 * i >= q.n) v.x = 0.f;
+        if (2 * i + 1 >= q.n) v.y = 0.f;
+        return v;
+    };
+    auto total = [&](float2 f) {
+        float v[1] = {f.x + f.y};
         sum(v, q);
-        rstd = rsqrtf(fmaf(v[0], inv, p.eps));
+        return v[0] * inv;
     };
     int row = q.first;
-    // the next row is on its way while this one's sums meet
-    Raw8<float> yr;
-    Raw8<T> ur, gr;
-    auto request = [&](int r) {
-        load_raw<float, VEC>(p.y + r * p.ld_y + q.col, q.n, yr);
-        if (p.u != nullptr) load_raw<T, VEC>((const T*)p.u + r * p.ld_u + q.col, q.n, ur);
-        if (p.gate != nullptr) load_raw<T, VEC>((const T*)p.gate + r * p.ld_gate + q.col, q.n, gr);
-    };
-    if (row < p.rows) request(row);
     while (row < p.rows) {
         const int next = q.step < p.rows - row ? row + q.step : p.rows;
         float mean_u = 0.f, rstd_u = 1.f, mean_y = 0.f, rstd_y = 1.f;
-        Oct y, u, g;
-        unpack<float>(yr, y);
-        if (p.u != nullptr) unpack<T>(ur, u);
-        if (p.gate != nullptr) unpack<T>(gr, g);
-        if (next < p.rows) request(next);
-        if (p.u != nullptr) {
-            Oct w, c;
+        if (!VEC) request(row, 0);
+        in.wait();
+        Oct y;
+        if (has_u) {
+            if (CENTER && p.post == MPODE_NORM_MEANVAR) {
+                float2 s = pair(0.f);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const Quad u = in.template get<1>(h);
+                    s = __fadd2_rn(s, __fadd2_rn(u.v[0], u.v[1]));
+                }
+                mean_u = total(s);
+            }
+            if (p.post != MPODE_NORM_NONE) {
+                float2 s = pair(0.f);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    Quad u = in.template get<1>(h);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (CENTER) u.v[j] = less(u.v[j], mean_u, 2 * h + j);
+                        s = __ffma2_rn(u.v[j], u.v[j], s);
+                    }
+                }
+                rstd_u = rsqrtf(total(s) + p.eps);
+            }
             Kept keep;
             if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
-            stats_of(u, p.post, mean_u, rstd_u);
-            load_weights<VEC>(p.w_post, q.col, q.n, w);
-            load_weights<VEC>(p.scale, q.col, q.n, c);
-            const float2 less = pair(-mean_u), r = pair(rstd_u), h = pair(p.h * p.drop.scale);
+            const float2 k = pair((in.broken ? __int_as_float(0x7fffffff) : p.h) * p.drop.scale * rstd_u);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float2 v = u.v[j], slope;
-                if (CENTER) v = __fadd2_rn(v, less);
-                v = __fmul2_rn(__fmul2_rn(v, r), w.v[j]);
-                if (p.gate != nullptr) v = __fmul2_rn(v, gate_of<T, false>(g.v[j], slope));
-                v = __fmul2_rn(v, __fmul2_rn(h, c.v[j]));
-                if (p.drop.on) {
-                    if (!keep[2 * j]) v.x = 0.f;
-                    if (!keep[2 * j + 1]) v.y = 0.f;
+            for (int h = 0; h < 2; ++h) {
+                const Quad u = in.template get<1>(h), yh = in.template get<0>(h);
+                Quad g;
+                if (has_gate) g = in.template get<2>(h);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int i = 2 * h + j;
+                    float2 v = u.v[j], slope;
+                    if (CENTER) v = less(v, mean_u, i);
+                    v = __fmul2_rn(__fmul2_rn(v, k), c.v[i]);
+                    if (has_gate) v = __fmul2_rn(v, gate_of<T, false>(g.v[j], slope));
+                    if (p.drop.on) {
+                        if (!keep[2 * i]) v.x = 0.f;
+                        if (!keep[2 * i + 1]) v.y = 0.f;
+                    }
+                    y.v[i] = __fadd2_rn(yh.v[j], v);
                 }
-                if (2 * j >= q.n) v.x = 0.f;                 // columns that do not exist stay zero in the sums below
-                if (2 * j + 1 >= q.n) v.y = 0.f;
-                y.v[j] = __fadd2_rn(y.v[j], v);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Quad yh = in.template get<0>(h);
+                y.v[2 * h] = yh.v[0];
+                y.v[2 * h + 1] = yh.v[1];
             }
         }
+        in.sync();                                          // everyone has read this stage
+        if (in.leader && row + (long long)in.kStages * q.step < p.rows) request(row + (long long)in.kStages * q.step, in.slot());
+        in.done();
         if (p.y_out != nullptr) store8<float, VEC>(p.y_out + row * p.ld_y + q.col, q.n, y);
         if (p.z != nullptr) {
-            Oct w;
-            stats_of(y, p.pre, mean_y, rstd_y);
-            load_weights<VEC>(p.w_pre, q.col, q.n, w);
-            const float2 less = pair(-mean_y), r = pair(rstd_y);
+            if (CENTER && p.pre == MPODE_NORM_MEANVAR) mean_y = total(__fadd2_rn(__fadd2_rn(y.v[0], y.v[1]), __fadd2_rn(y.v[2], y.v[3])));
+            if (p.pre != MPODE_NORM_NONE) {
+                float2 s = pair(0.f);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (CENTER) y.v[j] = __fadd2_rn(y.v[j], less);
-                y.v[j] = __fmul2_rn(__fmul2_rn(y.v[j], r), w.v[j]);
+                for (int i = 0; i < 4; ++i) {
+                    if (CENTER) y.v[i] = less(y.v[i], mean_y, i);
+                    s = __ffma2_rn(y.v[i], y.v[i], s);
+                }
+                rstd_y = rsqrtf(total(s) + p.eps);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y.v[i] = __fmul2_rn(__fmul2_rn(y.v[i], pair(rstd_y)), w_pre.v[i]);
             store8<T, VEC>((T*)p.z + row * p.ld_z + q.col, q.n, y);
         }
         if (p.stats != nullptr && q.col == 0) reinterpret_cast<float4*>(p.stats)[row] = make_float4(mean_u, rstd_u, mean_y, rstd_y);
@@ -109,11 +138,13 @@ cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResS
         return with_shape(s, [&](auto warps, auto cluster) {
             constexpr int W = warps.value;
             constexpr bool C = cluster.value;
+            constexpr size_t smem = Rows<T, true, W, C, 1, 2>::kBytes;
             if (!vec) {
                 if constexpr (W == 2 || W == 4) return cudaErrorInvalidValue;
                 else return launch_rows(residual_forward_kernel<T, false, true, W, C>, a, s, 0, st);
             }
-            return center ? launch_rows(residual_forward_kernel<T, true, true, W, C>, a, s, 0, st) : launch_rows(residual_forward_kernel<T, true, false, W, C>, a, s, 0, st);
+            return center ? launch_rows(residual_forward_kernel<T, true, true, W, C>, a, s, smem, st)
+                          : launch_rows(residual_forward_kernel<T, true, false, W, C>, a, s, smem, st);
         });
     });
 }

@@ -102,6 +102,38 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
     store_raw<T, VEC>(p, n, r);
 }
 
+// Four neighbouring elements (a half of the above): as pairs of float32, and their accesses
+struct Quad { float2 v[2]; };
+template <typename T, bool VEC> __device__ __forceinline__ Quad load4(const T* p, int n) {
+    Quad q;
+    if constexpr (VEC) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = *reinterpret_cast<const float4*>(p);
+            q.v[0] = make_float2(a.x, a.y); q.v[1] = make_float2(a.z, a.w);
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(p);
+            q.v[0] = Pair<T>::get(a.x); q.v[1] = Pair<T>::get(a.y);
+        }
+    } else {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = i < n ? Low<T>::to_f(p[i]) : 0.f;
+        q.v[0] = make_float2(f[0], f[1]); q.v[1] = make_float2(f[2], f[3]);
+    }
+    return q;
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store4(T* p, int n, const Quad& q) {
+    if constexpr (VEC) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(q.v[0].x, q.v[0].y, q.v[1].x, q.v[1].y);
+        else *reinterpret_cast<uint2*>(p) = make_uint2(Pair<T>::put(q.v[0].x, q.v[0].y), Pair<T>::put(q.v[1].x, q.v[1].y));
+    } else {
+        const float f[4] = {q.v[0].x, q.v[0].y, q.v[1].x, q.v[1].y};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = Low<T>::from_f(f[i]);
+    }
+}
+
 // Largest magnitude of the low-format values seen, as bits (infinities and NaN above every number): two instructions a word
 template <typename T> struct Largest {
     uint32_t m = 0;
@@ -116,6 +148,21 @@ template <typename T> struct Largest {
                 const bool half = sizeof(T) == 2 && j * 2 + 1 == n;          // an odd row's last word holds one element
                 see(half ? r.w[j] & 0xffffu : r.w[j]);
             }
+    }
+    // of four elements as they are stored
+    __device__ __forceinline__ void see(const Quad& q, int n) {
+        if constexpr (sizeof(T) == 4) {
+            const float f[4] = {q.v[0].x, q.v[0].y, q.v[1].x, q.v[1].y};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) see(__float_as_uint(f[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w = Pair<T>::put(q.v[i].x, q.v[i].y);
+                if (2 * i < n) see(2 * i + 1 < n ? w : w & 0xffffu);
+            }
+        }
     }
     __device__ __forceinline__ bool nonfinite() const {
         if constexpr (sizeof(T) == 4) return m >= 0x7f800000u;
