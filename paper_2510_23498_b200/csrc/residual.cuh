@@ -139,22 +139,25 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
     using L = Lane<WARPS, CLUSTER>;
     static constexpr int kStages = 2, kCols = WARPS * 256, kWide = kCols * 4, kLow = kCols * (int)sizeof(T), kStage = WIDE * kWide + LOW * kLow;
     static constexpr size_t kBytes = (size_t)L::kGroups * (kStages * kStage + 16);
-    char* mine;              // this row's stages
+    unsigned mine, at_wide, at_low;      // this row's stages, the thread's columns of the first wide and the first low array in the first one
     unsigned bar, bytes_wide, bytes_low, parity = 0;
-    int stage = 0, at;       // column of the thread in the block's part of the row
+    int stage = 0;
     bool broken = false, leader;
     __device__ __forceinline__ Rows(char* smem, const L& q) {
-        mine = smem + q.group * kStages * kStage;
+        char* const rows = smem + q.group * kStages * kStage;
+        mine = smem_of(rows);
         bar = smem_of(smem + L::kGroups * kStages * kStage) + q.group * 16;
         bytes_wide = q.cols * 4; bytes_low = q.cols * (unsigned)sizeof(T);
-        at = q.col - q.base;
+        const int at = q.col - q.base;
+        at_wide = mine + at * 4;
+        at_low = mine + WIDE * kWide + at * (unsigned)sizeof(T);
         leader = WARPS == 1 ? (threadIdx.x & 31) == 0 : threadIdx.x == 0;
         if (q.n <= 0)        // columns that do not exist are zero
             for (int s = 0; s < kStages; ++s) {
                 for (int k = 0; k < WIDE; ++k)
-                    for (int h = 0; h < 8; ++h) reinterpret_cast<float*>(mine + s * kStage + k * kWide)[at + h] = 0.f;
+                    for (int h = 0; h < 8; ++h) reinterpret_cast<float*>(rows + s * kStage + k * kWide)[at + h] = 0.f;
                 for (int k = 0; k < LOW; ++k)
-                    for (int h = 0; h < 8; ++h) reinterpret_cast<T*>(mine + s * kStage + WIDE * kWide + k * kLow)[at + h] = Low<T>::from_f(0.f);
+                    for (int h = 0; h < 8; ++h) reinterpret_cast<T*>(rows + s * kStage + WIDE * kWide + k * kLow)[at + h] = Low<T>::from_f(0.f);
             }
         if (leader)
             for (int s = 0; s < kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
@@ -176,7 +179,7 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
         for (int k = 0; k < WIDE + LOW; ++k)
             if (from[k] != nullptr && bytes > 0)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(smem_of(mine + s * kStage + (k < WIDE ? k * kWide : WIDE * kWide + (k - WIDE) * kLow))), "l"(from[k]),
+                             ::"r"(mine + s * kStage + (k < WIDE ? k * kWide : WIDE * kWide + (k - WIDE) * kLow)), "l"(from[k]),
                                "r"(k < WIDE ? bytes_wide : bytes_low), "r"(bar + 8 * s) : "memory");
     }
     __device__ __forceinline__ void wait() { wait_set(bar + 8 * stage, parity, broken); }
@@ -185,8 +188,17 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
         if (++stage == kStages) { stage = 0; parity ^= 1; }
     }
     template <int K> __device__ __forceinline__ Quad get(int h) const {
-        if constexpr (K < WIDE) return load4<float, true>(reinterpret_cast<const float*>(mine + stage * kStage + K * kWide) + at + 4 * h, 4);
-        else return load4<T, true>(reinterpret_cast<const T*>(mine + stage * kStage + WIDE * kWide + (K - WIDE) * kLow) + at + 4 * h, 4);
+        Quad q;
+        if constexpr (K < WIDE || sizeof(T) == 4) {
+            const unsigned a = (K < WIDE ? at_wide + K * kWide : at_low + (K - WIDE) * kLow) + stage * kStage + 16 * h;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.v[0].x), "=f"(q.v[0].y), "=f"(q.v[1].x), "=f"(q.v[1].y) : "r"(a));
+        } else {
+            uint32_t x, y;
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at_low + (K - WIDE) * kLow + stage * kStage + 8 * h));
+            q.v[0] = Pair<T>::get(x);
+            q.v[1] = Pair<T>::get(y);
+        }
+        return q;
     }
 };
 template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T, false, WARPS, CLUSTER, WIDE, LOW> {
