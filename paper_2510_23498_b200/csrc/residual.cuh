@@ -35,10 +35,13 @@ cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const Res
 __device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
 
 // Where a thread stands.  WARPS warps a row; one warp: eight rows a block.  CLUSTER: the row goes on in the other blocks of the cluster.
+// A thread has two times four neighbouring columns, the second four half a block's columns further on, so that the lanes' accesses lie side by side (eight
+// neighbouring columns a thread had twice the shared-memory cycles).
 template <int WARPS, bool CLUSTER> struct Lane {
     static constexpr int kGroups = WARPS == 1 ? kResGroups : 1, kThreads = 32 * WARPS * kGroups;
-    // base, cols: the block's part of a row; col, n: the thread's first column and how many exist; first row and distance of the rows
-    int group, warp, blocks, rank, base, cols, col, n, first, step;
+    // base, cols: the block's part of a row; at: the thread's first column in it; first row and distance of the rows
+    int group, warp, blocks, rank, base, cols, at, first, step;
+    static constexpr int kHalf = 128 * WARPS;
     __device__ __forceinline__ Lane(int width, int blocks_) {
         const int t = threadIdx.x;
         group = WARPS == 1 ? t >> 5 : 0;
@@ -49,11 +52,12 @@ template <int WARPS, bool CLUSTER> struct Lane {
         const int part = CLUSTER ? (width + 8 * blocks - 1) / (8 * blocks) * 8 : width;
         base = rank * part;
         cols = max(0, min(part, width - base));
-        col = base + (WARPS == 1 ? t & 31 : t) * 8;
-        n = min(8, base + cols - col);
+        at = (WARPS == 1 ? t & 31 : t) * 4;
         first = cluster * kGroups + group;
         step = (CLUSTER ? (int)(gridDim.x / blocks) : (int)gridDim.x) * kGroups;
     }
+    __device__ __forceinline__ int col(int h) const { return base + at + h * kHalf; }        // first column of the thread's quad h
+    __device__ __forceinline__ int n(int h) const { return cols - at - h * kHalf; }          // columns that exist from there on, or less than one
 };
 
 // Sums over a row's threads, the same bits in all of them.  One warp: shuffles.  One block: partial sums of its warps in shared memory.  A cluster: every
@@ -148,17 +152,18 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
         mine = smem_of(rows);
         bar = smem_of(smem + L::kGroups * kStages * kStage) + q.group * 16;
         bytes_wide = q.cols * 4; bytes_low = q.cols * (unsigned)sizeof(T);
-        const int at = q.col - q.base;
-        at_wide = mine + at * 4;
-        at_low = mine + WIDE * kWide + at * (unsigned)sizeof(T);
+        at_wide = mine + q.at * 4;
+        at_low = mine + WIDE * kWide + q.at * (unsigned)sizeof(T);
         leader = WARPS == 1 ? (threadIdx.x & 31) == 0 : threadIdx.x == 0;
-        if (q.n <= 0)        // columns that do not exist are zero
-            for (int s = 0; s < kStages; ++s) {
-                for (int k = 0; k < WIDE; ++k)
-                    for (int h = 0; h < 8; ++h) reinterpret_cast<float*>(rows + s * kStage + k * kWide)[at + h] = 0.f;
-                for (int k = 0; k < LOW; ++k)
-                    for (int h = 0; h < 8; ++h) reinterpret_cast<T*>(rows + s * kStage + WIDE * kWide + k * kLow)[at + h] = Low<T>::from_f(0.f);
-            }
+        for (int h = 0; h < 2; ++h)
+            if (q.n(h) <= 0)                         // columns that do not exist are zero
+                for (int s = 0; s < kStages; ++s) {
+                    const int at = q.at + h * L::kHalf;
+                    for (int k = 0; k < WIDE; ++k)
+                        for (int i = 0; i < 4; ++i) reinterpret_cast<float*>(rows + s * kStage + k * kWide)[at + i] = 0.f;
+                    for (int k = 0; k < LOW; ++k)
+                        for (int i = 0; i < 4; ++i) reinterpret_cast<T*>(rows + s * kStage + WIDE * kWide + k * kLow)[at + i] = Low<T>::from_f(0.f);
+                }
         if (leader)
             for (int s = 0; s < kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -190,11 +195,11 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
     template <int K> __device__ __forceinline__ Quad get(int h) const {
         Quad q;
         if constexpr (K < WIDE || sizeof(T) == 4) {
-            const unsigned a = (K < WIDE ? at_wide + K * kWide : at_low + (K - WIDE) * kLow) + stage * kStage + 16 * h;
+            const unsigned a = (K < WIDE ? at_wide + K * kWide : at_low + (K - WIDE) * kLow) + stage * kStage + L::kHalf * 4 * h;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.v[0].x), "=f"(q.v[0].y), "=f"(q.v[1].x), "=f"(q.v[1].y) : "r"(a));
         } else {
             uint32_t x, y;
-            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at_low + (K - WIDE) * kLow + stage * kStage + 8 * h));
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at_low + (K - WIDE) * kLow + stage * kStage + L::kHalf * 2 * h));
             q.v[0] = Pair<T>::get(x);
             q.v[1] = Pair<T>::get(y);
         }
@@ -208,7 +213,7 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
     const void* row[WIDE + LOW];
     int at, n;
     bool broken = false, leader = false;
-    __device__ __forceinline__ Rows(char*, const L& q) : at(q.col - q.base), n(q.n) {}
+    __device__ __forceinline__ Rows(char*, const L& q) : at(q.at), n(q.n(0)) {}
     __device__ __forceinline__ void sync() const {}
     __device__ __forceinline__ void request(int, const void* const (&from)[WIDE + LOW]) {
 #pragma unroll
@@ -218,17 +223,47 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
     __device__ __forceinline__ int slot() const { return 0; }
     __device__ __forceinline__ void done() {}
     template <int K> __device__ __forceinline__ Quad get(int h) const {
-        if constexpr (K < WIDE) return load4<float, false>((const float*)row[K] + at + 4 * h, n - 4 * h);
-        else return load4<T, false>((const T*)row[K] + at + 4 * h, n - 4 * h);
+        if constexpr (K < WIDE) return load4<float, false>((const float*)row[K] + at + L::kHalf * h, n - L::kHalf * h);
+        else return load4<T, false>((const T*)row[K] + at + L::kHalf * h, n - L::kHalf * h);
     }
 };
 
-template <bool VEC> __device__ __forceinline__ Oct weights_of(const float* w, int col, int n) {
+// weights of the thread's columns, ones where there are none
+template <bool VEC, int W, bool C> __device__ __forceinline__ Oct weights_of(const float* w, const Lane<W, C>& q) {
     Oct o;
-    if (w == nullptr) o.fill(1.f);
-    else load8<float, VEC>(w + col, n, o);
+    o.fill(w == nullptr ? 1.f : 0.f);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (w != nullptr && q.n(h) > 0) {
+            const Quad f = load4<float, VEC>(w + q.col(h), q.n(h));
+            o.v[2 * h] = f.v[0];
+            o.v[2 * h + 1] = f.v[1];
+        }
     return o;
 }
+template <typename T, bool VEC, int W, bool C> __device__ __forceinline__ void store_row(T* row, const Lane<W, C>& q, const Oct& o) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (q.n(h) > 0) store4<T, VEC>(row + q.col(h), q.n(h), Quad{{o.v[2 * h], o.v[2 * h + 1]}});
+}
+// Which of the thread's columns dropout keeps.  Two neighbouring lanes need a half each of the same two counters' words: each works one of them out and
+// gives the other lane its half.
+struct KeptRow {
+    uint32_t w[2][2], above;
+    template <int W, bool C> __device__ __forceinline__ void draw(const Dropout& d, uint64_t first, const Lane<W, C>& q, uint64_t seed, uint64_t step) {
+        const bool odd = threadIdx.x & 1;
+        above = d.above;
+        const Kept k(d, first + (q.col(0) + (odd ? q.kHalf : 0)) / 8, seed, step);
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, odd ? k.w.x : k.w.z, 1), y = __shfl_xor_sync(0xffffffffu, odd ? k.w.y : k.w.w, 1);
+        w[0][0] = odd ? x : k.w.x; w[0][1] = odd ? y : k.w.y;
+        w[1][0] = odd ? k.w.z : x; w[1][1] = odd ? k.w.w : y;
+    }
+    // element i of the thread's eight
+    __device__ __forceinline__ bool operator[](int i) const {
+        const uint32_t r = w[i >> 2][(i >> 1) & 1];
+        return (i & 1 ? r : r << 16) > above;
+    }
+};
 
 // sigmoid and its slope sig (1 - sig) = e sig^2 with e = exp(-g).  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the
 // argument's rounding adds |g| 2^-24); the exponent is kept below 2^126, so that e sig^2 is finite.

@@ -38,9 +38,9 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
     if (in.leader)
         for (int k = 0; k < in.kStages; ++k)
             if (q.first + (long long)k * q.step < p.rows) request(q.first + (long long)k * q.step, k);
-    Oct S, gw_pre, w_pre = weights_of<VEC>(p.w_pre, q.col, q.n), c = weights_of<VEC>(p.scale, q.col, q.n);
+    Oct S, gw_pre, w_pre = weights_of<VEC>(p.w_pre, q), c = weights_of<VEC>(p.scale, q);
     {
-        const Oct w_post = weights_of<VEC>(p.w_post, q.col, q.n);
+        const Oct w_post = weights_of<VEC>(p.w_post, q);
 #pragma unroll
         for (int k = 0; k < 4; ++k) c.v[k] = __fmul2_rn(c.v[k], w_post.v[k]);
     }
@@ -91,8 +91,8 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
             }
             means(m0, m1, p.pre, r_y * r_y, n0, n1);
         }
-        Kept keep;
-        if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
+        KeptRow keep;
+        if (p.drop.on) keep.draw(p.drop, (uint64_t)row * groups_row, q, seed, step);
         m0 = m1 = pair(0.f);
         const float2 hs = pair(p.h * p.drop.scale * s_u);
 #pragma unroll
@@ -111,7 +111,7 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
                     a.v[j] = __ffma2_rn(y.v[j], n0, a.v[j]);
                 }
             }
-            if (!VEC || q.n > 0) store4<float, VEC>(p.dy_out + row * p.ld_y + q.col + 4 * h, q.n - 4 * h, a);
+            if (q.n(h) > 0) store4<float, VEC>(p.dy_out + row * p.ld_y + q.col(h), q.n(h), a);
             if (!has_u) continue;
             const Quad u = less(in.template get<3>(h), pair(-st.x));
             Quad g;
@@ -125,8 +125,8 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
                     if (!keep[2 * i + 1]) t.y = 0.f;
                 }
                 if (CENTER) {                               // columns that do not exist, which the means would fill
-                    if (2 * i >= q.n) t.x = 0.f;
-                    if (2 * i + 1 >= q.n) t.y = 0.f;
+                    if (2 * j >= q.n(h)) t.x = 0.f;
+                    if (2 * j + 1 >= q.n(h)) t.y = 0.f;
                 }
                 float2 x = __fmul2_rn(t, u.v[j]);
                 if (has_gate) {
@@ -141,9 +141,9 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
                 kept.v[i] = __fmul2_rn(t, c.v[i]);
                 if (CENTER) m1 = __fadd2_rn(m1, kept.v[i]);
             }
-            if (has_gate && (!VEC || q.n > 0)) {
-                if (p.flag != nullptr) largest.see(g, q.n - 4 * h);
-                store4<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col + 4 * h, q.n - 4 * h, g);
+            if (has_gate && q.n(h) > 0) {
+                if (p.flag != nullptr) largest.see(g, q.n(h));
+                store4<T, VEC>((T*)p.dgate + row * p.ld_gate + q.col(h), q.n(h), g);
             }
         }
         if (has_u) {
@@ -157,9 +157,9 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
                     if (CENTER) t = __fadd2_rn(t, n1);
                     u.v[j] = __fmul2_rn(__ffma2_rn(u.v[j], n0, t), pair(p.cot_out));
                 }
-                if (!VEC || q.n > 0) {
-                    if (p.flag != nullptr) largest.see(u, q.n - 4 * h);
-                    store4<T, VEC>((T*)p.du + row * p.ld_u + q.col + 4 * h, q.n - 4 * h, u);
+                if (q.n(h) > 0) {
+                    if (p.flag != nullptr) largest.see(u, q.n(h));
+                    store4<T, VEC>((T*)p.du + row * p.ld_u + q.col(h), q.n(h), u);
                 }
             }
         }
@@ -170,9 +170,9 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
     }
     warp_flag_or(p.flag, largest.nonfinite());
     if (p.partial != nullptr) {
-        float* out = p.partial + (long long)q.first * 2 * p.width + q.col;
-        store8<float, VEC>(out, q.n, S);
-        store8<float, VEC>(out + p.width, q.n, gw_pre);
+        float* out = p.partial + (long long)q.first * 2 * p.width;
+        store_row<float, VEC>(out, q, S);
+        store_row<float, VEC>(out + p.width, q, gw_pre);
     }
     sum.end();
 }

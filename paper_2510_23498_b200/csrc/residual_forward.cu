@@ -27,17 +27,17 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
     if (in.leader)
         for (int k = 0; k < in.kStages; ++k)
             if (q.first + (long long)k * q.step < p.rows) request(q.first + (long long)k * q.step, k);
-    Oct w_pre = weights_of<VEC>(p.w_pre, q.col, q.n), c = weights_of<VEC>(p.scale, q.col, q.n);        // c = scale w_post
+    Oct w_pre = weights_of<VEC>(p.w_pre, q), c = weights_of<VEC>(p.scale, q);        // c = scale w_post
     {
-        const Oct w_post = weights_of<VEC>(p.w_post, q.col, q.n);
+        const Oct w_post = weights_of<VEC>(p.w_post, q);
 #pragma unroll
         for (int k = 0; k < 4; ++k) c.v[k] = __fmul2_rn(c.v[k], w_post.v[k]);
     }
     // less the mean, zero where no columns exist
     auto less = [&](float2 v, float mean, int i) {
         v = __fadd2_rn(v, pair(-mean));
-        if (2 * i >= q.n) v.x = 0.f;
-        if (2 * i + 1 >= q.n) v.y = 0.f;
+        if (2 * (i & 1) >= q.n(i >> 1)) v.x = 0.f;
+        if (2 * (i & 1) + 1 >= q.n(i >> 1)) v.y = 0.f;
         return v;
     };
     auto total = [&](float2 f) {
@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
                 }
                 rstd_u = rsqrtf(total(s) + p.eps);
             }
-            Kept keep;
-            if (p.drop.on) keep = Kept(p.drop, (uint64_t)row * groups_row + q.col / 8, seed, step);
+            KeptRow keep;
+            if (p.drop.on) keep.draw(p.drop, (uint64_t)row * groups_row, q, seed, step);
             const float2 k = pair((in.broken ? __int_as_float(0x7fffffff) : p.h) * p.drop.scale * rstd_u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
         in.sync();                                          // everyone has read this stage
         if (in.leader && row + (long long)in.kStages * q.step < p.rows) request(row + (long long)in.kStages * q.step, in.slot());
         in.done();
-        if (p.y_out != nullptr) store8<float, VEC>(p.y_out + row * p.ld_y + q.col, q.n, y);
+        if (p.y_out != nullptr) store_row<float, VEC>(p.y_out + row * p.ld_y, q, y);
         if (p.z != nullptr) {
             if (CENTER && p.pre == MPODE_NORM_MEANVAR) mean_y = total(__fadd2_rn(__fadd2_rn(y.v[0], y.v[1]), __fadd2_rn(y.v[2], y.v[3])));
             if (p.pre != MPODE_NORM_NONE) {
@@ -122,9 +122,9 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) y.v[i] = __fmul2_rn(__fmul2_rn(y.v[i], pair(rstd_y)), w_pre.v[i]);
-            store8<T, VEC>((T*)p.z + row * p.ld_z + q.col, q.n, y);
+            store_row<T, VEC>((T*)p.z + row * p.ld_z, q, y);
         }
-        if (p.stats != nullptr && q.col == 0) reinterpret_cast<float4*>(p.stats)[row] = make_float4(mean_u, rstd_u, mean_y, rstd_y);
+        if (p.stats != nullptr && q.col(0) == 0) reinterpret_cast<float4*>(p.stats)[row] = make_float4(mean_u, rstd_u, mean_y, rstd_y);
         row = next;
     }
     sum.end();
