@@ -22,6 +22,7 @@
 #include "cluster.cuh"
 #include "operators.h"
 #include "rows.cuh"
+#include "tensormap.h"
 
 namespace mpode {
 namespace {
@@ -36,7 +37,10 @@ struct RecArgs {
     unsigned* flag;
     long long in_seq, in_step, out_seq, out_step;
     int n_seq, n_steps, width;
+    int time_major;                    // STAGED: the maps' coordinates are (channel, sequence, step) instead of (channel, step, sequence)
 };
+// STAGED: tensor maps of gate and x (forward), of gate, dL/dy, y and x (backward)
+struct RecMaps { CUtensorMap m[4]; };
 
 // V channels of a row as one access: two (a 32-bit word, or 64 bits of float32), or one where widths or addresses are odd
 template <typename T, int V> struct Word;
@@ -318,73 +322,81 @@ template <int V> __device__ __forceinline__ Place place(const RecArgs& p, int bl
 template <bool B> struct Flag { static constexpr bool value = B; };
 
 // Where a warp finds its steps: a tile of N arrays, L steps of V channels a lane.
-//   STAGED: copied to shared memory 16 bytes at a time by asynchronous copies that run two rounds ahead (each warp its own two stages, so that
-//           no other warp has to be waited for), read from there as often as needed.  Rows of all arrays are multiples of 16 bytes from aligned pointers.
+//   STAGED: brought to shared memory by bulk tensor copies that run two rounds ahead (each warp its own two stages and barriers, so that no other warp has to
+//           be waited for), read from there as often as needed.  Rows of all arrays are multiples of 16 bytes from aligned pointers.  (Asynchronous
+//           copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
 //   else:   loaded into registers when the round starts.  For any alignment (V = 1), and for sequences of a round or two, where nothing runs ahead.
-// Step i of array k lies at base + off + i * step bytes: 32-bit offsets from an address that is the same for the whole block.
 template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 constexpr int kStages = 2;
+template <typename T, int V, int L, int N> constexpr int kWarpBytes = kStages * N * L * kRowBytes<T, V>;
 template <typename T, int V, int L, int N, bool STAGED> struct Tile;
 template <typename T, int V, int L, int N> struct Tile<T, V, L, N, false> {
     using word = typename Word<T, V>::type;
     word w[N][L];
-    unsigned lane;
-    __device__ __forceinline__ void bind(char*, int l) { lane = l * (unsigned)sizeof(word); }
-    template <bool FULL> __device__ __forceinline__ void request(int, int k, const char* base, unsigned off, unsigned step, int lo, int hi, int) {
-        off += lane;
+    // step i of array k lies at base + off + i * step bytes; steps lo .. hi - 1 exist
+    __device__ __forceinline__ void load(int k, const char* base, unsigned off, unsigned step, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < L; ++i, off += step) {
             w[k][i] = word_of<T, V>(0.f);
             if (i >= lo && i < hi) w[k][i] = *(const word*)(base + off);
         }
     }
-    __device__ __forceinline__ void commit() {}
-    __device__ __forceinline__ void wait() {}
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
 };
 template <typename T, int V, int L, int N> struct Tile<T, V, L, N, true> {
     using word = typename Word<T, V>::type;
-    static constexpr int kRow = kRowBytes<T, V>, kPieces = kRow / 16, kRows = 32 / kPieces;
-    static_assert(L % kRows == 0, "whole rows a copy");
-    char* at;
-    unsigned lane;
-    __device__ __forceinline__ void bind(char* smem, int l) {
-        at = smem + threadIdx.y * (kStages * N * L * kRow);
-        lane = l * (unsigned)sizeof(word);
-    }
-    // steps lo .. hi - 1 and `bytes` of a row exist; FULL: all of them
-    template <bool FULL> __device__ __forceinline__ void request(int stage, int k, const char* base, unsigned off, unsigned step, int lo, int hi, int bytes) {
-        const int piece = (threadIdx.x % kPieces) * 16;
-        int row = threadIdx.x / kPieces;
-        off += piece + row * step;
-        unsigned to = smem_of(at) + ((stage * N + k) * L + row) * kRow + piece;
-#pragma unroll
-        for (int j = 0; j < L / kRows; ++j, row += kRows, off += step * kRows, to += kRow * kRows)
-            if (FULL || (row >= lo && row < hi && piece < bytes)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(base + off) : "memory");
-    }
-    __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    __device__ __forceinline__ void wait() {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow;
+    unsigned at, lane, bar;
+    __device__ __forceinline__ void bind(char* smem, unsigned long long* bars, int l) {
+        at = smem_of(smem) + threadIdx.y * kWarpBytes<T, V, L, N>;
+        bar = smem_of(bars) + threadIdx.y * (kStages * 8);
+        lane = at + l * (unsigned)sizeof(word);
+        if (threadIdx.x == 0) {
+            sets_begin(bars + threadIdx.y * kStages);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
         __syncwarp();
     }
+    // one lane: L steps of `arrays` arrays from step t0[k] on, upwards; what lies outside is filled with zeros
+    __device__ __forceinline__ void request(int stage, const RecMaps& maps, unsigned mask, int tile, int seq, bool time_major, int t0, int t0_y) {
+        set_expects(bar + 8 * stage, __popc(mask) * kArray);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (mask >> k & 1) {
+                const int t = k == 2 ? t0_y : t0;
+                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                             ::"r"(at + (stage * N + k) * kArray), "l"(reinterpret_cast<unsigned long long>(&maps.m[k])), "r"(bar + 8 * stage), "r"(tile),
+                               "r"(time_major ? seq : t), "r"(time_major ? t : seq) : "memory");
+            }
+    }
+    __device__ __forceinline__ void wait(int stage, unsigned parity, bool& broken) { wait_set(bar + 8 * stage, parity, broken); }
     __device__ __forceinline__ word get(int stage, int k, int i) const {
-        return *(const word*)(at + ((stage * N + k) * L + i) * kRow + lane);
+        const unsigned a = lane + (stage * N + k) * kArray + i * kRow;
+        if constexpr (sizeof(word) == 8) {
+            float2 f;
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f.x), "=f"(f.y) : "r"(a));
+            return *reinterpret_cast<word*>(&f);
+        } else {
+            uint32_t u;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(a));
+            return *reinterpret_cast<word*>(&u);
+        }
     }
 };
 
 template <typename T, int V, bool COUPLED, int L, bool STAGED>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const int blocks) {
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
     using word = typename W::type;
-    extern __shared__ __align__(16) char staged[];
+    extern __shared__ __align__(128) char staged[];
     __shared__ Exchange<V> ex;
+    __shared__ unsigned long long arrived[STAGED ? kMaxWarps * kStages : 1];
     const Place q = place<V>(p, blocks);
     const bool alone = blocks == 1 && blockDim.y == 1;
     if (!alone) exchange_begin<V>(ex, blocks);
     const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es;
-    const unsigned in_at = q.tile * es + q.slot * L * in_step, out_at = q.col * es + q.slot * L * out_step;
-    const int row_bytes = (p.width - q.tile) * (int)es;
+    const unsigned in_at = q.col * es + q.slot * L * in_step, out_at = q.col * es + q.slot * L * out_step;
     const char* x = (const char*)p.x + q.seq * p.in_seq * es;
     const char* g = (const char*)p.gate + q.seq * p.in_seq * es;
     char* out = (char*)p.out + q.seq * p.out_seq * es;
@@ -398,33 +410,35 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
         if (COUPLED) carry[v] = -carry[v];
     }
     Tile<T, V, L, 2, STAGED> tile;
-    tile.bind(staged, q.lane);
     // steps of this warp's tile that exist
     auto count = [&](unsigned base) {
         const unsigned t0 = base + q.slot * L;
         return t0 < (unsigned)q.len ? (int)min((unsigned)L, (unsigned)q.len - t0) : 0;
     };
-    auto request = [&](auto full, unsigned base, int stage) {
-        const int n = count(base);
-        tile.template request<full.value>(stage, 0, x, in_at, in_step, 0, n, row_bytes);
-        tile.template request<full.value>(stage, 1, g, in_at, in_step, 0, n, row_bytes);
-        tile.commit();
-        x += in_round; g += in_round;
+    auto request = [&](unsigned base, int stage) {
+        if constexpr (STAGED)
+            if (threadIdx.x == 0 && base < (unsigned)q.len) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
     };
-    if (STAGED)
-        for (int k = 0; k < kStages; ++k) request(Flag<false>(), k * stride, k);
+    if constexpr (STAGED) {
+        tile.bind(staged, arrived, q.lane);
+        for (int k = 0; k < kStages; ++k) request(k * stride, k);
+    }
     if (blocks > 1) cluster_wait();
     unsigned round = 0;
-    // full: every step of the round exists; next: so does everything of the round that is requested
-    auto body = [&](auto full, auto next, unsigned base) {
+    // full: every step of the round exists
+    auto body = [&](auto full, unsigned base) {
         float nb[L][V], start[V];
         const int stage = round % kStages, n = count(base);
-        if (!STAGED) request(Flag<false>(), base, 0);
-        tile.wait();
+        if constexpr (STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+        else {
+            tile.load(0, g, in_at, in_step, 0, n);
+            tile.load(1, x, in_at, in_step, 0, n);
+            x += in_round; g += in_round;
+        }
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             float f[V], none[V];
-            W::get(tile.get(stage, 1, i), f);
+            W::get(tile.get(stage, 0, i), f);
             negated_gate<T, V, false>(f, nb[i], none);
             if (!full.value && i >= n) {                    // a step that does not exist keeps the state
 #pragma unroll
@@ -432,7 +446,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
             }
         }
         auto x_of = [&](int i, float (&xs)[V]) {
-            W::get(tile.get(stage, 0, i), xs);
+            W::get(tile.get(stage, 1, i), xs);
             if (!full.value && i >= n) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) xs[v] = 0.f;
@@ -463,21 +477,18 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
         out += out_round;
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = start[v];
+            for (int v = 0; v < V; ++v) carry[v] = STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
         }
         if (STAGED) {
             __syncwarp();                                   // all lanes have read this stage
-            request(next, base + kStages * stride, stage);
+            request(base + kStages * stride, stage);
         }
         ++round;
     };
     unsigned base = 0;
-    if (STAGED) {
-        if (row_bytes >= kRowBytes<T, V>)
-            for (; (unsigned long long)base + (kStages + 1) * stride <= (unsigned)q.len; base += stride) body(Flag<true>(), Flag<true>(), base);
-        for (; (unsigned long long)base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), Flag<false>(), base);
-    }
-    for (; base < (unsigned)q.len; base += stride) body(Flag<false>(), Flag<false>(), base);
+    if (STAGED)
+        for (; base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), base);
+    for (; base < (unsigned)q.len; base += stride) body(Flag<false>(), base);
     if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[state + v] = COUPLED ? -carry[v] : carry[v];
@@ -488,19 +499,19 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
 // Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
 template <typename T, int V, bool COUPLED, int L, bool STAGED>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const int blocks) {
+__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
     using word = typename W::type;
-    extern __shared__ __align__(16) char staged[];
+    extern __shared__ __align__(128) char staged[];
     __shared__ Exchange<V> ex;
+    __shared__ unsigned long long arrived[STAGED ? kMaxWarps * kStages : 1];
     const Place q = place<V>(p, blocks);
     const bool alone = blocks == 1 && blockDim.y == 1;
     if (!alone) exchange_begin<V>(ex, blocks);
     const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
     // offsets count down from the last time of the round
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es, back = (stride - 1) - q.slot * L;
-    const unsigned in_at = q.tile * es + back * in_step, out_at = q.tile * es + back * out_step, to_at = q.col * es + back * in_step;
-    const int row_bytes = (p.width - q.tile) * (int)es;
+    const unsigned in_at = q.col * es + back * in_step, out_at = q.col * es + back * out_step;
     const unsigned skipped = p.n_steps - q.len;             // steps at the start of the count that do not exist
     unsigned base = skipped / stride * stride;              // rounds that lie behind the sequence are passed over
     const long long in_round = (long long)stride * in_step, out_round = (long long)stride * out_step;
@@ -515,41 +526,46 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr ? p.dyT[state + v] : 0.f;
     Tile<T, V, L, COUPLED ? 4 : 3, STAGED> tile;
-    tile.bind(staged, q.lane);
     // the tile's steps lo .. hi - 1 exist
     auto range = [&](unsigned base, int& lo, int& hi) {
         const unsigned first = base + q.slot * L;
         lo = first < skipped ? (int)min((unsigned)L, skipped - first) : 0;
         hi = first < (unsigned)p.n_steps ? (int)min((unsigned)L, p.n_steps - first) : 0;
     };
-    auto request = [&](auto full, unsigned base, int stage) {
-        int lo, hi;
-        range(base, lo, hi);
-        const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;         // time 0 has no stored state in front of it
-        tile.template request<full.value>(stage, 0, g, in_at, 0u - in_step, lo, hi, row_bytes);
-        if (p.dy != nullptr) tile.template request<full.value>(stage, 1, dy, out_at, 0u - out_step, lo, hi, row_bytes);
-        tile.template request<full.value>(stage, 2, y, out_at, 0u - out_step, lo, before, row_bytes);
-        if constexpr (COUPLED) tile.template request<full.value>(stage, 3, x, in_at, 0u - in_step, lo, hi, row_bytes);
-        tile.commit();
-        x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
+    auto request = [&](unsigned base, int stage) {
+        if constexpr (STAGED)
+            if (threadIdx.x == 0 && base < (unsigned)p.n_steps) {
+                const int t0 = p.n_steps - (int)(base + q.slot * L) - L;                        // the tile's earliest time; its steps lie the other way round
+                tile.request(stage, maps, (COUPLED ? 13u : 5u) | (p.dy != nullptr ? 2u : 0u), q.tile, q.seq, p.time_major != 0, t0, t0 - 1);
+            }
     };
-    if (STAGED)
-        for (int k = 0; k < kStages; ++k) request(Flag<false>(), base + k * stride, k);
+    if constexpr (STAGED) {
+        tile.bind(staged, arrived, q.lane);
+        for (int k = 0; k < kStages; ++k) request(base + k * stride, k);
+    }
+    auto get = [&](int stage, int k, int i) { return tile.get(stage, k, STAGED ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
     unsigned round = 0;
     const bool no_dy = p.dy == nullptr;
-    auto body = [&](auto full, auto next) {
+    auto body = [&](auto full) {
         float nb[L][V], slope[L][V], start[V];
         const int stage = round % kStages;
         int lo, hi;
         range(base, lo, hi);
         const int zero = (int)(p.n_steps - 1 - (base + q.slot * L));                            // index of time 0
-        if (!STAGED) request(Flag<false>(), base, 0);
-        tile.wait();
+        if constexpr (STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+        else {
+            const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;     // time 0 has no stored state in front of it
+            tile.load(0, g, in_at, 0u - in_step, lo, hi);
+            if (!no_dy) tile.load(1, dy, out_at, 0u - out_step, lo, hi);
+            tile.load(2, y, out_at, 0u - out_step, lo, before);
+            if constexpr (COUPLED) tile.load(3, x, in_at, 0u - in_step, lo, hi);
+            x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
+        }
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             float f[V];
-            W::get(tile.get(stage, 0, i), f);
+            W::get(get(stage, 0, i), f);
             negated_gate<T, V, true>(f, nb[i], slope[i]);
             if (!full.value && (i < lo || i >= hi)) {                                           // a step that does not exist keeps the adjoint
 #pragma unroll
@@ -557,7 +573,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
             }
         }
         auto dy_of = [&](int i, float (&d)[V]) {
-            W::get(tile.get(stage, 1, i), d);
+            W::get(get(stage, 1, i), d);
             if (no_dy || (!full.value && (i < lo || i >= hi))) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[v] = 0.f;
@@ -578,12 +594,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
 #pragma unroll
             for (int v = 0; v < V; ++v) start[v] = carry[v];
         }
-        unsigned at = to_at;
+        unsigned at = in_at;
 #pragma unroll
         for (int i = 0; i < L; ++i, at -= in_step) {
             float ys[V], d[V], l[V], gx[V], gg[V];
             dy_of(i, d);
-            W::get(tile.get(stage, 2, i), ys);
+            W::get(get(stage, 2, i), ys);
             if (!full.value && i == zero) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[state + v] : 0.f;
@@ -593,7 +609,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
             Ops<V>::mul(gg, slope[i], l);
             if constexpr (COUPLED) {
                 float xs[V], minus[V];
-                W::get(tile.get(stage, 3, i), xs);
+                W::get(get(stage, 3, i), xs);
                 Ops<V>::mul(gx, nb[i], l);
 #pragma unroll
                 for (int v = 0; v < V; ++v) minus[v] = -1.f;
@@ -609,24 +625,22 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
         }
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = start[v];
+            for (int v = 0; v < V; ++v) carry[v] = STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
         }
         dx -= in_round; dg -= in_round;
         if (STAGED) {
             __syncwarp();
-            request(next, base + kStages * stride, stage);
+            request(base + kStages * stride, stage);
         }
         base += stride;
         ++round;
     };
     // (a full round does not hold time 0)
     if (STAGED) {
-        if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>(), Flag<false>());
-        if (row_bytes >= kRowBytes<T, V>)
-            while ((unsigned long long)base + (kStages + 1) * stride < (unsigned)p.n_steps) body(Flag<true>(), Flag<true>());
-        while ((unsigned long long)base + stride < (unsigned)p.n_steps) body(Flag<true>(), Flag<false>());
+        if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>());
+        while (base + stride < (unsigned)p.n_steps) body(Flag<true>());
     }
-    while (base < (unsigned)p.n_steps) body(Flag<false>(), Flag<false>());
+    while (base < (unsigned)p.n_steps) body(Flag<false>());
     if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[state + v] = carry[v];
@@ -653,7 +667,7 @@ Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int lanes_width
     return s;
 }
 
-cudaError_t launch(void (*kernel)(const RecArgs, const int), const RecArgs& a, const Shape& s, size_t smem, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), const RecArgs& a, const RecMaps& maps, const Shape& s, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.tiles * s.blocks));
     cfg.blockDim = dim3(32, s.warps);
@@ -673,7 +687,7 @@ cudaError_t launch(void (*kernel)(const RecArgs, const int), const RecArgs& a, c
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
     }
-    return cudaLaunchKernelEx(&cfg, kernel, a, s.blocks);
+    return cudaLaunchKernelEx(&cfg, kernel, a, maps, s.blocks);
 }
 
 template <typename T, int V> constexpr int kForwardSteps = sizeof(T) * V > 4 ? 8 : 16;
@@ -688,19 +702,36 @@ bool pieces_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
         if (misaligned(q, 16)) return false;
     return true;
 }
-template <typename T, int V, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
+// maps of [n_seq][n_steps][width] with boxes of L steps; the dimension with the larger stride comes last
+bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long long step, int channels, int steps, bool time_major, CUtensorMap* out) {
+    return time_major ? make_tensor_map(p, d.low, d.width, d.n_seq, d.n_steps, seq, step, channels, 1, steps, out)
+                      : make_tensor_map(p, d.low, d.width, d.n_steps, d.n_seq, step, seq, channels, steps, 1, out);
+}
+template <typename T, int V, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, RecArgs a, cudaStream_t st) {
     constexpr int L = BACKWARD ? kBackwardSteps<T, V> : kForwardSteps<T, V>;
     const Shape s = shape_of(d, a, 32 * V, L);
+    RecMaps maps;
     if constexpr (V == 2) {
         if (d.n_steps > 2 * s.warps * s.blocks * L && pieces_fit(d, a)) {
-            constexpr int arrays = BACKWARD ? (COUPLED ? 4 : 3) : 2;
-            const size_t smem = (size_t)s.warps * kStages * arrays * L * kRowBytes<T, V>;
-            if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, true>, a, s, smem, st);
-            else return launch(recurrence_forward_kernel<T, V, COUPLED, L, true>, a, s, smem, st);
+            constexpr int N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
+            a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;
+            // (all arrays take the coordinates in one order: where inputs and outputs differ in theirs, registers)
+            bool ok = a.time_major == (d.n_seq > 1 && a.out_seq < a.out_step);
+            const bool tm = a.time_major != 0;
+            ok = ok && map_of(a.gate, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[0]);
+            if constexpr (BACKWARD) {
+                if (ok && a.dy != nullptr) ok = map_of(a.dy, d, a.out_seq, a.out_step, 32 * V, L, tm, &maps.m[1]);
+                ok = ok && map_of(a.y, d, a.out_seq, a.out_step, 32 * V, L, tm, &maps.m[2]);
+                if (COUPLED) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[3]);
+                if (ok) return launch(recurrence_backward_kernel<T, V, COUPLED, L, true>, a, maps, s, s.warps * kWarpBytes<T, V, L, N>, st);
+            } else {
+                ok = ok && map_of(a.x, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[1]);
+                if (ok) return launch(recurrence_forward_kernel<T, V, COUPLED, L, true>, a, maps, s, s.warps * kWarpBytes<T, V, L, N>, st);
+            }
         }
     }
-    if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, false>, a, s, 0, st);
-    else return launch(recurrence_forward_kernel<T, V, COUPLED, L, false>, a, s, 0, st);
+    if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, false>, a, maps, s, 0, st);
+    else return launch(recurrence_forward_kernel<T, V, COUPLED, L, false>, a, maps, s, 0, st);
 }
 template <bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, bool two, cudaStream_t st) {
     return with_low(d.low, [&](auto t) {

@@ -105,6 +105,21 @@ bool get_tensor_map_nhwc(const void* ptr, int B, int H, int W, int C, int box_h,
     return true;
 }
 
+bool make_tensor_map(const void* ptr, mpode_dtype dt, long long d0, long long d1, long long d2, long long s1, long long s2, int b0, int b1, int b2,
+                     CUtensorMap* out) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t es = low_size(dt);
+    cuuint64_t gdim[3] = {(cuuint64_t)d0, (cuuint64_t)d1, (cuuint64_t)d2};
+    cuuint64_t gstr[2] = {(cuuint64_t)s1 * es, (cuuint64_t)s2 * es};
+    cuuint32_t box[3] = {(cuuint32_t)b0, (cuuint32_t)b1, (cuuint32_t)b2};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUtensorMapDataType type = dt == MPODE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                     : (dt == MPODE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+    return fn(out, type, 3, const_cast<void*>(ptr), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int current_device() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {

@@ -22,6 +22,11 @@ bool get_tensor_map_3d(const void* ptr, long long slots, long long rows, long lo
 // rows; coordinates outside the image (the zero padding of a convolution) read as zero.
 bool get_tensor_map_nhwc(const void* ptr, int B, int H, int W, int C, int box_h, mpode_dtype dt, CUtensorMap* out);
 
+// Map of a [d2][d1][d0] tensor of any format with strides s1, s2 in elements (multiples of 16 bytes), box [b2][b1][b0], rows as they are (no swizzle),
+// out-of-range elements read as zero.  Not cached.
+bool make_tensor_map(const void* ptr, mpode_dtype dt, long long d0, long long d1, long long d2, long long s1, long long s2, int b0, int b1, int b2,
+                     CUtensorMap* out);
+
 constexpr int kMaxDevices = 64;
 int current_device();     // index of the current CUDA device (0 when there is none)
 int sm_count();           // SM count of the current device
