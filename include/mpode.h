@@ -320,13 +320,14 @@ typedef struct {
     mpode_dtype low;              /* x, gate, y and their cotangents */
     int n_seq, n_steps, width;    /* sequences, longest sequence, channels */
     int coupled;
+    int zero_behind;              /* lengths: elements of y, dL_dx and dL_dgate behind a sequence's length: 0 = left as they are, else set to zero */
     long long in_seq_stride, in_step_stride;   /* x, gate, dL_dx, dL_dgate: element (s, i, c) at s * in_seq_stride + i * in_step_stride + c */
     long long out_seq_stride, out_step_stride; /* y, dL_dy; 0 = [n_seq][n_steps][width].  Rows must not overlap. */
 } mpode_recurrence_desc;
 
 /*
  * y0_dev: fp32 [n_seq][width] or NULL (zero).  lengths_dev: int [n_seq] or NULL (all n_steps); values are clamped to 0 .. n_steps.  Elements of x,
- * gate and y behind a sequence's length are neither read nor written.  yT_dev: NULL, or fp32 [n_seq][width], the state behind the last step (y0
+ * gate and y behind a sequence's length are not read, and y is not written there unless zero_behind.  yT_dev: NULL, or fp32 [n_seq][width], the state behind the last step (y0
  * where the length is 0); it may be y0_dev.  y_dev may be x_dev.  n_steps = 1 with yT_dev = y0_dev is the form for serving token by token.
  */
 mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
@@ -335,7 +336,7 @@ mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* c
 /*
  * Backward pass from the stored trajectory y_dev (Alg. 2's reading: derivatives are taken at the stored states, y_{-1} = y0 in float32).
  * dL_dy_dev: NULL (zero) or the cotangent of the stored y.  dL_dyT_dev: NULL (zero) or fp32, that of yT.  dL_dx_dev and dL_dgate_dev are written up to
- * each sequence's length and left alone behind it; dL_dy0_dev may be NULL.  dL_dx_dev may be dL_dy_dev where the strides agree, dL_dgate_dev may be
+ * each sequence's length (and set to zero behind it with zero_behind); dL_dy0_dev may be NULL.  dL_dx_dev may be dL_dy_dev where the strides agree, dL_dgate_dev may be
  * gate_dev, dL_dy0_dev may be dL_dyT_dev.  x_dev is not read when coupled == 0.
  * All cotangents carry the same power-of-two scale, whatever it is.
  */

@@ -65,7 +65,7 @@ class Stats(C.Structure):
 
 class RecurrenceDesc(C.Structure):
     _fields_ = [("low", C.c_int), ("n_seq", C.c_int), ("n_steps", C.c_int), ("width", C.c_int), ("coupled", C.c_int),
-                ("in_seq_stride", C.c_longlong), ("in_step_stride", C.c_longlong), ("out_seq_stride", C.c_longlong),
+                ("zero_behind", C.c_int), ("in_seq_stride", C.c_longlong), ("in_step_stride", C.c_longlong), ("out_seq_stride", C.c_longlong),
                 ("out_step_stride", C.c_longlong)]
 
 
@@ -466,8 +466,9 @@ def recurrence_forward(x, gate, y0=None, lengths=None, coupled: bool = True, y=N
     low, dtype = _low_of(x), x.dtype
     inner = _layout("x", x, shape, dtype)
     _same_layout("gate", gate, shape, dtype, inner)
-    if y is None:
-        y = torch.empty_like(x) if lengths is None else torch.zeros_like(x)       # (time-major inputs get a time-major trajectory)
+    new = y is None
+    if new:
+        y = torch.empty_like(x)                                                   # (time-major inputs get a time-major trajectory)
     outer = _layout("y", y, shape, dtype)
     states = (n, width)
     if yT is None:
@@ -476,7 +477,7 @@ def recurrence_forward(x, gate, y0=None, lengths=None, coupled: bool = True, y=N
         _expect("yT", yT, states, torch.float32)
     _expect("y0", y0, states, torch.float32)
     _expect("lengths", lengths, (n,), torch.int32)
-    _run(lib.mpode_recurrence_forward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, *inner, *outer), (x, gate, y0, lengths, y, yT),
+    _run(lib.mpode_recurrence_forward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, 1 if new and lengths is not None else 0, *inner, *outer), (x, gate, y0, lengths, y, yT),
          (_ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(yT)))
     return y, yT
 
@@ -492,17 +493,13 @@ def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, c
     inner, outer = _layout("x", x, shape, dtype), _layout("y", y, shape, dtype)
     _same_layout("gate", gate, shape, dtype, inner)
     _same_layout("dL_dy", dL_dy, shape, dtype, outer)
-    if dL_dx is None:
-        dL_dx = torch.empty_strided(shape, x.stride(), dtype=dtype, device=device)
-        if lengths is not None:
-            dL_dx.zero_()
+    new = dL_dx is None and dL_dgate is None
+    if new:
+        dL_dx, dL_dgate = (torch.empty_strided(shape, x.stride(), dtype=dtype, device=device) for _ in range(2))
+    elif dL_dx is None or dL_dgate is None:
+        _refuse("dL_dx and dL_dgate are given together or not at all")
     else:
         _same_layout("dL_dx", dL_dx, shape, dtype, inner)
-    if dL_dgate is None:
-        dL_dgate = torch.empty_strided(shape, x.stride(), dtype=dtype, device=device)
-        if lengths is not None:
-            dL_dgate.zero_()
-    else:
         _same_layout("dL_dgate", dL_dgate, shape, dtype, inner)
     states = (n, width)
     if dL_dy0 is None:
@@ -513,7 +510,7 @@ def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, c
     _expect("dL_dyT", dL_dyT, states, torch.float32)
     _expect("lengths", lengths, (n,), torch.int32)
     _expect("flag", flag, (1,), torch.int32)
-    _run(lib.mpode_recurrence_backward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, *inner, *outer),
+    _run(lib.mpode_recurrence_backward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, 1 if new and lengths is not None else 0, *inner, *outer),
          (x, gate, y, dL_dy, dL_dyT, y0, lengths, dL_dx, dL_dgate, dL_dy0, flag),
          (_ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(dL_dy), _ptr(dL_dyT), _ptr(dL_dx), _ptr(dL_dgate), _ptr(dL_dy0), _ptr(flag)))
     return dL_dx, dL_dgate, dL_dy0

@@ -37,36 +37,19 @@ struct RecArgs {
     unsigned* flag;
     long long in_seq, in_step, out_seq, out_step;
     int n_seq, n_steps, width;
+    int zero_behind;                   // what lies behind a sequence's length is set to zero
     int time_major;                    // STAGED: the maps' coordinates are (channel, sequence, step) instead of (channel, step, sequence)
 };
 // STAGED: tensor maps of gate and x (forward), of gate, dL/dy, y and x (backward)
 struct RecMaps { CUtensorMap m[4]; };
 
-// V channels of a row as one access: two (a 32-bit word, or 64 bits of float32), or one where widths or addresses are odd
+// Two channels of a row: a pair of 16-bit values in 32 bits, or of float32.  V = 2 throughout.
 template <typename T, int V> struct Word;
-template <> struct Word<float, 1> {
-    using type = float;
-    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = w; }
-    static __device__ __forceinline__ type put(const float (&f)[1]) { return f[0]; }
-    static __device__ __forceinline__ type negate(type w) { return -w; }
-};
 template <> struct Word<float, 2> {
     using type = float2;
     static __device__ __forceinline__ void get(type w, float (&f)[2]) { f[0] = w.x; f[1] = w.y; }
     static __device__ __forceinline__ type put(const float (&f)[2]) { return make_float2(f[0], f[1]); }
     static __device__ __forceinline__ type negate(type w) { return make_float2(-w.x, -w.y); }
-};
-template <> struct Word<__nv_bfloat16, 1> {
-    using type = __nv_bfloat16;
-    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = __bfloat162float(w); }
-    static __device__ __forceinline__ type put(const float (&f)[1]) { return __float2bfloat16_rn(f[0]); }
-    static __device__ __forceinline__ type negate(type w) { return __hneg(w); }
-};
-template <> struct Word<__half, 1> {
-    using type = __half;
-    static __device__ __forceinline__ void get(type w, float (&f)[1]) { f[0] = __half2float(w); }
-    static __device__ __forceinline__ type put(const float (&f)[1]) { return __float2half_rn(f[0]); }
-    static __device__ __forceinline__ type negate(type w) { return __hneg(w); }
 };
 template <typename T> struct Word<T, 2> {
     using type = uint32_t;
@@ -74,21 +57,9 @@ template <typename T> struct Word<T, 2> {
     static __device__ __forceinline__ type put(const float (&f)[2]) { return Pair<T>::put(f[0], f[1]); }
     static __device__ __forceinline__ type negate(type w) { return w ^ 0x80008000u; }
 };
-template <typename T, int V> __device__ __forceinline__ typename Word<T, V>::type word_of(float v) {
-    float f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = v;
-    return Word<T, V>::put(f);
-}
 template <typename T, int V> __device__ __forceinline__ void see(Largest<T>& m, const typename Word<T, V>::type& w) {
-    if constexpr (sizeof(T) == 2 && V == 2) m.see(w);
-    else if constexpr (sizeof(T) == 2) m.see((uint32_t)*reinterpret_cast<const uint16_t*>(&w));
-    else {
-        float f[V];
-        Word<T, V>::get(w, f);
-#pragma unroll
-        for (int v = 0; v < V; ++v) m.see(__float_as_uint(f[v]));
-    }
+    if constexpr (sizeof(T) == 2) m.see(w);
+    else { m.see(__float_as_uint(w.x)); m.see(__float_as_uint(w.y)); }
 }
 
 // a b + c, a + b and a b on all channels of a lane; two of them are one instruction
@@ -302,48 +273,78 @@ template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsig
     before.apply(start);
 }
 
-// Which channels and steps a thread works on.  Lanes behind the last channel do what the last one does, and write the same values to the same
+// How rows are read and written
+enum Access : int {
+    STAGED = 0,     // rows of multiples of 16 bytes from aligned pointers: bulk tensor copies to shared memory, neighbouring channels a lane
+    PAIRS = 1,      // even widths and strides, pointers aligned to two elements: neighbouring channels a lane, one access
+    SINGLES = 2     // anything: channels 32 apart a lane, an access each
+};
+// Which channels and steps a thread works on.  Channels behind the last one are the last one again (the last pair), and the same values go to the same
 // places: a condition at each store costs more than the rest of the second run (1320 cycles a round of 16 steps instead of 520).
-struct Place { int seq, tile, col, lane, len, rank; unsigned slot; };      // tile: the first channel of the warp
-template <int V> __device__ __forceinline__ Place place(const RecArgs& p, int blocks) {
-    const int tiles = (p.width + 32 * V - 1) / (32 * V), tile = blockIdx.x / blocks;
+struct Place { int seq, tile, lane, col[2], len, rank; unsigned slot; };      // tile: the first channel of the warp
+template <int ACCESS> __device__ __forceinline__ Place place(const RecArgs& p, int blocks) {
+    const int tiles = (p.width + 63) / 64, tile = blockIdx.x / blocks;
     Place q;
     q.rank = blockIdx.x - tile * blocks;
     q.seq = tile / tiles;
-    q.tile = (tile - q.seq * tiles) * 32 * V;
-    q.lane = min((int)threadIdx.x, (p.width - q.tile) / V - 1);
-    q.col = q.tile + q.lane * V;
+    q.tile = (tile - q.seq * tiles) * 64;
+    if (ACCESS == SINGLES) {
+        q.lane = threadIdx.x;
+        q.col[0] = min(q.tile + (int)threadIdx.x, p.width - 1);
+        q.col[1] = min(q.tile + (int)threadIdx.x + 32, p.width - 1);
+    } else {
+        q.lane = min((int)threadIdx.x, (p.width - q.tile) / 2 - 1);
+        q.col[0] = q.tile + 2 * q.lane;
+        q.col[1] = q.col[0] + 1;
+    }
     q.len = p.n_steps;
     if (p.lengths != nullptr) q.len = min(max(p.lengths[q.seq], 0), p.n_steps);
     q.slot = q.rank * blockDim.y + threadIdx.y;
     return q;
 }
+// a lane's two channels of the row at base + off; apart: bytes from one to the other (SINGLES)
+template <typename T, int ACCESS> __device__ __forceinline__ typename Word<T, 2>::type load_pair(const char* base, unsigned off, unsigned apart) {
+    using word = typename Word<T, 2>::type;
+    if constexpr (ACCESS != SINGLES) return *(const word*)(base + off);
+    else if constexpr (sizeof(T) == 4) return make_float2(*(const float*)(base + off), *(const float*)(base + off + apart));
+    else return (uint32_t)*(const uint16_t*)(base + off) | (uint32_t)*(const uint16_t*)(base + off + apart) << 16;
+}
+template <typename T, int ACCESS> __device__ __forceinline__ void store_pair(char* base, unsigned off, unsigned apart, typename Word<T, 2>::type w) {
+    using word = typename Word<T, 2>::type;
+    if constexpr (ACCESS != SINGLES) *(word*)(base + off) = w;
+    else if constexpr (sizeof(T) == 4) {
+        *(float*)(base + off) = w.x;
+        *(float*)(base + off + apart) = w.y;
+    } else {
+        *(uint16_t*)(base + off) = (uint16_t)w;
+        *(uint16_t*)(base + off + apart) = (uint16_t)(w >> 16);
+    }
+}
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
-// Where a warp finds its steps: a tile of N arrays, L steps of V channels a lane.
-//   STAGED: brought to shared memory by bulk tensor copies that run two rounds ahead (each warp its own two stages and barriers, so that no other warp has to
-//           be waited for), read from there as often as needed.  Rows of all arrays are multiples of 16 bytes from aligned pointers.  (Asynchronous
-//           copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
-//   else:   loaded into registers when the round starts.  For any alignment (V = 1), and for sequences of a round or two, where nothing runs ahead.
+// Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
+//   STAGED: brought to shared memory two rounds ahead (each warp its own two stages and barriers, so that no other warp has to be waited for), read from there
+//           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
+//   else:   loaded into registers when the round starts (a round ahead took more registers and more time).
 template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 constexpr int kStages = 2;
 template <typename T, int V, int L, int N> constexpr int kWarpBytes = kStages * N * L * kRowBytes<T, V>;
-template <typename T, int V, int L, int N, bool STAGED> struct Tile;
-template <typename T, int V, int L, int N> struct Tile<T, V, L, N, false> {
+template <typename T, int V, int L, int N, int ACCESS> struct Tile {
     using word = typename Word<T, V>::type;
     word w[N][L];
+    unsigned apart;
     // step i of array k lies at base + off + i * step bytes; steps lo .. hi - 1 exist
     __device__ __forceinline__ void load(int k, const char* base, unsigned off, unsigned step, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < L; ++i, off += step) {
-            w[k][i] = word_of<T, V>(0.f);
-            if (i >= lo && i < hi) w[k][i] = *(const word*)(base + off);
+            w[k][i] = word{};
+            if (i >= lo && i < hi) w[k][i] = load_pair<T, ACCESS>(base, off, apart);
         }
     }
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
 };
-template <typename T, int V, int L, int N> struct Tile<T, V, L, N, true> {
+template <typename T, int V, int L, int N> struct Tile<T, V, L, N, STAGED> {
     using word = typename Word<T, V>::type;
     static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow;
     unsigned at, lane, bar;
@@ -384,57 +385,60 @@ template <typename T, int V, int L, int N> struct Tile<T, V, L, N, true> {
     }
 };
 
-template <typename T, int V, bool COUPLED, int L, bool STAGED>
+template <typename T, int V, bool COUPLED, int L, int ACCESS>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
-    using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
     __shared__ Exchange<V> ex;
-    __shared__ unsigned long long arrived[STAGED ? kMaxWarps * kStages : 1];
-    const Place q = place<V>(p, blocks);
+    __shared__ unsigned long long arrived[ACCESS == STAGED ? kMaxWarps * kStages : 1];
+    const Place q = place<ACCESS>(p, blocks);
     const bool alone = blocks == 1 && blockDim.y == 1;
     if (!alone) exchange_begin<V>(ex, blocks);
-    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
+    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es;
-    const unsigned in_at = q.col * es + q.slot * L * in_step, out_at = q.col * es + q.slot * L * out_step;
+    const unsigned in_at = q.col[0] * es + q.slot * L * in_step, out_at = q.col[0] * es + q.slot * L * out_step;
     const char* x = (const char*)p.x + q.seq * p.in_seq * es;
     const char* g = (const char*)p.gate + q.seq * p.in_seq * es;
     char* out = (char*)p.out + q.seq * p.out_seq * es;
     const long long in_round = (long long)stride * in_step, out_round = (long long)stride * out_step;
-    const long long state = (long long)q.seq * p.width + q.col;
+    const long long states = (long long)q.seq * p.width;
     float carry[V];                                         // -y when coupled
     bool broken = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        carry[v] = p.y0 != nullptr ? p.y0[state + v] : 0.f;
+        carry[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
         if (COUPLED) carry[v] = -carry[v];
     }
-    Tile<T, V, L, 2, STAGED> tile;
+    Tile<T, V, L, 2, ACCESS> tile;
     // steps of this warp's tile that exist
     auto count = [&](unsigned base) {
         const unsigned t0 = base + q.slot * L;
         return t0 < (unsigned)q.len ? (int)min((unsigned)L, (unsigned)q.len - t0) : 0;
     };
     auto request = [&](unsigned base, int stage) {
-        if constexpr (STAGED)
+        if constexpr (ACCESS == STAGED)
             if (threadIdx.x == 0 && base < (unsigned)q.len) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
     };
-    if constexpr (STAGED) {
+    auto load = [&](unsigned base) {
+        if constexpr (ACCESS != STAGED) {
+            const int n = count(base);
+            tile.load(0, g, in_at, in_step, 0, n);
+            tile.load(1, x, in_at, in_step, 0, n);
+            x += in_round; g += in_round;
+        }
+    };
+    if constexpr (ACCESS == STAGED) {
         tile.bind(staged, arrived, q.lane);
         for (int k = 0; k < kStages; ++k) request(k * stride, k);
-    }
+    } else tile.apart = apart;
     if (blocks > 1) cluster_wait();
     unsigned round = 0;
     // full: every step of the round exists
     auto body = [&](auto full, unsigned base) {
         float nb[L][V], start[V];
         const int stage = round % kStages, n = count(base);
-        if constexpr (STAGED) tile.wait(stage, (round / kStages) & 1, broken);
-        else {
-            tile.load(0, g, in_at, in_step, 0, n);
-            tile.load(1, x, in_at, in_step, 0, n);
-            x += in_round; g += in_round;
-        }
+        if constexpr (ACCESS == STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+        else load(base);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             float f[V], none[V];
@@ -472,46 +476,48 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
             float xs[V];
             x_of(i, xs);
             step_forward<COUPLED, V>(start, nb[i], xs);
-            if (full.value || i < n) *(word*)(out + at) = COUPLED ? W::negate(W::put(start)) : W::put(start);
+            if (full.value || i < n) store_pair<T, ACCESS>(out, at, apart, COUPLED ? W::negate(W::put(start)) : W::put(start));
         }
         out += out_round;
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
+            for (int v = 0; v < V; ++v) carry[v] = ACCESS == STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
         }
-        if (STAGED) {
+        if (ACCESS == STAGED) {
             __syncwarp();                                   // all lanes have read this stage
             request(base + kStages * stride, stage);
         }
         ++round;
     };
     unsigned base = 0;
-    if (STAGED)
-        for (; base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), base);
+    for (; base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), base);
     for (; base < (unsigned)q.len; base += stride) body(Flag<false>(), base);
+    if (p.zero_behind)
+        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * blockDim.y)
+            store_pair<T, ACCESS>((char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es, 0, apart, typename W::type{});
     if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) p.last[state + v] = COUPLED ? -carry[v] : carry[v];
+        for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
     }
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written
 }
 
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
 // Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
-template <typename T, int V, bool COUPLED, int L, bool STAGED>
+template <typename T, int V, bool COUPLED, int L, int ACCESS>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
     using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
     __shared__ Exchange<V> ex;
-    __shared__ unsigned long long arrived[STAGED ? kMaxWarps * kStages : 1];
-    const Place q = place<V>(p, blocks);
+    __shared__ unsigned long long arrived[ACCESS == STAGED ? kMaxWarps * kStages : 1];
+    const Place q = place<ACCESS>(p, blocks);
     const bool alone = blocks == 1 && blockDim.y == 1;
     if (!alone) exchange_begin<V>(ex, blocks);
-    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T);
+    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
     // offsets count down from the last time of the round
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es, back = (stride - 1) - q.slot * L;
-    const unsigned in_at = q.col * es + back * in_step, out_at = q.col * es + back * out_step;
+    const unsigned in_at = q.col[0] * es + back * in_step, out_at = q.col[0] * es + back * out_step;
     const unsigned skipped = p.n_steps - q.len;             // steps at the start of the count that do not exist
     unsigned base = skipped / stride * stride;              // rounds that lie behind the sequence are passed over
     const long long in_round = (long long)stride * in_step, out_round = (long long)stride * out_step;
@@ -519,13 +525,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
     const long long first_out = q.seq * p.out_seq * es + ((long long)p.n_steps - stride - base) * out_step;
     const char *x = (const char*)p.x + first_in, *g = (const char*)p.gate + first_in, *y = (const char*)p.y + first_out - out_step, *dy = (const char*)p.dy + first_out;
     char *dx = (char*)p.out + first_in, *dg = (char*)p.out2 + first_in;
-    const long long state = (long long)q.seq * p.width + q.col;
+    const long long states = (long long)q.seq * p.width;
     float carry[V];
     bool broken = false;
     Largest<T> largest;
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr ? p.dyT[state + v] : 0.f;
-    Tile<T, V, L, COUPLED ? 4 : 3, STAGED> tile;
+    for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr ? p.dyT[states + q.col[v]] : 0.f;
+    Tile<T, V, L, COUPLED ? 4 : 3, ACCESS> tile;
     // the tile's steps lo .. hi - 1 exist
     auto range = [&](unsigned base, int& lo, int& hi) {
         const unsigned first = base + q.slot * L;
@@ -533,17 +539,29 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
         hi = first < (unsigned)p.n_steps ? (int)min((unsigned)L, p.n_steps - first) : 0;
     };
     auto request = [&](unsigned base, int stage) {
-        if constexpr (STAGED)
+        if constexpr (ACCESS == STAGED)
             if (threadIdx.x == 0 && base < (unsigned)p.n_steps) {
                 const int t0 = p.n_steps - (int)(base + q.slot * L) - L;                        // the tile's earliest time; its steps lie the other way round
                 tile.request(stage, maps, (COUPLED ? 13u : 5u) | (p.dy != nullptr ? 2u : 0u), q.tile, q.seq, p.time_major != 0, t0, t0 - 1);
             }
     };
-    if constexpr (STAGED) {
+    auto load = [&](unsigned base) {
+        if constexpr (ACCESS != STAGED) {
+            int lo, hi;
+            range(base, lo, hi);
+            const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;     // time 0 has no stored state in front of it
+            tile.load(0, g, in_at, 0u - in_step, lo, hi);
+            if (p.dy != nullptr) tile.load(1, dy, out_at, 0u - out_step, lo, hi);
+            tile.load(2, y, out_at, 0u - out_step, lo, before);
+            if constexpr (COUPLED) tile.load(3, x, in_at, 0u - in_step, lo, hi);
+            x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
+        }
+    };
+    if constexpr (ACCESS == STAGED) {
         tile.bind(staged, arrived, q.lane);
         for (int k = 0; k < kStages; ++k) request(base + k * stride, k);
-    }
-    auto get = [&](int stage, int k, int i) { return tile.get(stage, k, STAGED ? L - 1 - i : i); };
+    } else tile.apart = apart;
+    auto get = [&](int stage, int k, int i) { return tile.get(stage, k, ACCESS == STAGED ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
     unsigned round = 0;
     const bool no_dy = p.dy == nullptr;
@@ -553,15 +571,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
         int lo, hi;
         range(base, lo, hi);
         const int zero = (int)(p.n_steps - 1 - (base + q.slot * L));                            // index of time 0
-        if constexpr (STAGED) tile.wait(stage, (round / kStages) & 1, broken);
-        else {
-            const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;     // time 0 has no stored state in front of it
-            tile.load(0, g, in_at, 0u - in_step, lo, hi);
-            if (!no_dy) tile.load(1, dy, out_at, 0u - out_step, lo, hi);
-            tile.load(2, y, out_at, 0u - out_step, lo, before);
-            if constexpr (COUPLED) tile.load(3, x, in_at, 0u - in_step, lo, hi);
-            x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
-        }
+        if constexpr (ACCESS == STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+        else load(base);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             float f[V];
@@ -602,7 +613,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
             W::get(get(stage, 2, i), ys);
             if (!full.value && i == zero) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[state + v] : 0.f;
+                for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
             }
             Ops<V>::add(l, start, d);
             Ops<V>::fma(start, nb[i], l, l);
@@ -619,16 +630,16 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
             if (full.value || (i >= lo && i < hi)) {
                 const word wx = COUPLED ? W::negate(W::put(gx)) : W::put(l), wg = COUPLED ? W::put(gg) : W::negate(W::put(gg));
                 if (p.flag != nullptr) { see<T, V>(largest, wx); see<T, V>(largest, wg); }
-                *(word*)(dx + at) = wx;
-                *(word*)(dg + at) = wg;
+                store_pair<T, ACCESS>(dx, at, apart, wx);
+                store_pair<T, ACCESS>(dg, at, apart, wg);
             }
         }
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
+            for (int v = 0; v < V; ++v) carry[v] = ACCESS == STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
         }
         dx -= in_round; dg -= in_round;
-        if (STAGED) {
+        if (ACCESS == STAGED) {
             __syncwarp();
             request(base + kStages * stride, stage);
         }
@@ -636,14 +647,18 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
         ++round;
     };
     // (a full round does not hold time 0)
-    if (STAGED) {
-        if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>());
-        while (base + stride < (unsigned)p.n_steps) body(Flag<true>());
-    }
+    if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>());
+    while (base + stride < (unsigned)p.n_steps) body(Flag<true>());
     while (base < (unsigned)p.n_steps) body(Flag<false>());
+    if (p.zero_behind)
+        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * blockDim.y) {
+            const long long to = (q.seq * p.in_seq + i * p.in_step + q.col[0]) * es;
+            store_pair<T, ACCESS>((char*)p.out + to, 0, apart, typename W::type{});
+            store_pair<T, ACCESS>((char*)p.out2 + to, 0, apart, typename W::type{});
+        }
     if (p.last != nullptr && q.slot == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) p.last[state + v] = carry[v];
+        for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];
     }
     warp_flag_or(p.flag, largest.nonfinite());
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }
@@ -656,9 +671,9 @@ bool round_fits(const RecArgs& a, long long steps, int es) {
     const long long step = a.in_step > a.out_step ? a.in_step : a.out_step;
     return step < (1ll << 32) && (steps * step + a.width) * es < (1ll << 32);
 }
-Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int lanes_width, int steps_of_warp) {
+Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int steps_of_warp) {
     Shape s;
-    s.tiles = (long long)d.n_seq * ((d.width + lanes_width - 1) / lanes_width);
+    s.tiles = (long long)d.n_seq * ((d.width + 63) / 64);
     s.warps = s.blocks = 1;
     while (s.warps < kMaxWarps && (long long)s.warps * steps_of_warp < d.n_steps) s.warps *= 2;
     while (s.blocks < kMaxCluster && s.tiles * s.blocks < 148 && (long long)s.blocks * s.warps * steps_of_warp < d.n_steps) s.blocks *= 2;
@@ -690,9 +705,19 @@ cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), cons
     return cudaLaunchKernelEx(&cfg, kernel, a, maps, s.blocks);
 }
 
-template <typename T, int V> constexpr int kForwardSteps = sizeof(T) * V > 4 ? 8 : 16;
-template <typename T, int V> constexpr int kBackwardSteps = sizeof(T) * V > 4 ? 4 : 8;
+// steps of a warp in a round
+template <typename T> constexpr int kForwardSteps = sizeof(T) == 4 ? 8 : 16;
+template <typename T> constexpr int kBackwardSteps = sizeof(T) == 4 ? 4 : 8;
 
+// two channels an access need even widths and strides and rows aligned to two elements
+bool words_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
+    if (d.width & 1) return false;
+    if ((a.in_step | a.in_seq | a.out_step | a.out_seq) & 1) return false;
+    const void* const all[] = {a.x, a.gate, a.y, a.dy, a.out, a.out2};
+    for (const void* q : all)
+        if (misaligned(q, 2 * low_size(d.low))) return false;
+    return true;
+}
 // rows of multiples of 16 bytes from aligned pointers everywhere
 bool pieces_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
     const long long es = (long long)low_size(d.low);
@@ -702,42 +727,41 @@ bool pieces_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
         if (misaligned(q, 16)) return false;
     return true;
 }
+template <int A> struct Way { static constexpr int value = A; };
 // maps of [n_seq][n_steps][width] with boxes of L steps; the dimension with the larger stride comes last
-bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long long step, int channels, int steps, bool time_major, CUtensorMap* out) {
-    return time_major ? make_tensor_map(p, d.low, d.width, d.n_seq, d.n_steps, seq, step, channels, 1, steps, out)
-                      : make_tensor_map(p, d.low, d.width, d.n_steps, d.n_seq, step, seq, channels, steps, 1, out);
+bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long long step, int steps, bool time_major, CUtensorMap* out) {
+    return time_major ? make_tensor_map(p, d.low, d.width, d.n_seq, d.n_steps, seq, step, 64, 1, steps, out)
+                      : make_tensor_map(p, d.low, d.width, d.n_steps, d.n_seq, step, seq, 64, steps, 1, out);
 }
-template <typename T, int V, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, RecArgs a, cudaStream_t st) {
-    constexpr int L = BACKWARD ? kBackwardSteps<T, V> : kForwardSteps<T, V>;
-    const Shape s = shape_of(d, a, 32 * V, L);
+template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, RecArgs a, cudaStream_t st) {
+    constexpr int L = BACKWARD ? kBackwardSteps<T> : kForwardSteps<T>, N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
+    const Shape s = shape_of(d, a, L);
     RecMaps maps;
-    if constexpr (V == 2) {
-        if (d.n_steps > 2 * s.warps * s.blocks * L && pieces_fit(d, a)) {
-            constexpr int N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
-            a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;
-            // (all arrays take the coordinates in one order: where inputs and outputs differ in theirs, registers)
-            bool ok = a.time_major == (d.n_seq > 1 && a.out_seq < a.out_step);
-            const bool tm = a.time_major != 0;
-            ok = ok && map_of(a.gate, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[0]);
-            if constexpr (BACKWARD) {
-                if (ok && a.dy != nullptr) ok = map_of(a.dy, d, a.out_seq, a.out_step, 32 * V, L, tm, &maps.m[1]);
-                ok = ok && map_of(a.y, d, a.out_seq, a.out_step, 32 * V, L, tm, &maps.m[2]);
-                if (COUPLED) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[3]);
-                if (ok) return launch(recurrence_backward_kernel<T, V, COUPLED, L, true>, a, maps, s, s.warps * kWarpBytes<T, V, L, N>, st);
-            } else {
-                ok = ok && map_of(a.x, d, a.in_seq, a.in_step, 32 * V, L, tm, &maps.m[1]);
-                if (ok) return launch(recurrence_forward_kernel<T, V, COUPLED, L, true>, a, maps, s, s.warps * kWarpBytes<T, V, L, N>, st);
-            }
+    const auto go = [&](auto access) {
+        constexpr int A = access.value;
+        const size_t smem = A == STAGED ? s.warps * kWarpBytes<T, 2, L, N> : 0;
+        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, 2, COUPLED, L, A>, a, maps, s, smem, st);
+        else return launch(recurrence_forward_kernel<T, 2, COUPLED, L, A>, a, maps, s, smem, st);
+    };
+    if (d.n_steps > 2 * s.warps * s.blocks * L && pieces_fit(d, a)) {
+        a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;
+        const bool tm = a.time_major != 0;
+        // (all arrays take their coordinates in one order: where inputs and outputs differ in theirs, registers)
+        bool ok = tm == (d.n_seq > 1 && a.out_seq < a.out_step) && map_of(a.gate, d, a.in_seq, a.in_step, L, tm, &maps.m[0]);
+        if (!BACKWARD) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, L, tm, &maps.m[1]);
+        else {
+            if (a.dy != nullptr) ok = ok && map_of(a.dy, d, a.out_seq, a.out_step, L, tm, &maps.m[1]);
+            ok = ok && map_of(a.y, d, a.out_seq, a.out_step, L, tm, &maps.m[2]);
+            if (COUPLED) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, L, tm, &maps.m[3]);
         }
+        if (ok) return go(Way<STAGED>());
     }
-    if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, V, COUPLED, L, false>, a, maps, s, 0, st);
-    else return launch(recurrence_forward_kernel<T, V, COUPLED, L, false>, a, maps, s, 0, st);
+    return words_fit(d, a) ? go(Way<PAIRS>()) : go(Way<SINGLES>());
 }
-template <bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, bool two, cudaStream_t st) {
+template <bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, const RecArgs& a, cudaStream_t st) {
     return with_low(d.low, [&](auto t) {
         using T = decltype(t);
-        if (two) return d.coupled ? run<T, 2, true, BACKWARD>(d, a, st) : run<T, 2, false, BACKWARD>(d, a, st);
-        return d.coupled ? run<T, 1, true, BACKWARD>(d, a, st) : run<T, 1, false, BACKWARD>(d, a, st);
+        return d.coupled ? run<T, true, BACKWARD>(d, a, st) : run<T, false, BACKWARD>(d, a, st);
     });
 }
 
@@ -761,20 +785,11 @@ mpode_status check(const mpode_recurrence_desc* d, RecArgs& a) {
     if (S > 0 && N > 0 && ((a.in_seq <= N * a.in_step + lo - 1 && a.in_step <= S * a.in_seq + lo - 1) ||
                            (a.out_seq <= N * a.out_step + lo - 1 && a.out_step <= S * a.out_seq + lo - 1)))
         return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: the strides make rows overlap");
-    a.n_seq = d->n_seq; a.n_steps = d->n_steps; a.width = d->width;
+    a.n_seq = d->n_seq; a.n_steps = d->n_steps; a.width = d->width; a.zero_behind = d->zero_behind;
     if (d->n_steps <= 1) a.in_step = a.out_step = lo;
     if (!round_fits(a, 16, (int)low_size(d->low)))
         return operator_fail(MPODE_ERR_UNSUPPORTED, "recurrence: step strides %lld and %lld (16 steps have to lie within 4 GB)", a.in_step, a.out_step);
     return MPODE_OK;
-}
-// two channels an access need even widths and strides and rows aligned to two elements
-bool words_fit(const mpode_recurrence_desc& d, const RecArgs& a) {
-    if (d.width & 1) return false;
-    if ((a.in_step | a.in_seq | a.out_step | a.out_seq) & 1) return false;
-    const void* const all[] = {a.x, a.gate, a.y, a.dy, a.out, a.out2};
-    for (const void* q : all)
-        if (misaligned(q, 2 * low_size(d.low))) return false;
-    return true;
 }
 mpode_status check_pointers(const mpode_recurrence_desc& d, const RecArgs& a) {
     const void* const low[] = {a.x, a.gate, a.y, a.dy, a.out, a.out2};
@@ -821,7 +836,7 @@ mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* c
     if (desc->n_steps > 0 && (!x_dev || !gate_dev || !y_dev)) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_recurrence_forward: null pointer argument");
     const mpode_status off = check_pointers(*desc, a);
     if (off != MPODE_OK) return off;
-    return operator_launched(run<false>(*desc, a, words_fit(*desc, a), (cudaStream_t)cuda_stream), "mpode_recurrence_forward");
+    return operator_launched(run<false>(*desc, a, (cudaStream_t)cuda_stream), "mpode_recurrence_forward");
 }
 
 mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
@@ -837,7 +852,7 @@ mpode_status mpode_recurrence_backward(const mpode_recurrence_desc* desc, void* 
         return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_recurrence_backward: null pointer argument");
     const mpode_status off = check_pointers(*desc, a);
     if (off != MPODE_OK) return off;
-    return operator_launched(run<true>(*desc, a, words_fit(*desc, a), (cudaStream_t)cuda_stream), "mpode_recurrence_backward");
+    return operator_launched(run<true>(*desc, a, (cudaStream_t)cuda_stream), "mpode_recurrence_backward");
 }
 
 }  // extern "C"
