@@ -21,11 +21,20 @@ __device__ __forceinline__ void send(unsigned at, float f, float g, unsigned bar
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(f), "f"(g), "r"(bar) : "memory");
 }
 
-// Two barriers used in turn.  A set of places is written again two rounds later: a round is complete only when every sender of the cluster has sent, and each of them
-// sends behind its own reads of the round before.
-__device__ __forceinline__ void sets_begin(unsigned long long* bar) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&bar[0])) : "memory");
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&bar[1])) : "memory");
+// one lane of a converged warp, which the compiler knows to be one (behind lane == 0 a bulk copy's operands are moved in a loop over lanes)
+__device__ __forceinline__ bool elected() {
+    unsigned yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0u;
+}
+__device__ __forceinline__ void bar_init(unsigned long long* bar, unsigned count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_of(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// Barriers of sets of places that are used in turn, one thread of the block
+__device__ __forceinline__ void sets_begin(unsigned long long* bar, int sets) {
+    for (int i = 0; i < sets; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_of(&bar[i])) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
 // one thread a block and round: the bytes that will come

@@ -4,10 +4,11 @@
 // g = log(h lambda)) or y_i = a y_{i-1} + x_i.  Backward: l_i = dy_i + r_i, r_{i-1} = a_i l_i, from r behind the last step; coupled dx = b l,
 // dg = l (x - y_{i-1}) a b, else dx = l, dg = -l y_{i-1} a b.
 //
-// Every step is an affine map y -> A y + u.  A block holds 32 lanes of channels and W warps along the time axis; a warp's steps lie in its
-// registers.  First each warp composes its own steps, the blocks of a cluster exchange their products through distributed shared memory, and
-// then every warp runs its steps again from the state in front of them: the data is read once and written once, nothing is kept in device
-// memory and no block waits for another but at the cluster's barrier.
+// Every step is an affine map y -> A y + u.  A block holds 32 lanes of channels, two each, and some warps along the time axis; a warp's steps of a round
+// lie in its registers or its part of shared memory.  First each warp composes its own steps, then the warps' maps are exchanged, and every warp runs its
+// steps again from the state in front of them: the data is read once and written once, and nothing is kept in device memory.  Where a batch has too few
+// channels for the GPU, the blocks of a cluster share a sequence and exchange their maps through distributed shared memory; one more warp of each block does
+// that while the others are at the next round's first half.
 //
 // Precision: b is formed with a relative error (no cancellation for g << 0), and every decay is written y - b y in one rounding, so that memories of
 // a million steps (b = 1e-6) decay at the right rate, where a rounded a = 1 - b would not, and b = 1 forgets everything, exactly.  For the same reason a
@@ -16,6 +17,8 @@
 #include <stdio.h>
 
 #include <math.h>
+
+#include <atomic>
 
 #include <type_traits>
 
@@ -173,12 +176,23 @@ template <int V> struct Affine {
 
 constexpr int kMaxWarps = 8, kMaxCluster = 16;
 
-// Shared memory of the exchange: maps of the block's warps and of the cluster's blocks, two sets used in turn.  Places of warps and blocks
-// that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
+// Shared memory of the exchange inside a block or a cluster: maps of the block's warps and of the cluster's blocks, two sets in turn.  Places of warps and
+// blocks that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
+// A set is written again two rounds later: a block sends its map of round k + 1 when it has those of round k from all blocks, and each of them sends behind a
+// barrier of its warps, which have then read those of round k - 1.
 template <int V> struct __align__(16) Exchange {
     float warp[2][kMaxWarps][3][32 * V];
     float block[2][kMaxCluster][3][32 * V];
-    unsigned long long bar[2];                  // counts the bytes of a set's block maps
+    unsigned long long bytes[2];                // counts the bytes of a set's block maps
+};
+// The same with a warp that scans: also the states in front of the warps' steps, and barriers that count the warps' maps and the states.  A warp writes its
+// map of round k + 2 behind its second half of round k, for which the maps of round k had been read; states of round k + 2 are written when all maps of
+// it are there, behind the reads of round k's.
+template <int V> struct __align__(16) Scan {
+    float warp[2][kMaxWarps][3][32 * V];
+    float block[2][kMaxCluster][3][32 * V];
+    float start[2][kMaxWarps][32 * V];
+    unsigned long long maps[2], bytes[2], starts[2];
 };
 template <int V> __device__ __forceinline__ void lds(float (&f)[V], const float* p) {
     if constexpr (V == 2) {
@@ -201,29 +215,51 @@ template <int V> __device__ __forceinline__ void send_all(unsigned at, const flo
     else send(at, f[0], bar);
 }
 
-template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex, int blocks) {
+template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex, int warps, int blocks) {
     Affine<V> id;
 #pragma unroll
     for (int v = 0; v < V; ++v) { id.m[v] = id.u[v] = 0.f; id.k[v] = 1.f; }
     for (int set = 0; set < 2; ++set) {
-        for (int w = blockDim.y + threadIdx.y; w < kMaxWarps; w += blockDim.y) put<V>(ex.warp[set][w], id);
+        for (int w = warps + threadIdx.y; w < kMaxWarps; w += warps) put<V>(ex.warp[set][w], id);
         if (blocks > 1)
-            for (int r = blocks + threadIdx.y; r < kMaxCluster; r += blockDim.y) put<V>(ex.block[set][r], id);
+            for (int r = blocks + threadIdx.y; r < kMaxCluster; r += warps) put<V>(ex.block[set][r], id);
     }
     if (blocks == 1) return;
-    if (threadIdx.x == 0 && threadIdx.y == 0) sets_begin(ex.bar);
+    if (threadIdx.x == 0 && threadIdx.y == 0) sets_begin(ex.bytes, 2);
     cluster_arrive();                       // nobody writes into a block that has not started
 }
-
-// The state in front of this warp's steps, from the state in front of all of this round's steps (`carry`, replaced by the one behind them).
-// Called by all threads of the cluster in the same rounds.
-template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsigned round, const Map<V>& own, float (&carry)[V], float (&start)[V],
-                                                          int blocks, int rank, bool& broken) {
+// A round's exchange has two halves.  publish: this warp's map to the block, the block's map to every block of the cluster; returns the map of the steps of the
+// block that lie in front of this warp's.  collect: from the state in front of all of the round's steps (`carry`, replaced by the one behind them) the
+// state in front of this warp's.  Called by all threads of the cluster in the same order.
+template <int V> __device__ __forceinline__ void publish(Exchange<V>& ex, unsigned round, const Map<V>& own, Affine<V>& before, int blocks, int rank) {
     const int warp = threadIdx.y, set = round & 1;
     Affine<V> a;
     a.from(own);
-    put<V>(ex.warp[set][warp], a);
+    put<V>(ex.warp[round & 1][warp], a);
     __syncthreads();
+    if (blocks == 1) return;
+    const unsigned bar = smem_of(&ex.bytes[set]);
+    if (warp == 0 && threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
+    Map<V> all;
+#pragma unroll
+    for (int w = 0; w < kMaxWarps; ++w) {
+        if (w == warp) before.from(all);
+        fetch<V>(a, ex.warp[round & 1][w]);
+        a.follow(all);
+    }
+    a.from(all);
+    const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]);
+    for (int to = warp; to < blocks; to += (int)blockDim.y) {               // a warp to each block
+        const unsigned there = peer_of(at, to), count = peer_of(bar, to);
+        send_all<V>(there, a.m, count);
+        send_all<V>(there + 32 * V * 4, a.k, count);
+        send_all<V>(there + 64 * V * 4, a.u, count);
+    }
+}
+template <int V> __device__ __forceinline__ void collect(Exchange<V>& ex, unsigned round, const Affine<V>& before, float (&carry)[V], float (&start)[V],
+                                                                   int blocks, int rank, bool& broken) {
+    const int warp = threadIdx.y, set = round & 1;
+    Affine<V> a;
     if (blocks == 1) {
 #pragma unroll
         for (int w = 0; w < kMaxWarps; ++w) {
@@ -231,30 +267,12 @@ template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsig
 #pragma unroll
                 for (int v = 0; v < V; ++v) start[v] = carry[v];
             }
-            fetch<V>(a, ex.warp[set][w]);
+            fetch<V>(a, ex.warp[round & 1][w]);
             a.apply(carry);
         }
         return;
     }
-    const unsigned bar = smem_of(&ex.bar[set]);
-    if (warp == 0 && threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
-    Map<V> all;
-    Affine<V> before;
-#pragma unroll
-    for (int w = 0; w < kMaxWarps; ++w) {
-        if (w == warp) before.from(all);
-        fetch<V>(a, ex.warp[set][w]);
-        a.follow(all);
-    }
-    a.from(all);
-    const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]);
-    for (int to = warp; to < blocks; to += (int)blockDim.y) {               // this block's map to every block, a warp to each
-        const unsigned there = peer_of(at, to), count = peer_of(bar, to);
-        send_all<V>(there, a.m, count);
-        send_all<V>(there + 32 * V * 4, a.k, count);
-        send_all<V>(there + 64 * V * 4, a.u, count);
-    }
-    wait_set(bar, (round >> 1) & 1, broken);
+    wait_set(smem_of(&ex.bytes[set]), (round >> 1) & 1, broken);
     if (broken) {
 #pragma unroll
         for (int v = 0; v < V; ++v) carry[v] = __int_as_float(0x7fffffff);
@@ -273,16 +291,105 @@ template <int V> __device__ __forceinline__ void exchange(Exchange<V>& ex, unsig
     before.apply(start);
 }
 
+template <int V> __device__ __forceinline__ void exchange_begin(Scan<V>& ex, int warps, int) {
+    if (threadIdx.x == 0 && threadIdx.y == 0) {
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&ex.maps[i], warps);
+            bar_init(&ex.starts[i], 1);
+        }
+        sets_begin(ex.bytes, 2);
+    }
+    __syncthreads();
+    cluster_arrive();
+}
+// a warp's map of a round, and the state in front of its steps
+template <int V> __device__ __forceinline__ void publish(Scan<V>& ex, unsigned round, const Map<V>& own) {
+    const int set = round & 1;
+    Affine<V> a;
+    a.from(own);
+    put<V>(ex.warp[set][threadIdx.y], a);
+    __syncwarp();
+    if (threadIdx.x == 0) bar_arrive(smem_of(&ex.maps[set]));
+}
+template <int V> __device__ __forceinline__ void collect(Scan<V>& ex, unsigned round, float (&start)[V], bool& broken) {
+    const int set = round & 1;
+    wait_set(smem_of(&ex.starts[set]), (round >> 1) & 1, broken);
+    lds<V>(start, &ex.start[set][threadIdx.y][threadIdx.x * V]);
+    if (broken) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) start[v] = __int_as_float(0x7fffffff);
+    }
+}
+// The warp between them: `carry` is the state in front of the first round, and then the one behind the last
+template <int V> __device__ __forceinline__ void scan(Scan<V>& ex, unsigned base, unsigned stride, unsigned end, float (&carry)[V], int warps, int blocks, int rank) {
+    bool broken = false;
+    for (unsigned round = 0; base < end; base += stride, ++round) {
+        const int set = round & 1;
+        const unsigned parity = (round >> 1) & 1;
+        Affine<V> a;
+        wait_set(smem_of(&ex.maps[set]), parity, broken);
+        float state[V];
+        if (blocks > 1) {
+            Map<V> all;
+#pragma unroll 4
+            for (int w = 0; w < warps; ++w) {
+                fetch<V>(a, ex.warp[set][w]);
+                a.follow(all);
+            }
+            a.from(all);
+            const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]), bar = smem_of(&ex.bytes[set]);
+            if (threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
+            for (int to = 0; to < blocks; ++to) {
+                const unsigned there = peer_of(at, to), count = peer_of(bar, to);
+                send_all<V>(there, a.m, count);
+                send_all<V>(there + 32 * V * 4, a.k, count);
+                send_all<V>(there + 64 * V * 4, a.u, count);
+            }
+            wait_set(bar, parity, broken);
+#pragma unroll 4
+            for (int r = 0; r < blocks; ++r) {
+                if (r == rank) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) state[v] = carry[v];
+                }
+                fetch<V>(a, ex.block[set][r]);
+                a.apply(carry);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) state[v] = carry[v];
+        }
+        if (broken) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) state[v] = carry[v] = __int_as_float(0x7fffffff);
+        }
+#pragma unroll 4
+        for (int w = 0; w < warps; ++w) {
+            sts<V>(&ex.start[set][w][threadIdx.x * V], state);
+            fetch<V>(a, ex.warp[set][w]);
+            a.apply(state);
+        }
+        if (blocks == 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) carry[v] = state[v];
+        }
+        __syncwarp();
+        if (threadIdx.x == 0) bar_arrive(smem_of(&ex.starts[set]));
+    }
+}
+
 // How rows are read and written
 enum Access : int {
     STAGED = 0,     // rows of multiples of 16 bytes from aligned pointers: bulk tensor copies to shared memory, neighbouring channels a lane
     PAIRS = 1,      // even widths and strides, pointers aligned to two elements: neighbouring channels a lane, one access
-    SINGLES = 2     // anything: channels 32 apart a lane, an access each
+    SINGLES = 2,    // anything: channels 32 apart a lane, an access each
+    PIPED = 3       // STAGED, in clusters: the next round's maps are on their way while this round's are waited for
 };
+__host__ __device__ constexpr bool staged_rows(int access) { return access == STAGED || access == PIPED; }
 // Which channels and steps a thread works on.  Channels behind the last one are the last one again (the last pair), and the same values go to the same
 // places: a condition at each store costs more than the rest of the second run (1320 cycles a round of 16 steps instead of 520).
 struct Place { int seq, tile, lane, col[2], len, rank; unsigned slot; };      // tile: the first channel of the warp
-template <int ACCESS> __device__ __forceinline__ Place place(const RecArgs& p, int blocks) {
+template <int ACCESS> __device__ __forceinline__ Place place(const RecArgs& p, int blocks, int warps) {
     const int tiles = (p.width + 63) / 64, tile = blockIdx.x / blocks;
     Place q;
     q.rank = blockIdx.x - tile * blocks;
@@ -299,7 +406,7 @@ template <int ACCESS> __device__ __forceinline__ Place place(const RecArgs& p, i
     }
     q.len = p.n_steps;
     if (p.lengths != nullptr) q.len = min(max(p.lengths[q.seq], 0), p.n_steps);
-    q.slot = q.rank * blockDim.y + threadIdx.y;
+    q.slot = q.rank * warps + threadIdx.y;
     return q;
 }
 // a lane's two channels of the row at base + off; apart: bytes from one to the other (SINGLES)
@@ -322,15 +429,41 @@ template <typename T, int ACCESS> __device__ __forceinline__ void store_pair(cha
 }
 
 template <bool B> struct Flag { static constexpr bool value = B; };
+// The rounds from `base` to `end`: both halves of each in turn, or the first half of the next one in front of the second half of this one
+template <bool PIPED_ROUNDS, typename Turn, typename First, typename Second>
+__device__ __forceinline__ void rounds(unsigned base, unsigned stride, unsigned end, First& first, Second& second) {
+    unsigned round = 0;
+    if constexpr (!PIPED_ROUNDS) {
+        Turn a;
+        for (; base < end; base += stride) {
+            first(a, base, round++);
+            second(a);
+        }
+    } else {
+        if (base >= end) return;
+        Turn a, b;
+        first(a, base, round++);
+        while (true) {
+            base += stride;
+            if (base >= end) { second(a); return; }
+            first(b, base, round++);
+            second(a);
+            base += stride;
+            if (base >= end) { second(b); return; }
+            first(a, base, round++);
+            second(b);
+        }
+    }
+}
 
 // Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
-//   STAGED: brought to shared memory two rounds ahead (each warp its own two stages and barriers, so that no other warp has to be waited for), read from there
+//   STAGED, PIPED: brought to shared memory two rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
 //           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
 //   else:   loaded into registers when the round starts (a round ahead took more registers and more time).
 template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
-constexpr int kStages = 2;
-template <typename T, int V, int L, int N> constexpr int kWarpBytes = kStages * N * L * kRowBytes<T, V>;
-template <typename T, int V, int L, int N, int ACCESS> struct Tile {
+__host__ __device__ constexpr int stages(int access) { return access == PIPED ? 3 : access == STAGED ? 2 : 0; }
+template <typename T, int V, int L, int N, int ACCESS> constexpr int kWarpBytes = stages(ACCESS) * N * L * kRowBytes<T, V>;
+template <typename T, int V, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS)> struct Tile {
     using word = typename Word<T, V>::type;
     word w[N][L];
     unsigned apart;
@@ -344,16 +477,16 @@ template <typename T, int V, int L, int N, int ACCESS> struct Tile {
     }
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
 };
-template <typename T, int V, int L, int N> struct Tile<T, V, L, N, STAGED> {
+template <typename T, int V, int L, int N, int ACCESS> struct Tile<T, V, L, N, ACCESS, true> {
     using word = typename Word<T, V>::type;
-    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow;
+    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow, kStages = stages(ACCESS);
     unsigned at, lane, bar;
     __device__ __forceinline__ void bind(char* smem, unsigned long long* bars, int l) {
-        at = smem_of(smem) + threadIdx.y * kWarpBytes<T, V, L, N>;
+        at = smem_of(smem) + threadIdx.y * kWarpBytes<T, V, L, N, ACCESS>;
         bar = smem_of(bars) + threadIdx.y * (kStages * 8);
         lane = at + l * (unsigned)sizeof(word);
         if (threadIdx.x == 0) {
-            sets_begin(bars + threadIdx.y * kStages);
+            sets_begin(bars + threadIdx.y * kStages, kStages);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
@@ -386,15 +519,20 @@ template <typename T, int V, int L, int N> struct Tile<T, V, L, N, STAGED> {
 };
 
 template <typename T, int V, bool COUPLED, int L, int ACCESS>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
+__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
+    constexpr int kArrays = 2;
     extern __shared__ __align__(128) char staged[];
-    __shared__ Exchange<V> ex;
-    __shared__ unsigned long long arrived[ACCESS == STAGED ? kMaxWarps * kStages : 1];
-    const Place q = place<ACCESS>(p, blocks);
-    const bool alone = blocks == 1 && blockDim.y == 1;
-    if (!alone) exchange_begin<V>(ex, blocks);
-    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
+    constexpr int kStages = stages(ACCESS);
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kStages : 1];
+    constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
+    const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
+    const bool alone = !kScan && blocks == 1 && warps == 1;
+    using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * kWarpBytes<T, V, L, kArrays, ACCESS>);
+    const Place q = place<ACCESS>(p, blocks, warps);
+    if (!alone) exchange_begin(ex, warps, blocks);
+    const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es;
     const unsigned in_at = q.col[0] * es + q.slot * L * in_step, out_at = q.col[0] * es + q.slot * L * out_step;
     const char* x = (const char*)p.x + q.seq * p.in_seq * es;
@@ -409,93 +547,119 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
         carry[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
         if (COUPLED) carry[v] = -carry[v];
     }
-    Tile<T, V, L, 2, ACCESS> tile;
+    if constexpr (kScan)
+    if ((int)threadIdx.y == warps) {
+        cluster_wait();
+        scan(ex, 0u, stride, (unsigned)q.len, carry, warps, blocks, q.rank);
+        if (p.last != nullptr && q.rank == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
+        }
+        cluster_arrive();
+        cluster_wait();
+        return;
+    }
+    Tile<T, V, L, kArrays, ACCESS> tile;
     // steps of this warp's tile that exist
     auto count = [&](unsigned base) {
         const unsigned t0 = base + q.slot * L;
         return t0 < (unsigned)q.len ? (int)min((unsigned)L, (unsigned)q.len - t0) : 0;
     };
     auto request = [&](unsigned base, int stage) {
-        if constexpr (ACCESS == STAGED)
-            if (threadIdx.x == 0 && base < (unsigned)q.len) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
+        if constexpr (staged_rows(ACCESS))
+            if (base < (unsigned)q.len && elected()) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
     };
     auto load = [&](unsigned base) {
-        if constexpr (ACCESS != STAGED) {
+        if constexpr (!staged_rows(ACCESS)) {
             const int n = count(base);
             tile.load(0, g, in_at, in_step, 0, n);
             tile.load(1, x, in_at, in_step, 0, n);
             x += in_round; g += in_round;
         }
     };
-    if constexpr (ACCESS == STAGED) {
+    if constexpr (staged_rows(ACCESS)) {
         tile.bind(staged, arrived, q.lane);
         for (int k = 0; k < kStages; ++k) request(k * stride, k);
     } else tile.apart = apart;
     if (blocks > 1) cluster_wait();
-    unsigned round = 0;
-    // full: every step of the round exists
-    auto body = [&](auto full, unsigned base) {
-        float nb[L][V], start[V];
-        const int stage = round % kStages, n = count(base);
-        if constexpr (ACCESS == STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+    // A round's two halves: gates and the map of this warp's steps, published; then the steps again from the state in front of them
+    struct Turn { float nb[L][V]; Affine<V> before; unsigned base, round; };
+    auto first = [&](Turn& r, unsigned base, unsigned round) {
+        r.base = base;
+        r.round = round;
+        const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0, n = count(base);
+        if constexpr (staged_rows(ACCESS)) tile.wait(stage, (round / kStages) & 1, broken);
         else load(base);
+        auto run = [&](auto full) {
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            float f[V], none[V];
-            W::get(tile.get(stage, 0, i), f);
-            negated_gate<T, V, false>(f, nb[i], none);
-            if (!full.value && i >= n) {                    // a step that does not exist keeps the state
+            for (int i = 0; i < L; ++i) {
+                float f[V], none[V];
+                W::get(tile.get(stage, 0, i), f);
+                negated_gate<T, V, false>(f, r.nb[i], none);
+                if (!full.value && i >= n) {                // a step that does not exist keeps the state
 #pragma unroll
-                for (int v = 0; v < V; ++v) nb[i][v] = 0.f;
+                    for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
+                }
             }
-        }
-        auto x_of = [&](int i, float (&xs)[V]) {
-            W::get(tile.get(stage, 1, i), xs);
-            if (!full.value && i >= n) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) xs[v] = 0.f;
-            }
-        };
-        if (!alone) {
+            if (alone) return;
             Map<V> own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float xs[V];
-                x_of(i, xs);
-                own.decay(nb[i]);
-                step_forward<COUPLED, V>(own.u, nb[i], xs);
+                W::get(tile.get(stage, 1, i), xs);
+                if (!full.value && i >= n) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) xs[v] = 0.f;
+                }
+                own.decay(r.nb[i]);
+                step_forward<COUPLED, V>(own.u, r.nb[i], xs);
             }
-            exchange<V>(ex, round, own, carry, start, blocks, q.rank, broken);
-        } else {
+            if constexpr (kScan) publish(ex, round, own);
+            else publish(ex, round, own, r.before, blocks, q.rank);
+        };
+        if (base + stride <= (unsigned)q.len) run(Flag<true>());
+        else run(Flag<false>());
+    };
+    auto second = [&](const Turn& r) {
+        float start[V];
+        const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0, n = count(r.base);
+        if constexpr (kScan) collect(ex, r.round, start, broken);
+        else if (!alone) collect(ex, r.round, r.before, carry, start, blocks, q.rank, broken);
+        else {
 #pragma unroll
             for (int v = 0; v < V; ++v) start[v] = carry[v];
         }
-        unsigned at = out_at;
+        auto run = [&](auto full) {
+            unsigned at = out_at;
 #pragma unroll
-        for (int i = 0; i < L; ++i, at += out_step) {
-            float xs[V];
-            x_of(i, xs);
-            step_forward<COUPLED, V>(start, nb[i], xs);
-            if (full.value || i < n) store_pair<T, ACCESS>(out, at, apart, COUPLED ? W::negate(W::put(start)) : W::put(start));
-        }
+            for (int i = 0; i < L; ++i, at += out_step) {
+                float xs[V];
+                W::get(tile.get(stage, 1, i), xs);
+                if (!full.value && i >= n) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) xs[v] = 0.f;
+                }
+                step_forward<COUPLED, V>(start, r.nb[i], xs);
+                if (full.value || i < n) store_pair<T, ACCESS>(out, at, apart, COUPLED ? W::negate(W::put(start)) : W::put(start));
+            }
+        };
+        if (r.base + stride <= (unsigned)q.len) run(Flag<true>());
+        else run(Flag<false>());
         out += out_round;
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = ACCESS == STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
+            for (int v = 0; v < V; ++v) carry[v] = staged_rows(ACCESS) && broken ? __int_as_float(0x7fffffff) : start[v];
         }
-        if (ACCESS == STAGED) {
+        if constexpr (staged_rows(ACCESS)) {
             __syncwarp();                                   // all lanes have read this stage
-            request(base + kStages * stride, stage);
+            request(r.base + kStages * stride, stage);
         }
-        ++round;
     };
-    unsigned base = 0;
-    for (; base + stride <= (unsigned)q.len; base += stride) body(Flag<true>(), base);
-    for (; base < (unsigned)q.len; base += stride) body(Flag<false>(), base);
+    rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, first, second);
     if (p.zero_behind)
-        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * blockDim.y)
+        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps)
             store_pair<T, ACCESS>((char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es, 0, apart, typename W::type{});
-    if (p.last != nullptr && q.slot == 0) {
+    if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
     }
@@ -505,16 +669,21 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_forward_kernel(c
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
 // Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
 template <typename T, int V, bool COUPLED, int L, int ACCESS>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
+__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T, V>;
+    constexpr int kArrays = COUPLED ? 4 : 3;
     using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
-    __shared__ Exchange<V> ex;
-    __shared__ unsigned long long arrived[ACCESS == STAGED ? kMaxWarps * kStages : 1];
-    const Place q = place<ACCESS>(p, blocks);
-    const bool alone = blocks == 1 && blockDim.y == 1;
-    if (!alone) exchange_begin<V>(ex, blocks);
-    const unsigned stride = blocks * blockDim.y * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
+    constexpr int kStages = stages(ACCESS);
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kStages : 1];
+    constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
+    const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
+    const bool alone = !kScan && blocks == 1 && warps == 1;
+    using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * kWarpBytes<T, V, L, kArrays, ACCESS>);
+    const Place q = place<ACCESS>(p, blocks, warps);
+    if (!alone) exchange_begin(ex, warps, blocks);
+    const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
     // offsets count down from the last time of the round
     const unsigned in_step = (unsigned)p.in_step * es, out_step = (unsigned)p.out_step * es, back = (stride - 1) - q.slot * L;
     const unsigned in_at = q.col[0] * es + back * in_step, out_at = q.col[0] * es + back * out_step;
@@ -531,7 +700,19 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
     Largest<T> largest;
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = p.dyT != nullptr ? p.dyT[states + q.col[v]] : 0.f;
-    Tile<T, V, L, COUPLED ? 4 : 3, ACCESS> tile;
+    if constexpr (kScan)
+    if ((int)threadIdx.y == warps) {
+        cluster_wait();
+        scan(ex, base, stride, (unsigned)p.n_steps, carry, warps, blocks, q.rank);
+        if (p.last != nullptr && q.rank == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];
+        }
+        cluster_arrive();
+        cluster_wait();
+        return;
+    }
+    Tile<T, V, L, kArrays, ACCESS> tile;
     // the tile's steps lo .. hi - 1 exist
     auto range = [&](unsigned base, int& lo, int& hi) {
         const unsigned first = base + q.slot * L;
@@ -539,14 +720,14 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
         hi = first < (unsigned)p.n_steps ? (int)min((unsigned)L, p.n_steps - first) : 0;
     };
     auto request = [&](unsigned base, int stage) {
-        if constexpr (ACCESS == STAGED)
-            if (threadIdx.x == 0 && base < (unsigned)p.n_steps) {
+        if constexpr (staged_rows(ACCESS))
+            if (base < (unsigned)p.n_steps && elected()) {
                 const int t0 = p.n_steps - (int)(base + q.slot * L) - L;                        // the tile's earliest time; its steps lie the other way round
                 tile.request(stage, maps, (COUPLED ? 13u : 5u) | (p.dy != nullptr ? 2u : 0u), q.tile, q.seq, p.time_major != 0, t0, t0 - 1);
             }
     };
     auto load = [&](unsigned base) {
-        if constexpr (ACCESS != STAGED) {
+        if constexpr (!staged_rows(ACCESS)) {
             int lo, hi;
             range(base, lo, hi);
             const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;     // time 0 has no stored state in front of it
@@ -557,106 +738,122 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 2) recurrence_backward_kernel(
             x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
         }
     };
-    if constexpr (ACCESS == STAGED) {
+    if constexpr (staged_rows(ACCESS)) {
         tile.bind(staged, arrived, q.lane);
         for (int k = 0; k < kStages; ++k) request(base + k * stride, k);
     } else tile.apart = apart;
-    auto get = [&](int stage, int k, int i) { return tile.get(stage, k, ACCESS == STAGED ? L - 1 - i : i); };
+    auto get = [&](int stage, int k, int i) { return tile.get(stage, k, staged_rows(ACCESS) ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
-    unsigned round = 0;
     const bool no_dy = p.dy == nullptr;
-    auto body = [&](auto full) {
-        float nb[L][V], slope[L][V], start[V];
-        const int stage = round % kStages;
+    struct Turn { float nb[L][V], slope[L][V]; Affine<V> before; unsigned base, round; };
+    // every step of the round exists, and none is time 0
+    auto whole = [&](unsigned base) { return base >= skipped && base + stride < (unsigned)p.n_steps; };
+    auto first = [&](Turn& r, unsigned base, unsigned round) {
+        r.base = base;
+        r.round = round;
+        const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0;
         int lo, hi;
         range(base, lo, hi);
-        const int zero = (int)(p.n_steps - 1 - (base + q.slot * L));                            // index of time 0
-        if constexpr (ACCESS == STAGED) tile.wait(stage, (round / kStages) & 1, broken);
+        if constexpr (staged_rows(ACCESS)) tile.wait(stage, (round / kStages) & 1, broken);
         else load(base);
+        auto run = [&](auto full) {
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-            float f[V];
-            W::get(get(stage, 0, i), f);
-            negated_gate<T, V, true>(f, nb[i], slope[i]);
-            if (!full.value && (i < lo || i >= hi)) {                                           // a step that does not exist keeps the adjoint
+            for (int i = 0; i < L; ++i) {
+                float f[V];
+                W::get(get(stage, 0, i), f);
+                negated_gate<T, V, true>(f, r.nb[i], r.slope[i]);
+                if (!full.value && (i < lo || i >= hi)) {                                       // a step that does not exist keeps the adjoint
 #pragma unroll
-                for (int v = 0; v < V; ++v) nb[i][v] = 0.f;
+                    for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
+                }
             }
-        }
-        auto dy_of = [&](int i, float (&d)[V]) {
-            W::get(get(stage, 1, i), d);
-            if (no_dy || (!full.value && (i < lo || i >= hi))) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) d[v] = 0.f;
-            }
-        };
-        if (!alone) {
+            if (alone) return;
             Map<V> own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float d[V], l[V];
-                dy_of(i, d);
-                own.decay(nb[i]);
+                W::get(get(stage, 1, i), d);
+                if (no_dy || (!full.value && (i < lo || i >= hi))) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) d[v] = 0.f;
+                }
+                own.decay(r.nb[i]);
                 Ops<V>::add(l, own.u, d);
-                Ops<V>::fma(own.u, nb[i], l, l);
+                Ops<V>::fma(own.u, r.nb[i], l, l);
             }
-            exchange<V>(ex, round, own, carry, start, blocks, q.rank, broken);
-        } else {
+            if constexpr (kScan) publish(ex, round, own);
+            else publish(ex, round, own, r.before, blocks, q.rank);
+        };
+        if (whole(base)) run(Flag<true>());
+        else run(Flag<false>());
+    };
+    auto second = [&](const Turn& r) {
+        float start[V];
+        const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0;
+        int lo, hi;
+        range(r.base, lo, hi);
+        const int zero = (int)(p.n_steps - 1 - (r.base + q.slot * L));                          // index of time 0
+        if constexpr (kScan) collect(ex, r.round, start, broken);
+        else if (!alone) collect(ex, r.round, r.before, carry, start, blocks, q.rank, broken);
+        else {
 #pragma unroll
             for (int v = 0; v < V; ++v) start[v] = carry[v];
         }
-        unsigned at = in_at;
+        auto run = [&](auto full) {
+            unsigned at = in_at;
 #pragma unroll
-        for (int i = 0; i < L; ++i, at -= in_step) {
-            float ys[V], d[V], l[V], gx[V], gg[V];
-            dy_of(i, d);
-            W::get(get(stage, 2, i), ys);
-            if (!full.value && i == zero) {
+            for (int i = 0; i < L; ++i, at -= in_step) {
+                float ys[V], d[V], l[V], gx[V], gg[V];
+                W::get(get(stage, 1, i), d);
+                if (no_dy || (!full.value && (i < lo || i >= hi))) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
-            }
-            Ops<V>::add(l, start, d);
-            Ops<V>::fma(start, nb[i], l, l);
-            Ops<V>::mul(gg, slope[i], l);
-            if constexpr (COUPLED) {
-                float xs[V], minus[V];
-                W::get(get(stage, 3, i), xs);
-                Ops<V>::mul(gx, nb[i], l);
+                    for (int v = 0; v < V; ++v) d[v] = 0.f;
+                }
+                W::get(get(stage, 2, i), ys);
+                if (!full.value && i == zero) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) minus[v] = -1.f;
-                Ops<V>::fma(ys, ys, minus, xs);
+                    for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
+                }
+                Ops<V>::add(l, start, d);
+                Ops<V>::fma(start, r.nb[i], l, l);
+                Ops<V>::mul(gg, r.slope[i], l);
+                if constexpr (COUPLED) {
+                    float xs[V], minus[V];
+                    W::get(get(stage, 3, i), xs);
+                    Ops<V>::mul(gx, r.nb[i], l);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) minus[v] = -1.f;
+                    Ops<V>::fma(ys, ys, minus, xs);
+                }
+                Ops<V>::mul(gg, gg, ys);
+                if (full.value || (i >= lo && i < hi)) {
+                    const word wx = COUPLED ? W::negate(W::put(gx)) : W::put(l), wg = COUPLED ? W::put(gg) : W::negate(W::put(gg));
+                    if (p.flag != nullptr) { see<T, V>(largest, wx); see<T, V>(largest, wg); }
+                    store_pair<T, ACCESS>(dx, at, apart, wx);
+                    store_pair<T, ACCESS>(dg, at, apart, wg);
+                }
             }
-            Ops<V>::mul(gg, gg, ys);
-            if (full.value || (i >= lo && i < hi)) {
-                const word wx = COUPLED ? W::negate(W::put(gx)) : W::put(l), wg = COUPLED ? W::put(gg) : W::negate(W::put(gg));
-                if (p.flag != nullptr) { see<T, V>(largest, wx); see<T, V>(largest, wg); }
-                store_pair<T, ACCESS>(dx, at, apart, wx);
-                store_pair<T, ACCESS>(dg, at, apart, wg);
-            }
-        }
+        };
+        if (whole(r.base)) run(Flag<true>());
+        else run(Flag<false>());
         if (alone) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = ACCESS == STAGED && broken ? __int_as_float(0x7fffffff) : start[v];
+            for (int v = 0; v < V; ++v) carry[v] = staged_rows(ACCESS) && broken ? __int_as_float(0x7fffffff) : start[v];
         }
         dx -= in_round; dg -= in_round;
-        if (ACCESS == STAGED) {
+        if constexpr (staged_rows(ACCESS)) {
             __syncwarp();
-            request(base + kStages * stride, stage);
+            request(r.base + kStages * stride, stage);
         }
-        base += stride;
-        ++round;
     };
-    // (a full round does not hold time 0)
-    if (base < skipped && base < (unsigned)p.n_steps) body(Flag<false>());
-    while (base + stride < (unsigned)p.n_steps) body(Flag<true>());
-    while (base < (unsigned)p.n_steps) body(Flag<false>());
+    rounds<ACCESS == PIPED, Turn>(base, stride, (unsigned)p.n_steps, first, second);
     if (p.zero_behind)
-        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * blockDim.y) {
+        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps) {
             const long long to = (q.seq * p.in_seq + i * p.in_step + q.col[0]) * es;
             store_pair<T, ACCESS>((char*)p.out + to, 0, apart, typename W::type{});
             store_pair<T, ACCESS>((char*)p.out2 + to, 0, apart, typename W::type{});
         }
-    if (p.last != nullptr && q.slot == 0) {
+    if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];
     }
@@ -671,21 +868,27 @@ bool round_fits(const RecArgs& a, long long steps, int es) {
     const long long step = a.in_step > a.out_step ? a.in_step : a.out_step;
     return step < (1ll << 32) && (steps * step + a.width) * es < (1ll << 32);
 }
-Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int steps_of_warp) {
+// Blocks of a cluster: of the sizes that the GPU holds as many of at once as there are tiles, the largest (65536 steps of 1024 channels, 16 tiles: 148 SMs hold 15
+// clusters of 8 blocks and 22 of 6, 197 and 140 us).  `room` asks the runtime how many clusters of a size there is room for.
+template <typename Room> Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int steps_of_warp, Room&& room) {
     Shape s;
     s.tiles = (long long)d.n_seq * ((d.width + 63) / 64);
     s.warps = s.blocks = 1;
     while (s.warps < kMaxWarps && (long long)s.warps * steps_of_warp < d.n_steps) s.warps *= 2;
-    while (s.blocks < kMaxCluster && s.tiles * s.blocks < 148 && (long long)s.blocks * s.warps * steps_of_warp < d.n_steps) s.blocks *= 2;
-    while (s.blocks > 1 && !round_fits(a, (long long)s.blocks * s.warps * steps_of_warp, (int)low_size(d.low))) s.blocks /= 2;
+    if (s.tiles * 2 <= sm_count())
+        for (int c : {16, 8, 6, 4, 3, 2})
+            if ((c - 1ll) * s.warps * steps_of_warp < d.n_steps && round_fits(a, (long long)c * s.warps * steps_of_warp, (int)low_size(d.low)) && s.tiles <= room(c)) {
+                s.blocks = c;
+                break;
+            }
     while (s.warps > 1 && !round_fits(a, (long long)s.warps * steps_of_warp, (int)low_size(d.low))) s.warps /= 2;
     return s;
 }
 
-cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), const RecArgs& a, const RecMaps& maps, const Shape& s, size_t smem, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), const RecArgs& a, const RecMaps& maps, const Shape& s, bool scans, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.tiles * s.blocks));
-    cfg.blockDim = dim3(32, s.warps);
+    cfg.blockDim = dim3(32, s.warps + (scans ? 1 : 0));
     cfg.stream = st;
     cfg.dynamicSmemBytes = smem;
     if (smem > 0) {
@@ -733,17 +936,47 @@ bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long l
     return time_major ? make_tensor_map(p, d.low, d.width, d.n_seq, d.n_steps, seq, step, 64, 1, steps, out)
                       : make_tensor_map(p, d.low, d.width, d.n_steps, d.n_seq, step, seq, 64, steps, 1, out);
 }
+// How many clusters of a size the current device holds at once with one block an SM (asked once; the piped kernels are alike in what they need)
+int cluster_room(int blocks) {
+    static std::atomic<int> known[kMaxDevices][kMaxCluster + 1];
+    std::atomic<int>& slot = known[current_device()][blocks];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n > 0) return n - 1;
+    using T = __nv_bfloat16;
+    constexpr int L = kForwardSteps<T>;
+    const auto kernel = recurrence_forward_kernel<T, 2, true, L, PIPED>;
+    const size_t smem = kMaxWarps * kWarpBytes<T, 2, L, 2, PIPED> + sizeof(Scan<2>);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(32, kMaxWarps + 1);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)blocks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    n = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 0;
+    }
+    slot.store(n + 1, std::memory_order_relaxed);
+    return n;
+}
 template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, RecArgs a, cudaStream_t st) {
     constexpr int L = BACKWARD ? kBackwardSteps<T> : kForwardSteps<T>, N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
-    const Shape s = shape_of(d, a, L);
+    const Shape s = shape_of(d, a, L, cluster_room);
     RecMaps maps;
     const auto go = [&](auto access) {
         constexpr int A = access.value;
-        const size_t smem = A == STAGED ? s.warps * kWarpBytes<T, 2, L, N> : 0;
-        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, 2, COUPLED, L, A>, a, maps, s, smem, st);
-        else return launch(recurrence_forward_kernel<T, 2, COUPLED, L, A>, a, maps, s, smem, st);
+        const size_t smem = s.warps * kWarpBytes<T, 2, L, N, A> + (A == PIPED ? sizeof(Scan<2>) : sizeof(Exchange<2>));
+        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
+        else return launch(recurrence_forward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
     };
-    if (d.n_steps > 2 * s.warps * s.blocks * L && pieces_fit(d, a)) {
+    if (d.n_steps > 2 * s.warps * s.blocks * L && words_fit(d, a) && pieces_fit(d, a)) {
         a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;
         const bool tm = a.time_major != 0;
         // (all arrays take their coordinates in one order: where inputs and outputs differ in theirs, registers)
@@ -754,7 +987,7 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
             ok = ok && map_of(a.y, d, a.out_seq, a.out_step, L, tm, &maps.m[2]);
             if (COUPLED) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, L, tm, &maps.m[3]);
         }
-        if (ok) return go(Way<STAGED>());
+        if (ok) return s.blocks > 1 ? go(Way<PIPED>()) : go(Way<STAGED>());
     }
     return words_fit(d, a) ? go(Way<PAIRS>()) : go(Way<SINGLES>());
 }

@@ -61,7 +61,8 @@ template <int WARPS, bool CLUSTER> struct Lane {
 };
 
 // Sums over a row's threads, the same bits in all of them.  One warp: shuffles.  One block: partial sums of its warps in shared memory.  A cluster: every
-// warp's into every block's shared memory.  Two sets of partial sums in turn, so that one barrier a sum does.
+// warp's into every block's shared memory.  Two sets of partial sums in turn, so that one barrier a sum does: a sum is complete only when every warp has sent,
+// and each of them sends behind its own reads of the sum before, so that the set of the one before that is free.
 template <int N, int WARPS, bool CLUSTER> struct RowSum {
     static constexpr int kSlots = WARPS * (CLUSTER ? kResBlocks : 1);
     struct __align__(16) Shared {
@@ -74,7 +75,7 @@ template <int N, int WARPS, bool CLUSTER> struct RowSum {
     __device__ __forceinline__ RowSum(Shared& shared, int blocks) : s(shared) {
         if (!CLUSTER) return;
         for (int i = threadIdx.x; i < 2 * N * kSlots; i += blockDim.x) (&s.part[0][0][0])[i] = 0.f;      // (places of blocks that do not exist)
-        if (threadIdx.x == 0) sets_begin(s.bar);
+        if (threadIdx.x == 0) sets_begin(s.bar, 2);
         cluster_arrive();                                    // nobody writes into a block that has not started
         cluster_wait();
     }
