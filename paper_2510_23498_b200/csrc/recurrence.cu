@@ -428,30 +428,45 @@ template <typename T, int ACCESS> __device__ __forceinline__ void store_pair(cha
     }
 }
 
+// A round in which every step of every warp exists, one in which that has to be asked at each step, or it is not known which of the two
+enum Round : int { GUARDED = 0, WHOLE = 1, EITHER = 2 };
+template <int R> struct Kind { static constexpr int value = R; };
 template <bool B> struct Flag { static constexpr bool value = B; };
-// The rounds from `base` to `end`: both halves of each in turn, or the first half of the next one in front of the second half of this one
-template <bool PIPED_ROUNDS, typename Turn, typename First, typename Second>
-__device__ __forceinline__ void rounds(unsigned base, unsigned stride, unsigned end, First& first, Second& second) {
+template <typename K, typename F> __device__ __forceinline__ void of_kind(K, bool whole, F&& run) {
+    if constexpr (K::value == WHOLE) run(Flag<true>());
+    else if constexpr (K::value == GUARDED) run(Flag<false>());
+    else if (whole) run(Flag<true>());
+    else run(Flag<false>());
+}
+// The rounds from `base` to `end`: both halves of each in turn (whole ones in a loop of their own), or the first half of the next one in front of the second
+// half of this one
+template <bool PIPED_ROUNDS, typename Turn, typename Whole, typename First, typename Second>
+__device__ __forceinline__ void rounds(unsigned base, unsigned stride, unsigned end, Whole&& whole, First& first, Second& second) {
     unsigned round = 0;
     if constexpr (!PIPED_ROUNDS) {
-        Turn a;
-        for (; base < end; base += stride) {
-            first(a, base, round++);
-            second(a);
-        }
+        const auto one = [&](auto kind) {
+            Turn a;
+            first(kind, a, base, round++);
+            second(kind, a);
+            base += stride;
+        };
+        while (base < end && !whole(base)) one(Kind<GUARDED>());
+        while (base < end && whole(base)) one(Kind<WHOLE>());
+        while (base < end) one(Kind<GUARDED>());
     } else {
+        const Kind<EITHER> kind;
         if (base >= end) return;
         Turn a, b;
-        first(a, base, round++);
+        first(kind, a, base, round++);
         while (true) {
             base += stride;
-            if (base >= end) { second(a); return; }
-            first(b, base, round++);
-            second(a);
+            if (base >= end) { second(kind, a); return; }
+            first(kind, b, base, round++);
+            second(kind, a);
             base += stride;
-            if (base >= end) { second(b); return; }
-            first(a, base, round++);
-            second(b);
+            if (base >= end) { second(kind, b); return; }
+            first(kind, a, base, round++);
+            second(kind, b);
         }
     }
 }
@@ -584,7 +599,8 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     if (blocks > 1) cluster_wait();
     // A round's two halves: gates and the map of this warp's steps, published; then the steps again from the state in front of them
     struct Turn { float nb[L][V]; Affine<V> before; unsigned base, round; };
-    auto first = [&](Turn& r, unsigned base, unsigned round) {
+    auto whole = [&](unsigned base) { return base + stride <= (unsigned)q.len; };
+    auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
         r.base = base;
         r.round = round;
         const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0, n = count(base);
@@ -617,10 +633,9 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             if constexpr (kScan) publish(ex, round, own);
             else publish(ex, round, own, r.before, blocks, q.rank);
         };
-        if (base + stride <= (unsigned)q.len) run(Flag<true>());
-        else run(Flag<false>());
+        of_kind(kind, whole(base), run);
     };
-    auto second = [&](const Turn& r) {
+    auto second = [&](auto kind, const Turn& r) {
         float start[V];
         const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0, n = count(r.base);
         if constexpr (kScan) collect(ex, r.round, start, broken);
@@ -643,8 +658,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
                 if (full.value || i < n) store_pair<T, ACCESS>(out, at, apart, COUPLED ? W::negate(W::put(start)) : W::put(start));
             }
         };
-        if (r.base + stride <= (unsigned)q.len) run(Flag<true>());
-        else run(Flag<false>());
+        of_kind(kind, whole(r.base), run);
         out += out_round;
         if (alone) {
 #pragma unroll
@@ -655,7 +669,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             request(r.base + kStages * stride, stage);
         }
     };
-    rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, first, second);
+    rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, whole, first, second);
     if (p.zero_behind)
         for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps)
             store_pair<T, ACCESS>((char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es, 0, apart, typename W::type{});
@@ -664,6 +678,40 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
     }
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written
+}
+
+// A few steps of many sequences (serving token by token): a thread runs them for two channels; nothing to exchange and no shared memory, so that a call costs
+// little more than its launch (100 sequences of 1024 channels, one step: 4 us less than the kernel above)
+constexpr int kFewSteps = 4;
+template <typename T, bool COUPLED, int ACCESS> __global__ void __launch_bounds__(128) recurrence_steps_kernel(const RecArgs p) {
+    using W = Word<T, 2>;
+    const int pairs = (p.width + 1) / 2;
+    const long long i = (long long)blockIdx.x * 128 + threadIdx.x;
+    const int seq = (int)(i / pairs);
+    if (seq >= p.n_seq) return;
+    const int col = (int)(i - (long long)seq * pairs) * 2, col2 = min(col + 1, p.width - 1);
+    const unsigned es = sizeof(T), apart = (col2 - col) * es;
+    const int len = p.lengths != nullptr ? min(max(p.lengths[seq], 0), p.n_steps) : p.n_steps;
+    const long long states = (long long)seq * p.width;
+    float s[2] = {0.f, 0.f};
+    if (p.y0 != nullptr) { s[0] = p.y0[states + col]; s[1] = p.y0[states + col2]; }
+    if (COUPLED) { s[0] = -s[0]; s[1] = -s[1]; }
+    const char *x = (const char*)p.x + (seq * p.in_seq + col) * es, *g = (const char*)p.gate + (seq * p.in_seq + col) * es;
+    char* out = (char*)p.out + (seq * p.out_seq + col) * es;
+    for (int t = 0; t < len; ++t) {
+        float xs[2], f[2], nb[2], none[2];
+        W::get(load_pair<T, ACCESS>(x + t * p.in_step * es, 0, apart), xs);
+        W::get(load_pair<T, ACCESS>(g + t * p.in_step * es, 0, apart), f);
+        negated_gate<T, 2, false>(f, nb, none);
+        step_forward<COUPLED, 2>(s, nb, xs);
+        store_pair<T, ACCESS>(out + t * p.out_step * es, 0, apart, COUPLED ? W::negate(W::put(s)) : W::put(s));
+    }
+    if (p.zero_behind)
+        for (int t = len; t < p.n_steps; ++t) store_pair<T, ACCESS>(out + t * p.out_step * es, 0, apart, typename W::type{});
+    if (p.last != nullptr) {
+        p.last[states + col] = COUPLED ? -s[0] : s[0];
+        p.last[states + col2] = COUPLED ? -s[1] : s[1];
+    }
 }
 
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
@@ -748,7 +796,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     struct Turn { float nb[L][V], slope[L][V]; Affine<V> before; unsigned base, round; };
     // every step of the round exists, and none is time 0
     auto whole = [&](unsigned base) { return base >= skipped && base + stride < (unsigned)p.n_steps; };
-    auto first = [&](Turn& r, unsigned base, unsigned round) {
+    auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
         r.base = base;
         r.round = round;
         const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0;
@@ -784,10 +832,9 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             if constexpr (kScan) publish(ex, round, own);
             else publish(ex, round, own, r.before, blocks, q.rank);
         };
-        if (whole(base)) run(Flag<true>());
-        else run(Flag<false>());
+        of_kind(kind, whole(base), run);
     };
-    auto second = [&](const Turn& r) {
+    auto second = [&](auto kind, const Turn& r) {
         float start[V];
         const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0;
         int lo, hi;
@@ -834,8 +881,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
                 }
             }
         };
-        if (whole(r.base)) run(Flag<true>());
-        else run(Flag<false>());
+        of_kind(kind, whole(r.base), run);
         if (alone) {
 #pragma unroll
             for (int v = 0; v < V; ++v) carry[v] = staged_rows(ACCESS) && broken ? __int_as_float(0x7fffffff) : start[v];
@@ -846,7 +892,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             request(r.base + kStages * stride, stage);
         }
     };
-    rounds<ACCESS == PIPED, Turn>(base, stride, (unsigned)p.n_steps, first, second);
+    rounds<ACCESS == PIPED, Turn>(base, stride, (unsigned)p.n_steps, whole, first, second);
     if (p.zero_behind)
         for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps) {
             const long long to = (q.seq * p.in_seq + i * p.in_step + q.col[0]) * es;
@@ -874,7 +920,8 @@ template <typename Room> Shape shape_of(const mpode_recurrence_desc& d, const Re
     Shape s;
     s.tiles = (long long)d.n_seq * ((d.width + 63) / 64);
     s.warps = s.blocks = 1;
-    while (s.warps < kMaxWarps && (long long)s.warps * steps_of_warp < d.n_steps) s.warps *= 2;
+    // (128 sequences of 128 steps, 4096 tiles: 57 us with 2 warps, 65 with 4, 74 with 8)
+    while (s.warps < kMaxWarps && (long long)s.warps * steps_of_warp < d.n_steps && s.tiles * s.warps < 32 * sm_count()) s.warps *= 2;
     if (s.tiles * 2 <= sm_count())
         for (int c : {16, 8, 6, 4, 3, 2})
             if ((c - 1ll) * s.warps * steps_of_warp < d.n_steps && round_fits(a, (long long)c * s.warps * steps_of_warp, (int)low_size(d.low)) && s.tiles <= room(c)) {
@@ -968,6 +1015,12 @@ int cluster_room(int blocks) {
 }
 template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_recurrence_desc& d, RecArgs a, cudaStream_t st) {
     constexpr int L = BACKWARD ? kBackwardSteps<T> : kForwardSteps<T>, N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
+    if (!BACKWARD && d.n_steps <= kFewSteps) {
+        const unsigned grid = (unsigned)(((long long)d.n_seq * ((d.width + 1) / 2) + 127) / 128);
+        if (words_fit(d, a)) recurrence_steps_kernel<T, COUPLED, PAIRS><<<grid, 128, 0, st>>>(a);
+        else recurrence_steps_kernel<T, COUPLED, SINGLES><<<grid, 128, 0, st>>>(a);
+        return cudaGetLastError();
+    }
     const Shape s = shape_of(d, a, L, cluster_room);
     RecMaps maps;
     const auto go = [&](auto access) {
