@@ -20,4 +20,26 @@ template <typename F> inline cudaError_t with_low(mpode_dtype dt, F&& f) {
     return f(__half{});
 }
 
+// How many clusters of `blocks` blocks of this kernel the current device holds at once (0 when that cannot be told).  Clusters beyond that number would run
+// behind the others: the groups of SMs that a cluster has to fit into leave some of them idle.
+inline int clusters_at_once(const void* kernel, dim3 block, size_t smem, int blocks) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)blocks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess &&
+        (blocks <= 8 || cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) &&
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess)
+        return n;
+    (void)cudaGetLastError();
+    return 0;
+}
+
 }  // namespace mpode

@@ -991,25 +991,8 @@ int cluster_room(int blocks) {
     if (n > 0) return n - 1;
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
-    const auto kernel = recurrence_forward_kernel<T, 2, true, L, PIPED>;
     const size_t smem = kMaxWarps * kWarpBytes<T, 2, L, 2, PIPED> + sizeof(Scan<2>);
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(32, kMaxWarps + 1);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)blocks;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    n = 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-        (void)cudaGetLastError();
-        n = 0;
-    }
+    n = clusters_at_once((const void*)recurrence_forward_kernel<T, 2, true, L, PIPED>, dim3(32, kMaxWarps + 1), smem, blocks);
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }

@@ -12,21 +12,29 @@
 namespace mpode {
 namespace {
 
-// The weights' gradients from the partial rows [rows][2][width], summed in a fixed order: 32 columns and 16 slices of the rows a block.
-// dw_post = scale S, dscale = w_post S, dw_pre.
+// The weights' gradients from the partial rows [rows][2][width], summed in a fixed order: 8 columns (a 32-byte sector of each row) and 64 slices of the rows a
+// block.  dw_post = scale S, dscale = w_post S, dw_pre.
 struct FinishArgs { const float *partial, *w_post, *scale; float *dw_post, *dscale, *dw_pre; int rows, width, accumulate; };
 __global__ void __launch_bounds__(512) residual_finish_kernel(const FinishArgs p) {
-    __shared__ float part[16][33];
-    const int i = blockIdx.x * 32 + threadIdx.x;            // column of the two sums side by side
+    __shared__ float part[64][9];
+    chain_begin();
+    const int c = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    const int i = blockIdx.x * 8 + c;                       // column of the two sums side by side
     float s = 0.f;
-    if (i < 2 * p.width)
-        for (int r = threadIdx.y; r < p.rows; r += 16) s += p.partial[(long long)r * 2 * p.width + i];
-    part[threadIdx.y][threadIdx.x] = s;
+    if (i < 2 * p.width) {
+#pragma unroll 4
+        for (int r = slice; r < p.rows; r += 64) s += p.partial[(long long)r * 2 * p.width + i];
+    }
+    part[slice][c] = s;
     __syncthreads();
-    if (threadIdx.y != 0 || i >= 2 * p.width) return;
+    if (threadIdx.x >= 32) return;
+    // 4 lanes a column, 16 slices each, then the four
     s = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s += part[r][threadIdx.x];
+    for (int k = 0; k < 16; ++k) s += part[(threadIdx.x >> 3) * 16 + k][c];
+    s += __shfl_xor_sync(0xffffffffu, s, 8);
+    s += __shfl_xor_sync(0xffffffffu, s, 16);
+    if (threadIdx.x >= 8 || i >= 2 * p.width) return;
     auto put = [&](float* out, float v) {
         if (out != nullptr) *out = (p.accumulate ? *out : 0.f) + v;
     };
@@ -93,7 +101,13 @@ bool vectors_fit(const mpode_residual_desc& d, const ResArgs& a, bool& torn) {
 
 bool center(const mpode_residual_desc& d) { return d.post_norm == MPODE_NORM_MEANVAR || d.pre_norm == MPODE_NORM_MEANVAR; }
 
-// Rows of partial sums a backward pass leaves.  (The workspace is sized for the shapes of both layouts: which one a call takes depends on its pointers.)
+// no more clusters than run at once (4096 x 8192 bfloat16 backward: 111 of 4 blocks fill the SMs' registers, 104 fit the GPU's groups of SMs)
+ResShape within(ResShape s, int room) {
+    if (s.blocks > 1 && room > 0 && s.clusters > room) s.clusters = room;
+    return s;
+}
+
+// Rows of partial sums a backward pass leaves at most.  (The workspace is sized for the shapes of both layouts: which one a call takes depends on its pointers.)
 size_t partial_rows(int rows, int width, bool vec) {
     const ResShape s = shape_of(rows, width, vec, kBackwardBlocks);
     return (size_t)s.clusters * s.groups;
@@ -128,7 +142,9 @@ mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_
     bool torn;
     const bool vec = vectors_fit(*desc, a, torn);
     if (torn) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: a pointer is not aligned to its elements (stats_dev: 16 bytes)");
-    return operator_launched(launch_residual_forward(desc->low, a, shape_of(rows, desc->width, vec, kForwardBlocks), vec, center(*desc), (cudaStream_t)cuda_stream),
+    ResShape s = shape_of(rows, desc->width, vec, kForwardBlocks);
+    if (s.blocks > 1) s = within(s, residual_forward_room(desc->low, s.blocks));
+    return operator_launched(launch_residual_forward(desc->low, a, s, vec, center(*desc), (cudaStream_t)cuda_stream),
                              "mpode_residual_forward");
 }
 
@@ -169,14 +185,15 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
             if (workspace_bytes < mpode_residual_workspace_bytes(desc, rows)) return operator_fail(MPODE_ERR_WORKSPACE_TOO_SMALL, "%s: workspace too small", who);
             a.partial = (float*)workspace_dev;
         }
-        partials = (int)partial_rows(rows, desc->width, vec);
-        const mpode_status ran = operator_launched(launch_residual_backward(desc->low, a, shape_of(rows, desc->width, vec, kBackwardBlocks), vec, center(*desc), st), who);
+        ResShape s = shape_of(rows, desc->width, vec, kBackwardBlocks);
+        if (s.blocks > 1) s = within(s, residual_backward_room(desc->low, s.blocks));
+        partials = s.clusters * s.groups;
+        const mpode_status ran = operator_launched(launch_residual_backward(desc->low, a, s, vec, center(*desc), st), who);
         if (ran != MPODE_OK || !weights) return ran;
     }
     if (!weights) return MPODE_OK;
     FinishArgs f{a.partial, w_post_dev, scale_dev, dL_dw_post_dev, dL_dscale_dev, dL_dw_pre_dev, partials, desc->width, accumulate};
-    residual_finish_kernel<<<(2 * desc->width + 31) / 32, dim3(32, 16), 0, st>>>(f);
-    return operator_launched(cudaGetLastError(), who);
+    return operator_launched(launch_chain(residual_finish_kernel, dim3((2 * desc->width + 7) / 8), dim3(512), 0, st, f), who);
 }
 
 }  // extern "C"

@@ -1,9 +1,12 @@
 // What the two directions of the residual step share: arguments, how rows lie on threads, row sums.
 #pragma once
+#include <atomic>
+
 #include "cluster.cuh"
 #include "operators.h"
 #include "philox.cuh"
 #include "rows.cuh"
+#include "tensormap.h"
 
 namespace mpode {
 
@@ -30,6 +33,9 @@ constexpr int kResWarps = 8, kResBlocks = 8, kResMaxWidth = kResWarps * 256 * kR
 
 cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
 cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const ResShape& s, bool vec, bool center, cudaStream_t st);
+// clusters of `blocks` blocks that the current device holds at once, asked once for each format width
+int residual_forward_room(mpode_dtype dt, int blocks);
+int residual_backward_room(mpode_dtype dt, int blocks);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float2 pair(float f) { return make_float2(f, f); }
@@ -309,6 +315,16 @@ inline cudaError_t launch_rows(void (*kernel)(const ResArgs, const int), const R
     cfg.attrs = at;
     cfg.numAttrs = s.blocks > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a, s.blocks);
+}
+// the kernel's room, kept per device, format width and cluster size
+template <typename K> int room_of(std::atomic<int> (&known)[kMaxDevices][2][kResBlocks + 1], K kernel16, K kernel32, size_t smem16, size_t smem32, mpode_dtype dt, int blocks) {
+    const bool wide = dt == MPODE_F32;
+    std::atomic<int>& slot = known[current_device()][wide ? 1 : 0][blocks];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n > 0) return n - 1;
+    n = clusters_at_once((const void*)(wide ? kernel32 : kernel16), dim3(32 * kResWarps), wide ? smem32 : smem16, blocks);
+    slot.store(n + 1, std::memory_order_relaxed);
+    return n;
 }
 // Calls f with the shape as types: f(WARPS, CLUSTER).  Rows without 16-byte accesses take fewer shapes (more idle lanes in narrow rows).
 template <int N> struct Int { static constexpr int value = N; };

@@ -196,4 +196,10 @@ cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const Res
     });
 }
 
+int residual_backward_room(mpode_dtype dt, int blocks) {
+    static std::atomic<int> known[kMaxDevices][2][kResBlocks + 1];
+    return room_of(known, residual_backward_kernel<__nv_bfloat16, true, false, kResWarps, true>, residual_backward_kernel<float, true, false, kResWarps, true>,
+                   Rows<__nv_bfloat16, true, kResWarps, true, 2, 3>::kBytes, Rows<float, true, kResWarps, true, 2, 3>::kBytes, dt, blocks);
+}
+
 }  // namespace mpode

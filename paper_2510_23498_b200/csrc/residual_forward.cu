@@ -149,4 +149,10 @@ cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResS
     });
 }
 
+int residual_forward_room(mpode_dtype dt, int blocks) {
+    static std::atomic<int> known[kMaxDevices][2][kResBlocks + 1];
+    return room_of(known, residual_forward_kernel<__nv_bfloat16, true, false, kResWarps, true>, residual_forward_kernel<float, true, false, kResWarps, true>,
+                   Rows<__nv_bfloat16, true, kResWarps, true, 1, 2>::kBytes, Rows<float, true, kResWarps, true, 1, 2>::kBytes, dt, blocks);
+}
+
 }  // namespace mpode
