@@ -48,11 +48,15 @@ def _stored(ref, low, err):
 
 # ------------------------------------------------------------------------------------------------ gated linear recurrence
 def _layout(a, dtype, layout):
-    """[B, T, D] on the device: contiguous, time-major, or a slice of rows twice as long (odd offset)."""
+    """[B, T, D] on the device: contiguous, time-major, a slice of rows twice as long at an odd offset, or their first half."""
     torch, _, _ = _torch()
     t = _up(a, dtype)
     if layout == "time":
         return t.transpose(0, 1).contiguous().transpose(0, 1)
+    if layout == "half":
+        buf = torch.full((t.shape[0], t.shape[1], 2 * t.shape[2]), float("nan"), dtype=t.dtype, device=t.device)
+        buf[..., :t.shape[2]] = t
+        return buf[..., :t.shape[2]]
     if layout == "slice":
         buf = torch.full((t.shape[0], t.shape[1], 2 * t.shape[2] + 1), float("nan"), dtype=t.dtype, device=t.device)
         buf[..., 1:1 + t.shape[2]] = t
@@ -117,6 +121,9 @@ CASES = [
     (2, 8, 64, "bf16", {}), (2, 9, 66, "f16", {}), (2, 16, 32, "f32", {}), (2, 17, 65, "bf16", {}), (1, 129, 64, "bf16", {}), (5, 127, 130, "f16", dict(ragged=True)),
     # split over clusters, several rounds
     (1, 1100, 40, "bf16", {}), (1, 2049, 34, "f32", {}), (2, 1500, 31, "f16", dict(ragged=True)), (3, 700, 100, "bf16", dict(ragged=True, layout="time")),
+    # tiles brought to shared memory ahead: blocks by themselves (enough channels in all), and clusters over several rounds
+    (80, 300, 64, "bf16", dict(ragged=True)), (75, 290, 72, "f32", dict(layout="time")), (20, 700, 200, "f16", dict(ragged=True, layout="half")),
+    (1, 5000, 64, "bf16", {}), (2, 4500, 40, "f16", dict(ragged=True)), (1, 2600, 72, "f32", dict(layout="half")), (3, 3000, 328, "bf16", dict(ragged=True, layout="time")),
     # many short sequences
     (300, 5, 66, "bf16", dict(ragged=True)), (40, 33, 96, "f32", dict(ragged=True, layout="time")),
     # slices of wider rows at odd addresses
@@ -144,7 +151,7 @@ def test_recurrence_against_the_oracle(B, T, D, low, kw, coupled):
     _check_backward({**c, "y0": z, "dy": np.zeros_like(c["dy"])}, coupled, _np(y), got)
 
 
-@pytest.mark.parametrize("T", [1, 40, 1300])
+@pytest.mark.parametrize("T", [1, 40, 1300, 5000])
 @pytest.mark.parametrize("coupled", [True, False])
 def test_recurrence_with_extreme_gates(T, coupled):
     # Gates of infinity reset the state, of minus infinity keep it; 1e-6 a step is a memory of a million steps.  float32, both directions.
@@ -158,6 +165,54 @@ def test_recurrence_with_extreme_gates(T, coupled):
     y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"], coupled=coupled)
     _check_forward(c, coupled, y, yT)
     _check_backward(c, coupled, _np(y), b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"], coupled=coupled))
+
+
+@pytest.mark.parametrize("low", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 50, 5000])
+def test_recurrence_passes_on_what_is_not_a_number(low, T):
+    # A NaN in one channel's gate or input reaches that channel's later states and earlier gradients, and no other channel
+    torch, b, _ = _torch()
+    c = _recurrence_case(2, T, 64, low)
+    at = T // 2
+    for name, channel in (("t_gate", 5), ("t_x", 40)):
+        c[name][1, at, channel] = float("nan")
+    y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"])
+    want = torch.zeros_like(y, dtype=torch.bool)
+    want[1, at:, 5] = want[1, at:, 40] = True
+    assert torch.equal(y.isnan(), want) and torch.equal(yT.isnan(), want[:, -1])
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    dx, dg, dy0 = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], flag=flag)
+    assert dx[1, :at + 1, 5].isnan().all() and dy0[1, 5].isnan() and not dx[0].isnan().any() and not dy0[0].isnan().any()
+    assert not dx[1, at + 1:, 5].isnan().any() and not dx[1, :, 40].isnan().any() and dg[1, at, 40].isnan() and int(flag) == 1
+
+
+def test_recurrence_takes_outputs_of_other_strides_and_alignment_than_its_inputs():
+    # Inputs that bulk copies can read, outputs that they could not write: odd addresses, the other order of time and sequences
+    torch, b, _ = _torch()
+    for B, T, D, low in ((80, 300, 64, "bf16"), (1, 5000, 64, "f16"), (2, 2600, 64, "f32")):
+        c = _recurrence_case(B, T, D, low)
+        y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"])
+        ref = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"])
+
+        def odd(shape):
+            return torch.empty(shape[0] * shape[1] * shape[2] + 1, dtype=y.dtype, device=y.device)[1:].view(shape)
+
+        out, dx, dg = odd(y.shape), odd(y.shape), odd(y.shape)
+        b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"], y=out)
+        b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"], dL_dx=dx, dL_dgate=dg)
+        assert _same(out, y) and _same(dx, ref[0]) and _same(dg, ref[1])
+        if B > 1:
+            tm = torch.empty((T, B, D), dtype=y.dtype, device=y.device).transpose(0, 1)
+            b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"], y=tm)
+            dy = torch.empty_like(tm).copy_(c["t_dy"])
+            got = b.recurrence_backward(c["t_x"], c["t_gate"], tm, dy, dL_dyT=c["t_dyT"], y0=c["t_y0"])
+            assert _same(tm, y) and _same(got[0], ref[0]) and _same(got[1], ref[1])
+
+
+def _same(got, ref):
+    """Equal up to what the order of a composition may change: 2^-6 of a 16-bit value, 2^-15 of a float32 one, where the largest are about 10."""
+    tol = 2.0 ** -15 if got.dtype == ref.dtype and got.element_size() == 4 else 2.0 ** -6
+    return bool(((got.float() - ref.float()).abs() <= tol * (ref.float().abs() + 1)).all())
 
 
 def test_recurrence_slow_channels_keep_their_rate_over_long_sequences():
@@ -321,7 +376,10 @@ RES = [
     (33, 512, "f16", ("none", "rms"), dict(p=0.5)), (600, 64, "bf16", ("rms", "rms"), dict(weights=False)), (11, 785, "f32", ("meanvar", "meanvar"), dict(p=0.1)),
     (500, 1024, "bf16", ("rms", "rms"), {}), (7, 2048, "f16", ("rms", "meanvar"), dict(gated=False, p=0.25)), (5, 4096, "bf16", ("meanvar", "meanvar"), {}),
     (4, 4097, "f32", ("rms", "rms"), {}), (6, 8192, "bf16", ("rms", "rms"), dict(p=0.1)), (3, 16384, "f16", ("meanvar", "rms"), {}),
-    (3, 12300, "bf16", ("rms", "meanvar"), dict(weights=False)),
+    (3, 12300, "bf16", ("rms", "meanvar"), dict(weights=False)), (40, 4104, "bf16", ("meanvar", "rms"), dict(p=0.2)), (9, 6000, "f32", ("rms", "rms"), {}),
+    # more rows than run at once: every block goes through several
+    (2000, 1024, "bf16", ("rms", "rms"), dict(p=0.1)), (1500, 2048, "f16", ("meanvar", "rms"), {}), (9000, 64, "bf16", ("rms", "meanvar"), {}),
+    (700, 4096, "bf16", ("rms", "rms"), dict(p=0.1)), (1200, 785, "f32", ("rms", "rms"), {}), (5000, 40, "f32", ("meanvar", "meanvar"), dict(gated=False)),
     (12, 64, "bf16", ("rms", "rms"), dict(layout="slice")), (12, 1001, "f16", ("rms", "rms"), dict(layout="slice", p=0.2)),
 ]
 
@@ -379,6 +437,50 @@ def test_residual_step_without_block_or_without_next_input():
     inplace = c["t_y"].clone()
     out = step.forward(inplace, c["t_u"], y_out=inplace)
     assert out[0] is inplace and torch.equal(inplace, full[0]) and torch.equal(out[1], full[1])
+
+
+@pytest.mark.parametrize("D", [64, 785, 2048, 4096])
+def test_residual_step_over_its_own_inputs(D):
+    # y' over y; dL_dy over dL_dy', dL_du over u and dL_dgate over gate, through the C entry points
+    import ctypes as C
+    torch, b, _ = _torch()
+    M = 1000
+    c = _residual_case(M, D, "bf16")
+    w = dict(gate=c["t_gate"], w_post=c["t_w_post"], scale=c["t_scale"], w_pre=c["t_w_pre"])
+    step = b.ResidualStep(D, low="bf16", h=0.5)
+    y, z, stats = step.forward(c["t_y"], c["t_u"], **w)
+    ref = step.backward(y, c["t_u"], stats, dL_dy=c["t_dy"], dL_dz=c["t_dz"], **w)
+    inplace = c["t_y"].clone()
+    got = step.forward(inplace, c["t_u"], y_out=inplace, **w)
+    assert torch.equal(inplace, y) and torch.equal(got[1], z) and torch.equal(got[2], stats)
+    lib = b.load_library()
+    desc = step._desc(D, D, D, D)
+    a, u, g = c["t_dy"].clone(), c["t_u"].clone(), c["t_gate"].clone()
+    grads = [torch.empty(D, device="cuda:0") for _ in range(3)]
+    n = lib.mpode_residual_workspace_bytes(desc, M)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda:0")
+    at = [t.data_ptr() for t in (y, u, g, w["w_post"], w["scale"], w["w_pre"])] + [None] + [t.data_ptr() for t in (stats, a, c["t_dz"])]
+    st = lib.mpode_residual_backward(desc, torch.cuda.current_stream().cuda_stream, M, *at, 0, a.data_ptr(), u.data_ptr(), g.data_ptr(),
+                                     *[t.data_ptr() for t in grads], 0, None, ws.data_ptr(), n)
+    assert st == b.OK
+    assert torch.equal(a, ref["dy"]) and torch.equal(u, ref["du"]) and torch.equal(g, ref["dgate"])
+    assert all(torch.equal(x, ref[k]) for x, k in zip(grads, ("dw_post", "dscale", "dw_pre")))
+
+
+def test_residual_step_passes_on_what_is_not_a_number():
+    torch, b, _ = _torch()
+    for D in (64, 200, 2048, 4096):
+        c = _residual_case(40, D, "bf16")
+        step = b.ResidualStep(D, low="bf16")
+        c["t_u"][7, 3] = float("nan")
+        c["t_u"][9, 5] = float("inf")
+        y, z, stats = step.forward(c["t_y"], c["t_u"], gate=c["t_gate"])
+        clean = torch.ones(40, dtype=torch.bool, device="cuda:0")
+        clean[7] = clean[9] = False
+        assert y[7].isnan().all() and z[7].isnan().all() and z[9].isnan().any() and not y[clean].isnan().any() and not z[clean].isnan().any()
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+        g = step.backward(y, c["t_u"], stats, dL_dy=c["t_dy"], dL_dz=c["t_dz"], gate=c["t_gate"], flag=flag)
+        assert g["du"][7].isnan().all() and not g["du"][clean].isnan().any() and int(flag) == 1
 
 
 # ------------------------------------------------------------------------------------------------ dropout
@@ -555,6 +657,38 @@ def test_captured_and_replayed_on_another_stream_with_new_inputs():
     torch.cuda.synchronize()
     assert not torch.equal(new[0], eager[0])
     assert torch.equal(out[0], new[0]) and all(torch.equal(out[2][k], new[2][k]) for k in new[2])
+
+
+def test_calls_on_two_streams_at_once():
+    # Each operator on two streams, queued alternately with different inputs: the same bits as one after the other
+    torch, b, _ = _torch()
+    work = []
+    for seed in (1, 2):
+        long, batch, rows = _recurrence_case(1, 6000, 128, "bf16", seed=seed), _recurrence_case(90, 300, 64, "bf16", seed=seed), _residual_case(900, 4096, "bf16", seed=seed)
+        step = b.ResidualStep(4096, low="bf16")
+        w = dict(gate=rows["t_gate"], w_post=rows["t_w_post"], scale=rows["t_scale"], w_pre=rows["t_w_pre"])
+
+        def run(long=long, batch=batch, rows=rows, step=step, w=w):
+            out = []
+            for c in (long, batch):
+                y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"])
+                out += [y, yT, *b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"])]
+            y, z, stats = step.forward(rows["t_y"], rows["t_u"], **w)
+            g = step.backward(y, rows["t_u"], stats, dL_dy=rows["t_dy"], dL_dz=rows["t_dz"], **w)
+            return out + [y, z, stats] + [g[k] for k in sorted(g)]
+
+        work.append(run)
+    alone = [run() for run in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    for _ in range(4):
+        together = []
+        for run, s in zip(work, streams):
+            with torch.cuda.stream(s):
+                together.append(run())
+        torch.cuda.synchronize()
+        for x, y in zip(alone, together):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
 
 
 def test_operators_work_on_empty_batches():

@@ -109,6 +109,7 @@ def test_recurrence_refuses_bad_arguments():
     for kw in bad[:10] + [dict(at={0: None}), dict(at={1: None}), dict(at={4: None}), dict(at={7: None}), dict(at={8: None}), dict(at={10: AT[10] + 2})]:
         assert _recurrence(lib, "backward", **kw) == b.ERR_INVALID_ARG, kw
     assert _recurrence(lib, n_seq=1 << 30, width=1 << 20) == b.ERR_UNSUPPORTED
+    assert _recurrence(lib, n_seq=1, in_step_stride=1 << 27) == b.ERR_UNSUPPORTED        # 16 steps beyond 4 GB
     assert lib.mpode_recurrence_forward(None, None, *AT[:6]) == b.ERR_INVALID_ARG
     assert _recurrence(lib, n_seq=0, at={i: None for i in range(6)}) == b.OK            # nothing to do
 
@@ -170,6 +171,7 @@ def test_tensors_that_do_not_fit_are_refused_by_the_binding():
              lambda: b.recurrence_forward(x[:, :1].expand(2, 3, 8), x),
              lambda: b.recurrence_forward(x, x, y0=torch.zeros(2, 7)),
              lambda: b.recurrence_forward(x, x, lengths=torch.zeros(2, dtype=torch.int64)),
+             lambda: b.recurrence_backward(x, x, x, x, dL_dx=x.clone()),                        # dL_dx without dL_dgate
              lambda: b.recurrence_backward(x, x, x, x, dL_dyT=torch.zeros(2, 8, dtype=torch.float64)),
              lambda: b.ResidualStep(8).forward(torch.zeros(3, 8), torch.zeros(3, 8)),           # u is not bf16
              lambda: b.ResidualStep(8).forward(torch.zeros(3, 8), w_pre=torch.zeros(9)),
