@@ -297,8 +297,10 @@ const char* mpode_last_error(const mpode_ctx* ctx);
  * Operators of sequence and residual networks around a block that the caller evaluates (the paper has no counterpart; its formats, its
  * stored trajectory and its adjoint scaling carry over).  The velocities above are built in; a caller whose block is its own code takes
  * the steps of Alg. 1 and Alg. 2 with these calls.  They need no context.  Conventions beyond those at the top of this file:
- *   - Every call only queues kernels on `cuda_stream`: no allocation, no synchronisation, nothing kept between calls, so calls may be
+ *   - Every call only queues kernels on `cuda_stream`: no allocation, no synchronisation, nothing of the data kept between calls, so calls may be
  *     captured into a CUDA graph and run at the same time.  All buffers live on the current device.
+ *   - Blocks of a cluster wait for one another's partial results, and for their own bulk copies.  These waits end by construction; should one not within 2 s,
+ *     the rest of the outputs is NaN and the kernel ends.
  *   - Arguments are checked before anything is queued; mpode_operator_error returns the message of the last call of this host thread that failed.
  *   - The low format is that of the block's tensors; states, adjoints, statistics, weights and weight gradients are float32.  Results are
  *     rounded to the low format once, when written, and are the same bits in every run.
@@ -322,7 +324,8 @@ typedef struct {
     int coupled;
     int zero_behind;              /* lengths: elements of y, dL_dx and dL_dgate behind a sequence's length: 0 = left as they are, else set to zero */
     long long in_seq_stride, in_step_stride;   /* x, gate, dL_dx, dL_dgate: element (s, i, c) at s * in_seq_stride + i * in_step_stride + c */
-    long long out_seq_stride, out_step_stride; /* y, dL_dy; 0 = [n_seq][n_steps][width].  Rows must not overlap. */
+    long long out_seq_stride, out_step_stride; /* y, dL_dy; 0 = [n_seq][n_steps][width].  Rows must not overlap,
+                                                  and 16 steps have to lie within 4 GB (MPODE_ERR_UNSUPPORTED otherwise). */
 } mpode_recurrence_desc;
 
 /*

@@ -450,6 +450,11 @@ def _same_layout(name: str, t, shape, dtype, layout):
         _refuse("%s has to have the strides %s" % (name, layout))
 
 
+def _like(t):
+    """A tensor of the strides of t (a slice's gaps included)."""
+    return _torch.empty_like(t) if t.is_contiguous() else _torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
+
+
 def _sequences(x):
     if x.dim() != 3:
         _refuse("x has to be [n_seq, n_steps, width]")
@@ -489,13 +494,13 @@ def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, c
     lib, torch = _load()
     shape = _sequences(x)
     n, steps, width = shape
-    low, dtype, device = _low_of(x), x.dtype, x.device
+    low, dtype = _low_of(x), x.dtype
     inner, outer = _layout("x", x, shape, dtype), _layout("y", y, shape, dtype)
     _same_layout("gate", gate, shape, dtype, inner)
     _same_layout("dL_dy", dL_dy, shape, dtype, outer)
     new = dL_dx is None and dL_dgate is None
     if new:
-        dL_dx, dL_dgate = (torch.empty_strided(shape, x.stride(), dtype=dtype, device=device) for _ in range(2))
+        dL_dx, dL_dgate = _like(x), _like(x)
     elif dL_dx is None or dL_dgate is None:
         _refuse("dL_dx and dL_dgate are given together or not at all")
     else:
@@ -503,7 +508,7 @@ def recurrence_backward(x, gate, y, dL_dy, dL_dyT=None, y0=None, lengths=None, c
         _same_layout("dL_dgate", dL_dgate, shape, dtype, inner)
     states = (n, width)
     if dL_dy0 is None:
-        dL_dy0 = torch.empty(states, dtype=torch.float32, device=device)
+        dL_dy0 = x.new_empty(states, dtype=torch.float32) if dL_dyT is None else torch.empty_like(dL_dyT)
     else:
         _expect("dL_dy0", dL_dy0, states, torch.float32)
     _expect("y0", y0, states, torch.float32)
@@ -571,9 +576,9 @@ class ResidualStep:
         if y_out is not None:
             _same_rows("y_out", y_out, shape, f32, ld_y)
         elif u is not None:
-            y_out = torch.empty_like(y) if y.is_contiguous() else y.new_empty_strided(shape, y.stride())
+            y_out = _like(y)
         if want_z and z is None:
-            z = y.new_empty(shape, dtype=low)
+            z = torch.empty_like(u) if u is not None and u.is_contiguous() else y.new_empty(shape, dtype=low)
         stats = y.new_empty((shape[0], 4))
         desc = self._desc(ld_y, _rows("u", u, shape, low), _rows("gate", gate, shape, low), _rows("z", z, shape, low))
         _run(lib.mpode_residual_forward, desc, (y, u, gate, w_post, scale, w_pre, rng, y_out, z),
@@ -586,23 +591,19 @@ class ResidualStep:
         format, times 2^scale_exp; None without u, gate) and the gradients "dw_post", "dscale", "dw_pre" of the weights that were given (added to the
         tensors of that name in accumulate_into when given).  flag: int32 tensor of one element, set to 1 when du or dgate is not finite."""
         lib, torch = _load()
-        f32, low, device = torch.float32, self.low_torch, y_new.device
+        f32, low = torch.float32, self.low_torch
         shape = self._shape(y_new, w_post, scale, w_pre, rng)
         rows = shape[0]
         _expect("stats", stats, (rows, 4), f32)
         _expect("flag", flag, (1,), torch.int32)
         ld_y, ld_u, ld_gate = _rows("y_new", y_new, shape, f32), _rows("u", u, shape, low), _rows("gate", gate, shape, low)
         _same_rows("dL_dy", dL_dy, shape, f32, ld_y)
-        out = {"dy": torch.empty_strided(shape, y_new.stride(), dtype=f32, device=device), "du": None, "dgate": None}
-        if u is not None:
-            out["du"] = torch.empty_strided(shape, u.stride(), dtype=low, device=device)
-        if gate is not None:
-            out["dgate"] = torch.empty_strided(shape, gate.stride(), dtype=low, device=device)
+        out = {"dy": _like(y_new), "du": None if u is None else _like(u), "dgate": None if gate is None else _like(gate)}
         for key, w in (("dw_post", w_post), ("dscale", scale), ("dw_pre", w_pre)):
             g = None
             if want_weights and w is not None:
                 if accumulate_into is None:
-                    g = torch.empty(self.width, dtype=f32, device=device)
+                    g = torch.empty_like(w)
                 else:
                     g = accumulate_into[key]
                     _expect(key, g, (self.width,), f32)
@@ -610,9 +611,9 @@ class ResidualStep:
         grads = (out["dw_post"], out["dscale"], out["dw_pre"])
         desc = self._desc(ld_y, ld_u, ld_gate, _rows("dL_dz", dL_dz, shape, low))
         ws, nbytes = None, 0
-        if rows > 0 and grads != (None, None, None):
+        if rows > 0 and not (grads[0] is None and grads[1] is None and grads[2] is None):
             nbytes = lib.mpode_residual_workspace_bytes(desc, rows)
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            ws = y_new.new_empty(nbytes // 4)
         _run(lib.mpode_residual_backward, desc, (y_new, u, stats, dL_dy, dL_dz, gate, w_post, scale, w_pre, rng, flag) + grads,
              (rows, _ptr(y_new), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(rng), _ptr(stats), _ptr(dL_dy), _ptr(dL_dz),
               int(scale_exp), _ptr(out["dy"]), _ptr(out["du"]), _ptr(out["dgate"]), _ptr(grads[0]), _ptr(grads[1]), _ptr(grads[2]),

@@ -46,12 +46,11 @@ __global__ void __launch_bounds__(512) residual_finish_kernel(const FinishArgs p
 }
 
 // at_once: clusters (of one warp row each) that the GPU is to hold
-ResShape shape_of(int rows, int width, bool vec, int at_once) {
+ResShape shape_of(int rows, int width, int at_once) {
     ResShape s;
     s.blocks = (width + kResWarps * 256 - 1) / (kResWarps * 256);
     s.warps = 1;
     while (s.warps * 256 < width && s.warps < kResWarps) s.warps *= 2;
-    if (!vec && (s.warps == 2 || s.warps == 4)) s.warps = 8;
     s.groups = s.warps == 1 ? kResGroups : 1;
     const int need = (rows + s.groups - 1) / s.groups;
     int most = at_once * (s.warps >= 8 || s.warps == 1 ? 1 : 8 / s.warps);
@@ -107,9 +106,9 @@ ResShape within(ResShape s, int room) {
     return s;
 }
 
-// Rows of partial sums a backward pass leaves at most.  (The workspace is sized for the shapes of both layouts: which one a call takes depends on its pointers.)
-size_t partial_rows(int rows, int width, bool vec) {
-    const ResShape s = shape_of(rows, width, vec, kBackwardBlocks);
+// Rows of partial sums a backward pass leaves at most
+size_t partial_rows(int rows, int width) {
+    const ResShape s = shape_of(rows, width, kBackwardBlocks);
     return (size_t)s.clusters * s.groups;
 }
 
@@ -122,8 +121,7 @@ extern "C" {
 
 size_t mpode_residual_workspace_bytes(const mpode_residual_desc* desc, int rows) {
     if (check(desc, rows, "mpode_residual_workspace_bytes") != MPODE_OK || rows == 0) return 0;
-    const size_t a = partial_rows(rows, desc->width, true), b = partial_rows(rows, desc->width, false);
-    return (a > b ? a : b) * 2 * desc->width * sizeof(float);
+    return partial_rows(rows, desc->width) * 2 * desc->width * sizeof(float);
 }
 
 mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_stream, int rows, const float* y_dev, const void* u_dev,
@@ -142,7 +140,7 @@ mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_
     bool torn;
     const bool vec = vectors_fit(*desc, a, torn);
     if (torn) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_residual_forward: a pointer is not aligned to its elements (stats_dev: 16 bytes)");
-    ResShape s = shape_of(rows, desc->width, vec, kForwardBlocks);
+    ResShape s = shape_of(rows, desc->width, kForwardBlocks);
     if (s.blocks > 1) s = within(s, residual_forward_room(desc->low, s.blocks));
     return operator_launched(launch_residual_forward(desc->low, a, s, vec, center(*desc), (cudaStream_t)cuda_stream),
                              "mpode_residual_forward");
@@ -185,7 +183,7 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
             if (workspace_bytes < mpode_residual_workspace_bytes(desc, rows)) return operator_fail(MPODE_ERR_WORKSPACE_TOO_SMALL, "%s: workspace too small", who);
             a.partial = (float*)workspace_dev;
         }
-        ResShape s = shape_of(rows, desc->width, vec, kBackwardBlocks);
+        ResShape s = shape_of(rows, desc->width, kBackwardBlocks);
         if (s.blocks > 1) s = within(s, residual_backward_room(desc->low, s.blocks));
         partials = s.clusters * s.groups;
         const mpode_status ran = operator_launched(launch_residual_backward(desc->low, a, s, vec, center(*desc), st), who);

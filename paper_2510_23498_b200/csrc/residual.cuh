@@ -180,6 +180,7 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
         if (WARPS == 1) __syncwarp();
         else __syncthreads();
     }
+    __device__ __forceinline__ void touch(const void* const (&)[WIDE + LOW]) const {}
     // by the leader, for the arrays that are there: from[k] is the row's first column of this block, or null
     __device__ __forceinline__ void request(int s, const void* const (&from)[WIDE + LOW]) {
         unsigned bytes = 0;
@@ -222,6 +223,15 @@ template <typename T, int WARPS, bool CLUSTER, int WIDE, int LOW> struct Rows<T,
     bool broken = false, leader = false;
     __device__ __forceinline__ Rows(char*, const L& q) : at(q.at), n(q.n(0)) {}
     __device__ __forceinline__ void sync() const {}
+    // The row after this one: all its arrays are on their way to the cache at once, a row ahead of the phases that read them
+    __device__ __forceinline__ void touch(const void* const (&from)[WIDE + LOW]) const {
+#pragma unroll
+        for (int k = 0; k < WIDE + LOW; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (from[k] != nullptr && n > L::kHalf * h)
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"((const char*)from[k] + (at + L::kHalf * h) * (k < WIDE ? 4 : (int)sizeof(T))));
+    }
     __device__ __forceinline__ void request(int, const void* const (&from)[WIDE + LOW]) {
 #pragma unroll
         for (int k = 0; k < WIDE + LOW; ++k) row[k] = from[k];
@@ -326,7 +336,7 @@ template <typename K> int room_of(std::atomic<int> (&known)[kMaxDevices][2][kRes
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }
-// Calls f with the shape as types: f(WARPS, CLUSTER).  Rows without 16-byte accesses take fewer shapes (more idle lanes in narrow rows).
+// Calls f with the shape as types: f(WARPS, CLUSTER)
 template <int N> struct Int { static constexpr int value = N; };
 template <bool B> struct Bool { static constexpr bool value = B; };
 template <typename F> cudaError_t with_shape(const ResShape& s, F&& f) {

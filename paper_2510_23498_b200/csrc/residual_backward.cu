@@ -28,12 +28,13 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
     const int groups_row = (p.width + 7) / 8;
     const float inv = 1.f / (float)p.width;
     const bool has_dz = p.dz != nullptr, has_dy = p.dy != nullptr, has_u = p.u != nullptr, has_gate = p.gate != nullptr;
-    auto request = [&](long long r, int stage) {
+    auto request = [&](long long r, int stage, bool ahead = false) {
         const int c = q.base;
         const void* const from[5] = {has_dz ? p.y + r * p.ld_y + c : nullptr, has_dy ? p.dy + r * p.ld_y + c : nullptr,
                                      has_dz ? (const T*)p.dz + r * p.ld_z + c : nullptr, has_u ? (const T*)p.u + r * p.ld_u + c : nullptr,
                                      has_gate ? (const T*)p.gate + r * p.ld_gate + c : nullptr};
-        in.request(stage, from);
+        if (ahead) in.touch(from);
+        else in.request(stage, from);
     };
     if (in.leader)
         for (int k = 0; k < in.kStages; ++k)
@@ -68,7 +69,11 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
         const int next = q.step < p.rows - row ? row + q.step : p.rows;
         const float4 st = stats;
         if (p.stats != nullptr && next < p.rows) stats = reinterpret_cast<const float4*>(p.stats)[next];
-        if (!VEC) request(row, 0);
+        if (!VEC) {
+            if (row == q.first) request(row, 0, true);
+            if (next < p.rows) request(next, 0, true);
+            request(row, 0);
+        }
         in.wait();
         const float s_u = st.y, r_y = in.broken ? __int_as_float(0x7fffffff) : st.w;
         float2 m0 = pair(0.f), m1 = pair(0.f), n0, n1;
@@ -186,10 +191,7 @@ cudaError_t launch_residual_backward(mpode_dtype dt, const ResArgs& a, const Res
             constexpr int W = warps.value;
             constexpr bool C = cluster.value;
             constexpr size_t smem = Rows<T, true, W, C, 2, 3>::kBytes;
-            if (!vec) {
-                if constexpr (W == 2 || W == 4) return cudaErrorInvalidValue;
-                else return launch_rows(residual_backward_kernel<T, false, true, W, C>, a, s, 0, st);
-            }
+            if (!vec) return launch_rows(residual_backward_kernel<T, false, true, W, C>, a, s, 0, st);
             return center ? launch_rows(residual_backward_kernel<T, true, true, W, C>, a, s, smem, st)
                           : launch_rows(residual_backward_kernel<T, true, false, W, C>, a, s, smem, st);
         });

@@ -19,10 +19,11 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
     const int groups_row = (p.width + 7) / 8;
     const float inv = 1.f / (float)p.width;
     const bool has_u = p.u != nullptr, has_gate = p.gate != nullptr;
-    auto request = [&](long long r, int stage) {
+    auto request = [&](long long r, int stage, bool ahead = false) {
         const void* const from[3] = {p.y + r * p.ld_y + q.base, has_u ? (const T*)p.u + r * p.ld_u + q.base : nullptr,
                                      has_gate ? (const T*)p.gate + r * p.ld_gate + q.base : nullptr};
-        in.request(stage, from);
+        if (ahead) in.touch(from);
+        else in.request(stage, from);
     };
     if (in.leader)
         for (int k = 0; k < in.kStages; ++k)
@@ -49,7 +50,11 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
     while (row < p.rows) {
         const int next = q.step < p.rows - row ? row + q.step : p.rows;
         float mean_u = 0.f, rstd_u = 1.f, mean_y = 0.f, rstd_y = 1.f;
-        if (!VEC) request(row, 0);
+        if (!VEC) {
+            if (row == q.first) request(row, 0, true);
+            if (next < p.rows) request(next, 0, true);
+            request(row, 0);
+        }
         in.wait();
         Oct y;
         if (has_u) {
@@ -139,10 +144,7 @@ cudaError_t launch_residual_forward(mpode_dtype dt, const ResArgs& a, const ResS
             constexpr int W = warps.value;
             constexpr bool C = cluster.value;
             constexpr size_t smem = Rows<T, true, W, C, 1, 2>::kBytes;
-            if (!vec) {
-                if constexpr (W == 2 || W == 4) return cudaErrorInvalidValue;
-                else return launch_rows(residual_forward_kernel<T, false, true, W, C>, a, s, 0, st);
-            }
+            if (!vec) return launch_rows(residual_forward_kernel<T, false, true, W, C>, a, s, 0, st);
             return center ? launch_rows(residual_forward_kernel<T, true, true, W, C>, a, s, smem, st)
                           : launch_rows(residual_forward_kernel<T, true, false, W, C>, a, s, smem, st);
         });
