@@ -471,10 +471,17 @@ __device__ __forceinline__ void rounds(unsigned base, unsigned stride, unsigned 
     }
 }
 
+// the cache lines of a row's part of `bytes` bytes
+template <typename T> __device__ __forceinline__ void touch_row(const char* p, int bytes) {
+    asm volatile("prefetch.global.L1 [%0];" ::"l"(p));
+    asm volatile("prefetch.global.L1 [%0];" ::"l"(p + bytes - 1));
+    if (sizeof(T) == 4) asm volatile("prefetch.global.L1 [%0];" ::"l"(p + bytes / 2));
+}
+
 // Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
 //   STAGED, PIPED: brought to shared memory two rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
 //           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
-//   else:   loaded into registers when the round starts (a round ahead took more registers and more time).
+//   else:   loaded into registers when the round starts, from the cache, for which a lane has asked for one row of the round a round ahead.
 template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 __host__ __device__ constexpr int stages(int access) { return access == PIPED ? 3 : access == STAGED ? 2 : 0; }
 template <typename T, int V, int L, int N, int ACCESS> constexpr int kWarpBytes = stages(ACCESS) * N * L * kRowBytes<T, V>;
@@ -590,6 +597,9 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             tile.load(0, g, in_at, in_step, 0, n);
             tile.load(1, x, in_at, in_step, 0, n);
             x += in_round; g += in_round;
+            const int k = threadIdx.x / L, i = threadIdx.x % L;
+            if (k < 2 && i < count(base + stride))
+                touch_row<T>((k == 0 ? g : x) + (unsigned)(in_at - (q.col[0] - q.tile) * es + i * in_step), min(64, p.width - q.tile) * (int)es);
         }
     };
     if constexpr (staged_rows(ACCESS)) {
@@ -784,6 +794,14 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             tile.load(2, y, out_at, 0u - out_step, lo, before);
             if constexpr (COUPLED) tile.load(3, x, in_at, 0u - in_step, lo, hi);
             x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
+            const int k = threadIdx.x / L, i = threadIdx.x % L;
+            range(base + stride, lo, hi);
+            const bool last = k == 2 && base + stride + q.slot * L + i + 1 == (unsigned)p.n_steps;
+            if (k < kArrays && (k != 1 || p.dy != nullptr) && i >= lo && i < hi && !last) {
+                const unsigned to_tile = (q.col[0] - q.tile) * es;
+                const char* const from = k == 0 ? g : k == 1 ? dy : k == 2 ? y : x;
+                touch_row<T>(from + (unsigned)((k == 0 || k == 3 ? in_at - i * in_step : out_at - i * out_step) - to_tile), min(64, p.width - q.tile) * (int)es);
+            }
         }
     };
     if constexpr (staged_rows(ACCESS)) {
