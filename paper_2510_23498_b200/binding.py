@@ -176,7 +176,7 @@ NAMED_TABLEAUX = {
 
 def _ptr(t) -> int:
     """Device (or pinned host) address of a torch tensor, or 0."""
-    return 0 if t is None else int(t.data_ptr())
+    return 0 if t is None else t.data_ptr()
 
 
 class Context:
@@ -470,20 +470,25 @@ def recurrence_forward(x, gate, y0=None, lengths=None, coupled: bool = True, y=N
     n, steps, width = shape
     low, dtype = _low_of(x), x.dtype
     inner = _layout("x", x, shape, dtype)
-    _same_layout("gate", gate, shape, dtype, inner)
-    new = y is None
-    if new:
+    if gate.shape != shape or gate.dtype != dtype or gate.stride() != x.stride():
+        _same_layout("gate", gate, shape, dtype, inner)
+    zero_behind = 0
+    if y is None:
         y = torch.empty_like(x)                                                   # (time-major inputs get a time-major trajectory)
-    outer = _layout("y", y, shape, dtype)
+        outer = inner if y.stride() == x.stride() else _layout("y", y, shape, dtype)
+        if lengths is not None:
+            zero_behind = 1
+    else:
+        outer = _layout("y", y, shape, dtype)
     states = (n, width)
+    _expect("y0", y0, states, torch.float32)
     if yT is None:
-        yT = x.new_empty(states, dtype=torch.float32) if y0 is None else torch.empty_like(y0, memory_format=torch.contiguous_format)
+        yT = x.new_empty(states, dtype=torch.float32) if y0 is None else torch.empty_like(y0)
     else:
         _expect("yT", yT, states, torch.float32)
-    _expect("y0", y0, states, torch.float32)
     _expect("lengths", lengths, (n,), torch.int32)
-    _run(lib.mpode_recurrence_forward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, 1 if new and lengths is not None else 0, *inner, *outer), (x, gate, y0, lengths, y, yT),
-         (_ptr(x), _ptr(gate), _ptr(y0), _ptr(lengths), _ptr(y), _ptr(yT)))
+    _run(lib.mpode_recurrence_forward, RecurrenceDesc(low, n, steps, width, 1 if coupled else 0, zero_behind, *inner, *outer),
+         (x, gate, y0, lengths, y, yT), (x.data_ptr(), gate.data_ptr(), _ptr(y0), _ptr(lengths), y.data_ptr(), yT.data_ptr()))
     return y, yT
 
 
