@@ -14,6 +14,7 @@
 // a million steps (b = 1e-6) decay at the right rate, where a rounded a = 1 - b would not, and b = 1 forgets everything, exactly.  For the same reason a
 // composed map is kept as y -> y - C y + u with C = 1 - A.
 #include <stdarg.h>
+#include <stddef.h>
 #include <stdio.h>
 
 #include <math.h>
@@ -40,6 +41,7 @@ struct RecArgs {
     unsigned* flag;
     long long in_seq, in_step, out_seq, out_step;
     int n_seq, n_steps, width;
+    int stages;                        // STAGED, PIPED: rounds in shared memory
     int zero_behind;                   // what lies behind a sequence's length is set to zero
     int time_major;                    // STAGED: the maps' coordinates are (channel, sequence, step) instead of (channel, step, sequence)
 };
@@ -182,9 +184,10 @@ constexpr int kMaxWarps = 8, kMaxCluster = 16;
 // barrier of its warps, which have then read those of round k - 1.
 template <int V> struct __align__(16) Exchange {
     float warp[2][kMaxWarps][3][32 * V];
-    float block[2][kMaxCluster][3][32 * V];
     unsigned long long bytes[2];                // counts the bytes of a set's block maps
+    float block[2][kMaxCluster][3][32 * V];     // (not there where the kernel is launched without clusters)
 };
+template <int V> constexpr size_t kBlockExchange = offsetof(Exchange<V>, block);
 // The same with a warp that scans: also the states in front of the warps' steps, and barriers that count the warps' maps and the states.  A warp writes its
 // map of round k + 2 behind its second half of round k, for which the maps of round k had been read; states of round k + 2 are written when all maps of
 // it are there, behind the reads of round k's.
@@ -479,12 +482,12 @@ template <typename T> __device__ __forceinline__ void touch_row(const char* p, i
 }
 
 // Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
-//   STAGED, PIPED: brought to shared memory two rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
+//   STAGED, PIPED: brought to shared memory two or three rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
 //           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
 //   else:   loaded into registers when the round starts, from the cache, for which a lane has asked for one row of the round a round ahead.
 template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
-__host__ __device__ constexpr int stages(int access) { return access == PIPED ? 3 : access == STAGED ? 2 : 0; }
-template <typename T, int V, int L, int N, int ACCESS> constexpr int kWarpBytes = stages(ACCESS) * N * L * kRowBytes<T, V>;
+constexpr int kMaxStages = 3;
+template <typename T, int V, int L, int N> constexpr int kStageBytes = N * L * kRowBytes<T, V>;      // of a warp
 template <typename T, int V, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS)> struct Tile {
     using word = typename Word<T, V>::type;
     word w[N][L];
@@ -501,14 +504,15 @@ template <typename T, int V, int L, int N, int ACCESS, bool SHARED = staged_rows
 };
 template <typename T, int V, int L, int N, int ACCESS> struct Tile<T, V, L, N, ACCESS, true> {
     using word = typename Word<T, V>::type;
-    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow, kStages = stages(ACCESS);
-    unsigned at, lane, bar;
-    __device__ __forceinline__ void bind(char* smem, unsigned long long* bars, int l) {
-        at = smem_of(smem) + threadIdx.y * kWarpBytes<T, V, L, N, ACCESS>;
-        bar = smem_of(bars) + threadIdx.y * (kStages * 8);
+    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow;
+    unsigned at, lane, bar, next = 0, parity = 0, count;
+    __device__ __forceinline__ void bind(char* smem, unsigned long long* bars, int l, int stages) {
+        count = stages;
+        at = smem_of(smem) + threadIdx.y * stages * kStageBytes<T, V, L, N>;
+        bar = smem_of(bars) + threadIdx.y * (kMaxStages * 8);
         lane = at + l * (unsigned)sizeof(word);
         if (threadIdx.x == 0) {
-            sets_begin(bars + threadIdx.y * kStages, kStages);
+            sets_begin(bars + threadIdx.y * kMaxStages, stages);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
@@ -525,7 +529,13 @@ template <typename T, int V, int L, int N, int ACCESS> struct Tile<T, V, L, N, A
                                "r"(time_major ? seq : t), "r"(time_major ? t : seq) : "memory");
             }
     }
-    __device__ __forceinline__ void wait(int stage, unsigned parity, bool& broken) { wait_set(bar + 8 * stage, parity, broken); }
+    // the next round's stage, once it is there
+    __device__ __forceinline__ int wait(bool& broken) {
+        const int stage = next;
+        wait_set(bar + 8 * stage, parity, broken);
+        if (++next == count) { next = 0; parity ^= 1; }
+        return stage;
+    }
     __device__ __forceinline__ word get(int stage, int k, int i) const {
         const unsigned a = lane + (stage * N + k) * kArray + i * kRow;
         if constexpr (sizeof(word) == 8) {
@@ -545,13 +555,12 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     using W = Word<T, V>;
     constexpr int kArrays = 2;
     extern __shared__ __align__(128) char staged[];
-    constexpr int kStages = stages(ACCESS);
-    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kStages : 1];
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kMaxStages : 1];
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
     using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
-    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * kWarpBytes<T, V, L, kArrays, ACCESS>);
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, V, L, kArrays>);
     const Place q = place<ACCESS>(p, blocks, warps);
     if (!alone) exchange_begin(ex, warps, blocks);
     const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
@@ -603,19 +612,21 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         }
     };
     if constexpr (staged_rows(ACCESS)) {
-        tile.bind(staged, arrived, q.lane);
-        for (int k = 0; k < kStages; ++k) request(k * stride, k);
+        tile.bind(staged, arrived, q.lane, p.stages);
+        for (int k = 0; k < p.stages; ++k) request(k * stride, k);
     } else tile.apart = apart;
     if (blocks > 1) cluster_wait();
     // A round's two halves: gates and the map of this warp's steps, published; then the steps again from the state in front of them
-    struct Turn { float nb[L][V]; Affine<V> before; unsigned base, round; };
+    struct Turn { float nb[L][V]; Affine<V> before; unsigned base, round; int stage; };
     auto whole = [&](unsigned base) { return base + stride <= (unsigned)q.len; };
     auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
         r.base = base;
         r.round = round;
-        const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0, n = count(base);
-        if constexpr (staged_rows(ACCESS)) tile.wait(stage, (round / kStages) & 1, broken);
+        const int n = count(base);
+        int stage = 0;
+        if constexpr (staged_rows(ACCESS)) stage = tile.wait(broken);
         else load(base);
+        r.stage = stage;
         auto run = [&](auto full) {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
@@ -647,7 +658,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     };
     auto second = [&](auto kind, const Turn& r) {
         float start[V];
-        const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0, n = count(r.base);
+        const int stage = r.stage, n = count(r.base);
         if constexpr (kScan) collect(ex, r.round, start, broken);
         else if (!alone) collect(ex, r.round, r.before, carry, start, blocks, q.rank, broken);
         else {
@@ -676,7 +687,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         }
         if constexpr (staged_rows(ACCESS)) {
             __syncwarp();                                   // all lanes have read this stage
-            request(r.base + kStages * stride, stage);
+            request(r.base + p.stages * stride, stage);
         }
     };
     rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, whole, first, second);
@@ -732,13 +743,12 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     constexpr int kArrays = COUPLED ? 4 : 3;
     using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
-    constexpr int kStages = stages(ACCESS);
-    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kStages : 1];
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kMaxStages : 1];
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
     using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
-    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * kWarpBytes<T, V, L, kArrays, ACCESS>);
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, V, L, kArrays>);
     const Place q = place<ACCESS>(p, blocks, warps);
     if (!alone) exchange_begin(ex, warps, blocks);
     const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
@@ -805,23 +815,23 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         }
     };
     if constexpr (staged_rows(ACCESS)) {
-        tile.bind(staged, arrived, q.lane);
-        for (int k = 0; k < kStages; ++k) request(base + k * stride, k);
+        tile.bind(staged, arrived, q.lane, p.stages);
+        for (int k = 0; k < p.stages; ++k) request(base + k * stride, k);
     } else tile.apart = apart;
     auto get = [&](int stage, int k, int i) { return tile.get(stage, k, staged_rows(ACCESS) ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
     const bool no_dy = p.dy == nullptr;
-    struct Turn { float nb[L][V], slope[L][V]; Affine<V> before; unsigned base, round; };
+    struct Turn { float nb[L][V], slope[L][V]; Affine<V> before; unsigned base, round; int stage; };
     // every step of the round exists, and none is time 0
     auto whole = [&](unsigned base) { return base >= skipped && base + stride < (unsigned)p.n_steps; };
     auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
         r.base = base;
         r.round = round;
-        const int stage = staged_rows(ACCESS) ? round % (kStages + !kStages) : 0;
-        int lo, hi;
+        int stage = 0, lo, hi;
         range(base, lo, hi);
-        if constexpr (staged_rows(ACCESS)) tile.wait(stage, (round / kStages) & 1, broken);
+        if constexpr (staged_rows(ACCESS)) stage = tile.wait(broken);
         else load(base);
+        r.stage = stage;
         auto run = [&](auto full) {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
@@ -854,7 +864,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     };
     auto second = [&](auto kind, const Turn& r) {
         float start[V];
-        const int stage = staged_rows(ACCESS) ? r.round % (kStages + !kStages) : 0;
+        const int stage = r.stage;
         int lo, hi;
         range(r.base, lo, hi);
         const int zero = (int)(p.n_steps - 1 - (r.base + q.slot * L));                          // index of time 0
@@ -907,7 +917,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         dx -= in_round; dg -= in_round;
         if constexpr (staged_rows(ACCESS)) {
             __syncwarp();
-            request(r.base + kStages * stride, stage);
+            request(r.base + p.stages * stride, stage);
         }
     };
     rounds<ACCESS == PIPED, Turn>(base, stride, (unsigned)p.n_steps, whole, first, second);
@@ -1009,7 +1019,7 @@ int cluster_room(int blocks) {
     if (n > 0) return n - 1;
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
-    const size_t smem = kMaxWarps * kWarpBytes<T, 2, L, 2, PIPED> + sizeof(Scan<2>);
+    const size_t smem = kMaxWarps * kMaxStages * kStageBytes<T, 2, L, 2> + sizeof(Scan<2>);
     n = clusters_at_once((const void*)recurrence_forward_kernel<T, 2, true, L, PIPED>, dim3(32, kMaxWarps + 1), smem, blocks);
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
@@ -1024,9 +1034,12 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
     }
     const Shape s = shape_of(d, a, L, cluster_room);
     RecMaps maps;
+    // Three rounds in shared memory, or two where two blocks of 8 warps share an SM (us with 2 / 3: backward of 8 x 4096 x 2048 bfloat16, 256 tiles, 143 / 152;
+    // 8 x 2048 x 1024 float32, 128 tiles, 87 / 80; 128 x 128 x 2048, 2 warps a block, 96 / 82)
     const auto go = [&](auto access) {
         constexpr int A = access.value;
-        const size_t smem = s.warps * kWarpBytes<T, 2, L, N, A> + (A == PIPED ? sizeof(Scan<2>) : sizeof(Exchange<2>));
+        a.stages = A == PIPED || s.warps < kMaxWarps || s.tiles <= sm_count() ? 3 : 2;
+        const size_t smem = (staged_rows(A) ? s.warps * a.stages * kStageBytes<T, 2, L, N> : 0) + (A == PIPED ? sizeof(Scan<2>) : s.blocks > 1 ? sizeof(Exchange<2>) : kBlockExchange<2>);
         if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
         else return launch(recurrence_forward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
     };
