@@ -48,51 +48,45 @@ struct RecArgs {
 // STAGED: tensor maps of gate and x (forward), of gate, dL/dy, y and x (backward)
 struct RecMaps { CUtensorMap m[4]; };
 
-// Two channels of a row: a pair of 16-bit values in 32 bits, or of float32.  V = 2 throughout.
-template <typename T, int V> struct Word;
-template <> struct Word<float, 2> {
-    using type = float2;
-    static __device__ __forceinline__ void get(type w, float (&f)[2]) { f[0] = w.x; f[1] = w.y; }
-    static __device__ __forceinline__ type put(const float (&f)[2]) { return make_float2(f[0], f[1]); }
-    static __device__ __forceinline__ type negate(type w) { return make_float2(-w.x, -w.y); }
-};
-template <typename T> struct Word<T, 2> {
+constexpr int V = 2;                   // channels of a lane
+// Two channels of a row: a pair of 16-bit values in 32 bits, or of float32
+template <typename T> struct Word {
     using type = uint32_t;
     static __device__ __forceinline__ void get(type w, float (&f)[2]) { const float2 t = Pair<T>::get(w); f[0] = t.x; f[1] = t.y; }
     static __device__ __forceinline__ type put(const float (&f)[2]) { return Pair<T>::put(f[0], f[1]); }
     static __device__ __forceinline__ type negate(type w) { return w ^ 0x80008000u; }
 };
-template <typename T, int V> __device__ __forceinline__ void see(Largest<T>& m, const typename Word<T, V>::type& w) {
+template <> struct Word<float> {
+    using type = float2;
+    static __device__ __forceinline__ void get(type w, float (&f)[2]) { f[0] = w.x; f[1] = w.y; }
+    static __device__ __forceinline__ type put(const float (&f)[2]) { return make_float2(f[0], f[1]); }
+    static __device__ __forceinline__ type negate(type w) { return make_float2(-w.x, -w.y); }
+};
+template <typename T> __device__ __forceinline__ void see(Largest<T>& m, const typename Word<T>::type& w) {
     if constexpr (sizeof(T) == 2) m.see(w);
     else { m.see(__float_as_uint(w.x)); m.see(__float_as_uint(w.y)); }
 }
 
-// a b + c, a + b and a b on all channels of a lane; two of them are one instruction
-template <int V> struct Ops {
+// a b + c, a + b and a b on a lane's channels, one instruction each
+struct Ops {
     static __device__ __forceinline__ void fma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
-        if constexpr (V == 2) {
-            const float2 r = __ffma2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]), make_float2(c[0], c[1]));
-            d[0] = r.x; d[1] = r.y;
-        } else d[0] = fmaf(a[0], b[0], c[0]);
+        const float2 r = __ffma2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]), make_float2(c[0], c[1]));
+        d[0] = r.x; d[1] = r.y;
     }
     static __device__ __forceinline__ void add(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
-        if constexpr (V == 2) {
-            const float2 r = __fadd2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
-            d[0] = r.x; d[1] = r.y;
-        } else d[0] = a[0] + b[0];
+        const float2 r = __fadd2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+        d[0] = r.x; d[1] = r.y;
     }
     static __device__ __forceinline__ void mul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
-        if constexpr (V == 2) {
-            const float2 r = __fmul2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
-            d[0] = r.x; d[1] = r.y;
-        } else d[0] = a[0] * b[0];
+        const float2 r = __fmul2_rn(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+        d[0] = r.x; d[1] = r.y;
     }
 };
 
 // -sigmoid(g) = -b, and the slope b (1 - b), which is e b^2 with e = exp(-g).  16-bit gates: the device's approximate power and quotient (2^-22
 // relative, and the argument's rounding adds |g| 2^-24), which cost 3 instructions a channel where the accurate ones of float32 cost 15; for the slope
 // the exponent is kept below 2^126, so that e b^2 is finite: b is 1e-38 instead of less, which no float32 state feels.
-template <typename T, int V, bool SLOPE> __device__ __forceinline__ void negated_gate(const float (&g)[V], float (&nb)[V], float (&slope)[V]) {
+template <typename T, bool SLOPE> __device__ __forceinline__ void negated_gate(const float (&g)[V], float (&nb)[V], float (&slope)[V]) {
     float e[V];
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -106,33 +100,33 @@ template <typename T, int V, bool SLOPE> __device__ __forceinline__ void negated
         float k[V], d[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) k[v] = -1.4426950408889634f;
-        Ops<V>::mul(e, g, k);
+        Ops::mul(e, g, k);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (SLOPE) asm("min.NaN.f32 %0, %0, %1;" : "+f"(e[v]) : "f"(126.f));
             asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[v]));
             k[v] = -1.f;
         }
-        Ops<V>::fma(d, e, k, k);
+        Ops::fma(d, e, k, k);
 #pragma unroll
         for (int v = 0; v < V; ++v) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb[v]) : "f"(d[v]));
         if (SLOPE) {
-            Ops<V>::mul(slope, nb, nb);
-            Ops<V>::mul(slope, slope, e);
+            Ops::mul(slope, nb, nb);
+            Ops::mul(slope, slope, e);
         }
     }
 }
 
 // One step of the state s, nb = -b.  The coupled forward pass runs on s = -y, where b x is taken away without a change of sign: s - b s - b x.
-template <bool COUPLED, int V> __device__ __forceinline__ void step_forward(float (&s)[V], const float (&nb)[V], const float (&x)[V]) {
+template <bool COUPLED> __device__ __forceinline__ void step_forward(float (&s)[V], const float (&nb)[V], const float (&x)[V]) {
     float kept[V];
-    Ops<V>::fma(kept, nb, s, s);
-    if constexpr (COUPLED) Ops<V>::fma(s, nb, x, kept);
-    else Ops<V>::add(s, kept, x);
+    Ops::fma(kept, nb, s, s);
+    if constexpr (COUPLED) Ops::fma(s, nb, x, kept);
+    else Ops::add(s, kept, x);
 }
 // The composed map s -> A s + u of some steps, C = 1 - A: A exact to its last bits where it is small (a reset leaves A = 0), C where the steps
 // forget little.  Kept per lane as A, -C and u.
-template <int V> struct Map {
+struct Map {
     float A[V], nC[V], u[V];
     __device__ __forceinline__ Map() {
 #pragma unroll
@@ -142,15 +136,15 @@ template <int V> struct Map {
         float one[V], left[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) one[v] = 1.f;
-        Ops<V>::fma(A, nb, A, A);
-        Ops<V>::add(left, one, nC);
-        Ops<V>::fma(nC, nb, left, nC);
+        Ops::fma(A, nb, A, A);
+        Ops::add(left, one, nC);
+        Ops::fma(nC, nb, left, nC);
     }
 };
 // As the warps and blocks exchange it: s -> m s + (k s + u), with (m, k) = (A, 0) or (-C, 1), whichever is the smaller one
-template <int V> struct Affine {
+struct Affine {
     float m[V], k[V], u[V];
-    __device__ __forceinline__ void from(const Map<V>& p) {
+    __device__ __forceinline__ void from(const Map& p) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const bool fast = p.A[v] < 0.5f;
@@ -159,19 +153,19 @@ template <int V> struct Affine {
     }
     __device__ __forceinline__ void apply(float (&s)[V]) const {
         float t[V];
-        Ops<V>::fma(t, k, s, u);
-        Ops<V>::fma(s, m, s, t);
+        Ops::fma(t, k, s, u);
+        Ops::fma(s, m, s, t);
     }
     // p, then this map
-    __device__ __forceinline__ void follow(Map<V>& p) const {
+    __device__ __forceinline__ void follow(Map& p) const {
         float t[V], one[V], k1[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) { one[v] = 1.f; k1[v] = k[v] - 1.f; }
-        Ops<V>::mul(t, k, p.A);
-        Ops<V>::fma(p.A, m, p.A, t);
-        Ops<V>::add(t, one, p.nC);
-        Ops<V>::fma(p.nC, k, p.nC, k1);              // -C - c (1 - C) with c = -m, or 1 - m: -1 + m (1 - C)
-        Ops<V>::fma(p.nC, m, t, p.nC);
+        Ops::mul(t, k, p.A);
+        Ops::fma(p.A, m, p.A, t);
+        Ops::add(t, one, p.nC);
+        Ops::fma(p.nC, k, p.nC, k1);              // -C - c (1 - C) with c = -m, or 1 - m: -1 + m (1 - C)
+        Ops::fma(p.nC, m, t, p.nC);
         apply(p.u);
     }
 };
@@ -182,50 +176,43 @@ constexpr int kMaxWarps = 8, kMaxCluster = 16;
 // blocks that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
 // A set is written again two rounds later: a block sends its map of round k + 1 when it has those of round k from all blocks, and each of them sends behind a
 // barrier of its warps, which have then read those of round k - 1.
-template <int V> struct __align__(16) Exchange {
+struct __align__(16) Exchange {
     float warp[2][kMaxWarps][3][32 * V];
     unsigned long long bytes[2];                // counts the bytes of a set's block maps
     float block[2][kMaxCluster][3][32 * V];     // (not there where the kernel is launched without clusters)
 };
-template <int V> constexpr size_t kBlockExchange = offsetof(Exchange<V>, block);
+constexpr size_t kBlockExchange = offsetof(Exchange, block);
 // The same with a warp that scans: also the states in front of the warps' steps, and barriers that count the warps' maps and the states.  A warp writes its
 // map of round k + 2 behind its second half of round k, for which the maps of round k had been read; states of round k + 2 are written when all maps of
 // it are there, behind the reads of round k's.
-template <int V> struct __align__(16) Scan {
+struct __align__(16) Scan {
     float warp[2][kMaxWarps][3][32 * V];
     float block[2][kMaxCluster][3][32 * V];
     float start[2][kMaxWarps][32 * V];
     unsigned long long maps[2], bytes[2], starts[2];
 };
-template <int V> __device__ __forceinline__ void lds(float (&f)[V], const float* p) {
-    if constexpr (V == 2) {
-        const float2 t = *reinterpret_cast<const float2*>(p);
-        f[0] = t.x; f[1] = t.y;
-    } else f[0] = *p;
+__device__ __forceinline__ void lds(float (&f)[V], const float* p) {
+    const float2 t = *reinterpret_cast<const float2*>(p);
+    f[0] = t.x; f[1] = t.y;
 }
-template <int V> __device__ __forceinline__ void sts(float* p, const float (&f)[V]) {
-    if constexpr (V == 2) *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
-    else *p = f[0];
+__device__ __forceinline__ void sts(float* p, const float (&f)[V]) {
+    *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
 }
-template <int V> __device__ __forceinline__ void fetch(Affine<V>& a, const float (&t)[3][32 * V]) {
-    lds<V>(a.m, &t[0][threadIdx.x * V]); lds<V>(a.k, &t[1][threadIdx.x * V]); lds<V>(a.u, &t[2][threadIdx.x * V]);
+__device__ __forceinline__ void fetch(Affine& a, const float (&t)[3][32 * V]) {
+    lds(a.m, &t[0][threadIdx.x * V]); lds(a.k, &t[1][threadIdx.x * V]); lds(a.u, &t[2][threadIdx.x * V]);
 }
-template <int V> __device__ __forceinline__ void put(float (&t)[3][32 * V], const Affine<V>& a) {
-    sts<V>(&t[0][threadIdx.x * V], a.m); sts<V>(&t[1][threadIdx.x * V], a.k); sts<V>(&t[2][threadIdx.x * V], a.u);
-}
-template <int V> __device__ __forceinline__ void send_all(unsigned at, const float (&f)[V], unsigned bar) {
-    if constexpr (V == 2) send(at, f[0], f[1], bar);
-    else send(at, f[0], bar);
+__device__ __forceinline__ void put(float (&t)[3][32 * V], const Affine& a) {
+    sts(&t[0][threadIdx.x * V], a.m); sts(&t[1][threadIdx.x * V], a.k); sts(&t[2][threadIdx.x * V], a.u);
 }
 
-template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex, int warps, int blocks) {
-    Affine<V> id;
+__device__ __forceinline__ void exchange_begin(Exchange& ex, int warps, int blocks) {
+    Affine id;
 #pragma unroll
     for (int v = 0; v < V; ++v) { id.m[v] = id.u[v] = 0.f; id.k[v] = 1.f; }
     for (int set = 0; set < 2; ++set) {
-        for (int w = warps + threadIdx.y; w < kMaxWarps; w += warps) put<V>(ex.warp[set][w], id);
+        for (int w = warps + threadIdx.y; w < kMaxWarps; w += warps) put(ex.warp[set][w], id);
         if (blocks > 1)
-            for (int r = blocks + threadIdx.y; r < kMaxCluster; r += warps) put<V>(ex.block[set][r], id);
+            for (int r = blocks + threadIdx.y; r < kMaxCluster; r += warps) put(ex.block[set][r], id);
     }
     if (blocks == 1) return;
     if (threadIdx.x == 0 && threadIdx.y == 0) sets_begin(ex.bytes, 2);
@@ -234,35 +221,35 @@ template <int V> __device__ __forceinline__ void exchange_begin(Exchange<V>& ex,
 // A round's exchange has two halves.  publish: this warp's map to the block, the block's map to every block of the cluster; returns the map of the steps of the
 // block that lie in front of this warp's.  collect: from the state in front of all of the round's steps (`carry`, replaced by the one behind them) the
 // state in front of this warp's.  Called by all threads of the cluster in the same order.
-template <int V> __device__ __forceinline__ void publish(Exchange<V>& ex, unsigned round, const Map<V>& own, Affine<V>& before, int blocks, int rank) {
+__device__ __forceinline__ void publish(Exchange& ex, unsigned round, const Map& own, Affine& before, int blocks, int rank) {
     const int warp = threadIdx.y, set = round & 1;
-    Affine<V> a;
+    Affine a;
     a.from(own);
-    put<V>(ex.warp[round & 1][warp], a);
+    put(ex.warp[round & 1][warp], a);
     __syncthreads();
     if (blocks == 1) return;
     const unsigned bar = smem_of(&ex.bytes[set]);
     if (warp == 0 && threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
-    Map<V> all;
+    Map all;
 #pragma unroll
     for (int w = 0; w < kMaxWarps; ++w) {
         if (w == warp) before.from(all);
-        fetch<V>(a, ex.warp[round & 1][w]);
+        fetch(a, ex.warp[round & 1][w]);
         a.follow(all);
     }
     a.from(all);
     const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]);
     for (int to = warp; to < blocks; to += (int)blockDim.y) {               // a warp to each block
         const unsigned there = peer_of(at, to), count = peer_of(bar, to);
-        send_all<V>(there, a.m, count);
-        send_all<V>(there + 32 * V * 4, a.k, count);
-        send_all<V>(there + 64 * V * 4, a.u, count);
+        send(there, a.m[0], a.m[1], count);
+        send(there + 32 * V * 4, a.k[0], a.k[1], count);
+        send(there + 64 * V * 4, a.u[0], a.u[1], count);
     }
 }
-template <int V> __device__ __forceinline__ void collect(Exchange<V>& ex, unsigned round, const Affine<V>& before, float (&carry)[V], float (&start)[V],
+__device__ __forceinline__ void collect(Exchange& ex, unsigned round, const Affine& before, float (&carry)[V], float (&start)[V],
                                                                    int blocks, int rank, bool& broken) {
     const int warp = threadIdx.y, set = round & 1;
-    Affine<V> a;
+    Affine a;
     if (blocks == 1) {
 #pragma unroll
         for (int w = 0; w < kMaxWarps; ++w) {
@@ -270,7 +257,7 @@ template <int V> __device__ __forceinline__ void collect(Exchange<V>& ex, unsign
 #pragma unroll
                 for (int v = 0; v < V; ++v) start[v] = carry[v];
             }
-            fetch<V>(a, ex.warp[round & 1][w]);
+            fetch(a, ex.warp[round & 1][w]);
             a.apply(carry);
         }
         return;
@@ -287,14 +274,14 @@ template <int V> __device__ __forceinline__ void collect(Exchange<V>& ex, unsign
 #pragma unroll
                 for (int v = 0; v < V; ++v) start[v] = carry[v];
             }
-            fetch<V>(a, ex.block[set][r0 + r]);
+            fetch(a, ex.block[set][r0 + r]);
             a.apply(carry);
         }
     }
     before.apply(start);
 }
 
-template <int V> __device__ __forceinline__ void exchange_begin(Scan<V>& ex, int warps, int) {
+__device__ __forceinline__ void exchange_begin(Scan& ex, int warps, int) {
     if (threadIdx.x == 0 && threadIdx.y == 0) {
         for (int i = 0; i < 2; ++i) {
             bar_init(&ex.maps[i], warps);
@@ -306,61 +293,56 @@ template <int V> __device__ __forceinline__ void exchange_begin(Scan<V>& ex, int
     cluster_arrive();
 }
 // a warp's map of a round, and the state in front of its steps
-template <int V> __device__ __forceinline__ void publish(Scan<V>& ex, unsigned round, const Map<V>& own) {
+__device__ __forceinline__ void publish(Scan& ex, unsigned round, const Map& own) {
     const int set = round & 1;
-    Affine<V> a;
+    Affine a;
     a.from(own);
-    put<V>(ex.warp[set][threadIdx.y], a);
+    put(ex.warp[set][threadIdx.y], a);
     __syncwarp();
     if (threadIdx.x == 0) bar_arrive(smem_of(&ex.maps[set]));
 }
-template <int V> __device__ __forceinline__ void collect(Scan<V>& ex, unsigned round, float (&start)[V], bool& broken) {
+__device__ __forceinline__ void collect(Scan& ex, unsigned round, float (&start)[V], bool& broken) {
     const int set = round & 1;
     wait_set(smem_of(&ex.starts[set]), (round >> 1) & 1, broken);
-    lds<V>(start, &ex.start[set][threadIdx.y][threadIdx.x * V]);
+    lds(start, &ex.start[set][threadIdx.y][threadIdx.x * V]);
     if (broken) {
 #pragma unroll
         for (int v = 0; v < V; ++v) start[v] = __int_as_float(0x7fffffff);
     }
 }
 // The warp between them: `carry` is the state in front of the first round, and then the one behind the last
-template <int V> __device__ __forceinline__ void scan(Scan<V>& ex, unsigned base, unsigned stride, unsigned end, float (&carry)[V], int warps, int blocks, int rank) {
+__device__ __forceinline__ void scan(Scan& ex, unsigned base, unsigned stride, unsigned end, float (&carry)[V], int warps, int blocks, int rank) {
     bool broken = false;
     for (unsigned round = 0; base < end; base += stride, ++round) {
         const int set = round & 1;
         const unsigned parity = (round >> 1) & 1;
-        Affine<V> a;
+        Affine a;
         wait_set(smem_of(&ex.maps[set]), parity, broken);
         float state[V];
-        if (blocks > 1) {
-            Map<V> all;
+        Map all;
 #pragma unroll 4
-            for (int w = 0; w < warps; ++w) {
-                fetch<V>(a, ex.warp[set][w]);
-                a.follow(all);
-            }
-            a.from(all);
-            const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]), bar = smem_of(&ex.bytes[set]);
-            if (threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
-            for (int to = 0; to < blocks; ++to) {
-                const unsigned there = peer_of(at, to), count = peer_of(bar, to);
-                send_all<V>(there, a.m, count);
-                send_all<V>(there + 32 * V * 4, a.k, count);
-                send_all<V>(there + 64 * V * 4, a.u, count);
-            }
-            wait_set(bar, parity, broken);
+        for (int w = 0; w < warps; ++w) {
+            fetch(a, ex.warp[set][w]);
+            a.follow(all);
+        }
+        a.from(all);
+        const unsigned at = smem_of(&ex.block[set][rank][0][threadIdx.x * V]), bar = smem_of(&ex.bytes[set]);
+        if (threadIdx.x == 0) set_expects(bar, blocks * 3 * 32 * V * 4);
+        for (int to = 0; to < blocks; ++to) {
+            const unsigned there = peer_of(at, to), count = peer_of(bar, to);
+            send(there, a.m[0], a.m[1], count);
+            send(there + 32 * V * 4, a.k[0], a.k[1], count);
+            send(there + 64 * V * 4, a.u[0], a.u[1], count);
+        }
+        wait_set(bar, parity, broken);
 #pragma unroll 4
-            for (int r = 0; r < blocks; ++r) {
-                if (r == rank) {
+        for (int r = 0; r < blocks; ++r) {
+            if (r == rank) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) state[v] = carry[v];
-                }
-                fetch<V>(a, ex.block[set][r]);
-                a.apply(carry);
+                for (int v = 0; v < V; ++v) state[v] = carry[v];
             }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) state[v] = carry[v];
+            fetch(a, ex.block[set][r]);
+            a.apply(carry);
         }
         if (broken) {
 #pragma unroll
@@ -368,13 +350,9 @@ template <int V> __device__ __forceinline__ void scan(Scan<V>& ex, unsigned base
         }
 #pragma unroll 4
         for (int w = 0; w < warps; ++w) {
-            sts<V>(&ex.start[set][w][threadIdx.x * V], state);
-            fetch<V>(a, ex.warp[set][w]);
+            sts(&ex.start[set][w][threadIdx.x * V], state);
+            fetch(a, ex.warp[set][w]);
             a.apply(state);
-        }
-        if (blocks == 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = state[v];
         }
         __syncwarp();
         if (threadIdx.x == 0) bar_arrive(smem_of(&ex.starts[set]));
@@ -413,14 +391,14 @@ template <int ACCESS> __device__ __forceinline__ Place place(const RecArgs& p, i
     return q;
 }
 // a lane's two channels of the row at base + off; apart: bytes from one to the other (SINGLES)
-template <typename T, int ACCESS> __device__ __forceinline__ typename Word<T, 2>::type load_pair(const char* base, unsigned off, unsigned apart) {
-    using word = typename Word<T, 2>::type;
+template <typename T, int ACCESS> __device__ __forceinline__ typename Word<T>::type load_pair(const char* base, unsigned off, unsigned apart) {
+    using word = typename Word<T>::type;
     if constexpr (ACCESS != SINGLES) return *(const word*)(base + off);
     else if constexpr (sizeof(T) == 4) return make_float2(*(const float*)(base + off), *(const float*)(base + off + apart));
     else return (uint32_t)*(const uint16_t*)(base + off) | (uint32_t)*(const uint16_t*)(base + off + apart) << 16;
 }
-template <typename T, int ACCESS> __device__ __forceinline__ void store_pair(char* base, unsigned off, unsigned apart, typename Word<T, 2>::type w) {
-    using word = typename Word<T, 2>::type;
+template <typename T, int ACCESS> __device__ __forceinline__ void store_pair(char* base, unsigned off, unsigned apart, typename Word<T>::type w) {
+    using word = typename Word<T>::type;
     if constexpr (ACCESS != SINGLES) *(word*)(base + off) = w;
     else if constexpr (sizeof(T) == 4) {
         *(float*)(base + off) = w.x;
@@ -485,11 +463,11 @@ template <typename T> __device__ __forceinline__ void touch_row(const char* p, i
 //   STAGED, PIPED: brought to shared memory two or three rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
 //           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
 //   else:   loaded into registers when the round starts, from the cache, for which a lane has asked for one row of the round a round ahead.
-template <typename T, int V> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
+template <typename T> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 constexpr int kMaxStages = 3;
-template <typename T, int V, int L, int N> constexpr int kStageBytes = N * L * kRowBytes<T, V>;      // of a warp
-template <typename T, int V, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS)> struct Tile {
-    using word = typename Word<T, V>::type;
+template <typename T, int L, int N> constexpr int kStageBytes = N * L * kRowBytes<T>;      // of a warp
+template <typename T, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS)> struct Tile {
+    using word = typename Word<T>::type;
     word w[N][L];
     unsigned apart;
     // step i of array k lies at base + off + i * step bytes; steps lo .. hi - 1 exist
@@ -502,13 +480,13 @@ template <typename T, int V, int L, int N, int ACCESS, bool SHARED = staged_rows
     }
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
 };
-template <typename T, int V, int L, int N, int ACCESS> struct Tile<T, V, L, N, ACCESS, true> {
-    using word = typename Word<T, V>::type;
-    static constexpr int kRow = kRowBytes<T, V>, kArray = L * kRow;
+template <typename T, int L, int N, int ACCESS> struct Tile<T, L, N, ACCESS, true> {
+    using word = typename Word<T>::type;
+    static constexpr int kRow = kRowBytes<T>, kArray = L * kRow;
     unsigned at, lane, bar, next = 0, parity = 0, count;
     __device__ __forceinline__ void bind(char* smem, unsigned long long* bars, int l, int stages) {
         count = stages;
-        at = smem_of(smem) + threadIdx.y * stages * kStageBytes<T, V, L, N>;
+        at = smem_of(smem) + threadIdx.y * stages * kStageBytes<T, L, N>;
         bar = smem_of(bars) + threadIdx.y * (kMaxStages * 8);
         lane = at + l * (unsigned)sizeof(word);
         if (threadIdx.x == 0) {
@@ -550,17 +528,17 @@ template <typename T, int V, int L, int N, int ACCESS> struct Tile<T, V, L, N, A
     }
 };
 
-template <typename T, int V, bool COUPLED, int L, int ACCESS>
+template <typename T, bool COUPLED, int L, int ACCESS>
 __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
-    using W = Word<T, V>;
+    using W = Word<T>;
     constexpr int kArrays = 2;
     extern __shared__ __align__(128) char staged[];
     __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kMaxStages : 1];
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
-    using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
-    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, V, L, kArrays>);
+    using Shared = std::conditional_t<kScan, Scan, Exchange>;
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, L, kArrays>);
     const Place q = place<ACCESS>(p, blocks, warps);
     if (!alone) exchange_begin(ex, warps, blocks);
     const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
@@ -590,7 +568,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         cluster_wait();
         return;
     }
-    Tile<T, V, L, kArrays, ACCESS> tile;
+    Tile<T, L, kArrays, ACCESS> tile;
     // steps of this warp's tile that exist
     auto count = [&](unsigned base) {
         const unsigned t0 = base + q.slot * L;
@@ -617,7 +595,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     } else tile.apart = apart;
     if (blocks > 1) cluster_wait();
     // A round's two halves: gates and the map of this warp's steps, published; then the steps again from the state in front of them
-    struct Turn { float nb[L][V]; Affine<V> before; unsigned base, round; int stage; };
+    struct Turn { float nb[L][V]; Affine before; unsigned base, round; int stage; };
     auto whole = [&](unsigned base) { return base + stride <= (unsigned)q.len; };
     auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
         r.base = base;
@@ -632,14 +610,14 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             for (int i = 0; i < L; ++i) {
                 float f[V], none[V];
                 W::get(tile.get(stage, 0, i), f);
-                negated_gate<T, V, false>(f, r.nb[i], none);
+                negated_gate<T, false>(f, r.nb[i], none);
                 if (!full.value && i >= n) {                // a step that does not exist keeps the state
 #pragma unroll
                     for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
                 }
             }
             if (alone) return;
-            Map<V> own;
+            Map own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float xs[V];
@@ -649,7 +627,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
                     for (int v = 0; v < V; ++v) xs[v] = 0.f;
                 }
                 own.decay(r.nb[i]);
-                step_forward<COUPLED, V>(own.u, r.nb[i], xs);
+                step_forward<COUPLED>(own.u, r.nb[i], xs);
             }
             if constexpr (kScan) publish(ex, round, own);
             else publish(ex, round, own, r.before, blocks, q.rank);
@@ -675,7 +653,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
 #pragma unroll
                     for (int v = 0; v < V; ++v) xs[v] = 0.f;
                 }
-                step_forward<COUPLED, V>(start, r.nb[i], xs);
+                step_forward<COUPLED>(start, r.nb[i], xs);
                 if (full.value || i < n) store_pair<T, ACCESS>(out, at, apart, COUPLED ? W::negate(W::put(start)) : W::put(start));
             }
         };
@@ -705,7 +683,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
 // little more than its launch (100 sequences of 1024 channels, one step: 4 us less than the kernel above)
 constexpr int kFewSteps = 4;
 template <typename T, bool COUPLED, int ACCESS> __global__ void __launch_bounds__(128) recurrence_steps_kernel(const RecArgs p) {
-    using W = Word<T, 2>;
+    using W = Word<T>;
     const int pairs = (p.width + 1) / 2;
     const long long i = (long long)blockIdx.x * 128 + threadIdx.x;
     const int seq = (int)(i / pairs);
@@ -723,8 +701,8 @@ template <typename T, bool COUPLED, int ACCESS> __global__ void __launch_bounds_
         float xs[2], f[2], nb[2], none[2];
         W::get(load_pair<T, ACCESS>(x + t * p.in_step * es, 0, apart), xs);
         W::get(load_pair<T, ACCESS>(g + t * p.in_step * es, 0, apart), f);
-        negated_gate<T, 2, false>(f, nb, none);
-        step_forward<COUPLED, 2>(s, nb, xs);
+        negated_gate<T, false>(f, nb, none);
+        step_forward<COUPLED>(s, nb, xs);
         store_pair<T, ACCESS>(out + t * p.out_step * es, 0, apart, COUPLED ? W::negate(W::put(s)) : W::put(s));
     }
     if (p.zero_behind)
@@ -737,9 +715,9 @@ template <typename T, bool COUPLED, int ACCESS> __global__ void __launch_bounds_
 
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
 // Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
-template <typename T, int V, bool COUPLED, int L, int ACCESS>
+template <typename T, bool COUPLED, int L, int ACCESS>
 __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
-    using W = Word<T, V>;
+    using W = Word<T>;
     constexpr int kArrays = COUPLED ? 4 : 3;
     using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
@@ -747,8 +725,8 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
-    using Shared = std::conditional_t<kScan, Scan<V>, Exchange<V>>;
-    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, V, L, kArrays>);
+    using Shared = std::conditional_t<kScan, Scan, Exchange>;
+    Shared& ex = *reinterpret_cast<Shared*>(staged + warps * (staged_rows(ACCESS) ? p.stages : 0) * kStageBytes<T, L, kArrays>);
     const Place q = place<ACCESS>(p, blocks, warps);
     if (!alone) exchange_begin(ex, warps, blocks);
     const unsigned stride = blocks * warps * L, es = sizeof(T), apart = (q.col[1] - q.col[0]) * es;
@@ -780,7 +758,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
         cluster_wait();
         return;
     }
-    Tile<T, V, L, kArrays, ACCESS> tile;
+    Tile<T, L, kArrays, ACCESS> tile;
     // the tile's steps lo .. hi - 1 exist
     auto range = [&](unsigned base, int& lo, int& hi) {
         const unsigned first = base + q.slot * L;
@@ -821,7 +799,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     auto get = [&](int stage, int k, int i) { return tile.get(stage, k, staged_rows(ACCESS) ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
     const bool no_dy = p.dy == nullptr;
-    struct Turn { float nb[L][V], slope[L][V]; Affine<V> before; unsigned base, round; int stage; };
+    struct Turn { float nb[L][V], slope[L][V]; Affine before; unsigned base, round; int stage; };
     // every step of the round exists, and none is time 0
     auto whole = [&](unsigned base) { return base >= skipped && base + stride < (unsigned)p.n_steps; };
     auto first = [&](auto kind, Turn& r, unsigned base, unsigned round) {
@@ -837,14 +815,14 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             for (int i = 0; i < L; ++i) {
                 float f[V];
                 W::get(get(stage, 0, i), f);
-                negated_gate<T, V, true>(f, r.nb[i], r.slope[i]);
+                negated_gate<T, true>(f, r.nb[i], r.slope[i]);
                 if (!full.value && (i < lo || i >= hi)) {                                       // a step that does not exist keeps the adjoint
 #pragma unroll
                     for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
                 }
             }
             if (alone) return;
-            Map<V> own;
+            Map own;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float d[V], l[V];
@@ -854,8 +832,8 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
                     for (int v = 0; v < V; ++v) d[v] = 0.f;
                 }
                 own.decay(r.nb[i]);
-                Ops<V>::add(l, own.u, d);
-                Ops<V>::fma(own.u, r.nb[i], l, l);
+                Ops::add(l, own.u, d);
+                Ops::fma(own.u, r.nb[i], l, l);
             }
             if constexpr (kScan) publish(ex, round, own);
             else publish(ex, round, own, r.before, blocks, q.rank);
@@ -889,21 +867,21 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
 #pragma unroll
                     for (int v = 0; v < V; ++v) ys[v] = p.y0 != nullptr ? p.y0[states + q.col[v]] : 0.f;
                 }
-                Ops<V>::add(l, start, d);
-                Ops<V>::fma(start, r.nb[i], l, l);
-                Ops<V>::mul(gg, r.slope[i], l);
+                Ops::add(l, start, d);
+                Ops::fma(start, r.nb[i], l, l);
+                Ops::mul(gg, r.slope[i], l);
                 if constexpr (COUPLED) {
                     float xs[V], minus[V];
                     W::get(get(stage, 3, i), xs);
-                    Ops<V>::mul(gx, r.nb[i], l);
+                    Ops::mul(gx, r.nb[i], l);
 #pragma unroll
                     for (int v = 0; v < V; ++v) minus[v] = -1.f;
-                    Ops<V>::fma(ys, ys, minus, xs);
+                    Ops::fma(ys, ys, minus, xs);
                 }
-                Ops<V>::mul(gg, gg, ys);
+                Ops::mul(gg, gg, ys);
                 if (full.value || (i >= lo && i < hi)) {
                     const word wx = COUPLED ? W::negate(W::put(gx)) : W::put(l), wg = COUPLED ? W::put(gg) : W::negate(W::put(gg));
-                    if (p.flag != nullptr) { see<T, V>(largest, wx); see<T, V>(largest, wg); }
+                    if (p.flag != nullptr) { see<T>(largest, wx); see<T>(largest, wg); }
                     store_pair<T, ACCESS>(dx, at, apart, wx);
                     store_pair<T, ACCESS>(dg, at, apart, wg);
                 }
@@ -1019,8 +997,8 @@ int cluster_room(int blocks) {
     if (n > 0) return n - 1;
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
-    const size_t smem = kMaxWarps * kMaxStages * kStageBytes<T, 2, L, 2> + sizeof(Scan<2>);
-    n = clusters_at_once((const void*)recurrence_forward_kernel<T, 2, true, L, PIPED>, dim3(32, kMaxWarps + 1), smem, blocks);
+    const size_t smem = kMaxWarps * kMaxStages * kStageBytes<T, L, 2> + sizeof(Scan);
+    n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kMaxWarps + 1), smem, blocks);
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }
@@ -1039,9 +1017,9 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
     const auto go = [&](auto access) {
         constexpr int A = access.value;
         a.stages = A == PIPED || s.warps < kMaxWarps || s.tiles <= sm_count() ? 3 : 2;
-        const size_t smem = (staged_rows(A) ? s.warps * a.stages * kStageBytes<T, 2, L, N> : 0) + (A == PIPED ? sizeof(Scan<2>) : s.blocks > 1 ? sizeof(Exchange<2>) : kBlockExchange<2>);
-        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
-        else return launch(recurrence_forward_kernel<T, 2, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
+        const size_t smem = (staged_rows(A) ? s.warps * a.stages * kStageBytes<T, L, N> : 0) + (A == PIPED ? sizeof(Scan) : s.blocks > 1 ? sizeof(Exchange) : kBlockExchange);
+        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
+        else return launch(recurrence_forward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
     };
     if (d.n_steps > 2 * s.warps * s.blocks * L && words_fit(d, a) && pieces_fit(d, a)) {
         a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;

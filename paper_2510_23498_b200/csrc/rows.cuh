@@ -26,11 +26,6 @@ template <> struct Pair<__half> {
 
 struct Oct {
     float2 v[4];
-    __device__ __forceinline__ float get(int i) const { return i & 1 ? v[i >> 1].y : v[i >> 1].x; }
-    __device__ __forceinline__ float sum() const {
-        const float2 s = __fadd2_rn(__fadd2_rn(v[0], v[1]), __fadd2_rn(v[2], v[3]));
-        return s.x + s.y;
-    }
     __device__ __forceinline__ void fill(float f) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = make_float2(f, f);
@@ -95,11 +90,6 @@ template <typename T, bool VEC> __device__ __forceinline__ void store_raw(T* p, 
         for (int i = 0; i < 8; ++i)
             if (i < n) h[i] = (uint16_t)(r.w[i / 2] >> (16 * (i & 1)));
     }
-}
-template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int n, const Oct& o) {
-    Raw8<T> r;
-    pack<T>(o, r);
-    store_raw<T, VEC>(p, n, r);
 }
 
 // Four neighbouring elements (a half of the above): as pairs of float32, and their accesses
