@@ -938,16 +938,17 @@ template <typename Room> Shape shape_of(const mpode_recurrence_desc& d, const Re
     return s;
 }
 
-cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), const RecArgs& a, const RecMaps& maps, const Shape& s, bool scans, size_t smem, cudaStream_t st) {
+// most: the shared memory that any call of this kernel asks for.  The limit is set to that and not to this call's, which another host thread's call may be about
+// to replace by its own.
+cudaError_t launch(void (*kernel)(const RecArgs, const RecMaps, const int), const RecArgs& a, const RecMaps& maps, const Shape& s, bool scans, size_t smem, size_t most,
+                   cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.tiles * s.blocks));
     cfg.blockDim = dim3(32, s.warps + (scans ? 1 : 0));
     cfg.stream = st;
     cfg.dynamicSmemBytes = smem;
-    if (smem > 0) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (set != cudaSuccess) return set;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)s.blocks;
@@ -989,6 +990,11 @@ bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long l
     return time_major ? make_tensor_map(p, d.low, d.width, d.n_seq, d.n_steps, seq, step, 64, 1, steps, out)
                       : make_tensor_map(p, d.low, d.width, d.n_steps, d.n_seq, step, seq, 64, steps, 1, out);
 }
+// Shared memory of a block: the stages of its warps, and the exchange
+template <typename T, int L, int N> constexpr size_t smem_bytes(int access, int warps, int stages, int blocks) {
+    return (staged_rows(access) ? warps * stages * kStageBytes<T, L, N> : 0) + (access == PIPED ? sizeof(Scan) : blocks > 1 ? sizeof(Exchange) : kBlockExchange);
+}
+template <typename T, int L, int N> constexpr size_t most_bytes(int access) { return smem_bytes<T, L, N>(access, kMaxWarps, kMaxStages, access == STAGED ? 1 : kMaxCluster); }
 // How many clusters of a size the current device holds at once with one block an SM (asked once; the piped kernels are alike in what they need)
 int cluster_room(int blocks) {
     static std::atomic<int> known[kMaxDevices][kMaxCluster + 1];
@@ -997,8 +1003,7 @@ int cluster_room(int blocks) {
     if (n > 0) return n - 1;
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
-    const size_t smem = kMaxWarps * kMaxStages * kStageBytes<T, L, 2> + sizeof(Scan);
-    n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kMaxWarps + 1), smem, blocks);
+    n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kMaxWarps + 1), most_bytes<T, L, 2>(PIPED), blocks);
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }
@@ -1017,9 +1022,9 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
     const auto go = [&](auto access) {
         constexpr int A = access.value;
         a.stages = A == PIPED || s.warps < kMaxWarps || s.tiles <= sm_count() ? 3 : 2;
-        const size_t smem = (staged_rows(A) ? s.warps * a.stages * kStageBytes<T, L, N> : 0) + (A == PIPED ? sizeof(Scan) : s.blocks > 1 ? sizeof(Exchange) : kBlockExchange);
-        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
-        else return launch(recurrence_forward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, st);
+        const size_t smem = smem_bytes<T, L, N>(A, s.warps, a.stages, s.blocks), most = most_bytes<T, L, N>(A);
+        if constexpr (BACKWARD) return launch(recurrence_backward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, most, st);
+        else return launch(recurrence_forward_kernel<T, COUPLED, L, A>, a, maps, s, A == PIPED, smem, most, st);
     };
     if (d.n_steps > 2 * s.warps * s.blocks * L && words_fit(d, a) && pieces_fit(d, a)) {
         a.time_major = d.n_seq > 1 && a.in_seq < a.in_step;

@@ -691,6 +691,39 @@ def test_calls_on_two_streams_at_once():
             assert all(torch.equal(p, q) for p, q in zip(x, y))
 
 
+def test_calls_from_several_host_threads_at_once():
+    # Sizes of one kernel that need different amounts of shared memory, each from its own thread on its own stream
+    import threading
+    torch, b, _ = _torch()
+    cases = [_recurrence_case(B, T, D, "bf16") for B, T, D in ((300, 160, 64), (2500, 160, 64), (1, 9000, 64), (1, 9000, 72))]
+
+    def run(c):
+        y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"])
+        return [y, yT, *b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"])]
+
+    alone = [run(c) for c in cases]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(300):
+                    got = run(cases[i])
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(p, q) for p, q in zip(got, alone[i])):
+                    wrong.append("values of case %d" % i)
+        except Exception as e:
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+
+
 def test_operators_work_on_empty_batches():
     torch, b, _ = _torch()
     x = torch.zeros(0, 5, 8, dtype=torch.bfloat16, device="cuda:0")
