@@ -560,12 +560,12 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     if ((int)threadIdx.y == warps) {
         cluster_wait();
         scan(ex, 0u, stride, (unsigned)q.len, carry, warps, blocks, q.rank);
+        cluster_arrive();
+        cluster_wait();                                     // every block has read the state that the one behind the last step may replace
         if (p.last != nullptr && q.rank == 0) {
 #pragma unroll
             for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
         }
-        cluster_arrive();
-        cluster_wait();
         return;
     }
     Tile<T, L, kArrays, ACCESS> tile;
@@ -672,11 +672,11 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     if (p.zero_behind)
         for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps)
             store_pair<T, ACCESS>((char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es, 0, apart, typename W::type{});
+    if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written, and every block has read its y0
     if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
     }
-    if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written
 }
 
 // A few steps of many sequences (serving token by token): a thread runs them for two channels; nothing to exchange and no shared memory, so that a call costs
@@ -750,12 +750,12 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
     if ((int)threadIdx.y == warps) {
         cluster_wait();
         scan(ex, base, stride, (unsigned)p.n_steps, carry, warps, blocks, q.rank);
+        cluster_arrive();
+        cluster_wait();                                     // every block has read the state that the one behind the last step may replace
         if (p.last != nullptr && q.rank == 0) {
 #pragma unroll
             for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];
         }
-        cluster_arrive();
-        cluster_wait();
         return;
     }
     Tile<T, L, kArrays, ACCESS> tile;
@@ -905,12 +905,12 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWa
             store_pair<T, ACCESS>((char*)p.out + to, 0, apart, typename W::type{});
             store_pair<T, ACCESS>((char*)p.out2 + to, 0, apart, typename W::type{});
         }
+    warp_flag_or(p.flag, largest.nonfinite());
+    if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // as in the forward pass
     if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];
     }
-    warp_flag_or(p.flag, largest.nonfinite());
-    if (blocks > 1) { cluster_arrive(); cluster_wait(); }
 }
 
 // How a call is spread over the GPU: warps along the time axis of a block, then blocks of a cluster, until every SM has its warps or no steps are left

@@ -274,6 +274,21 @@ def test_recurrence_in_place_and_over_its_inputs():
         assert torch.equal(dy, ref[0]) and torch.equal(g, ref[1]) and torch.equal(dyT, ref[2])
 
 
+@pytest.mark.parametrize("T,D,n", [(9000, 64, 1), (9000, 64, 33), (9000, 30, 500), (20000, 65, 7), (20000, 65, 0)])
+def test_recurrence_state_in_place_where_blocks_share_a_sequence(T, D, n):
+    # Few steps of a long sequence: the first block writes the state while the others have no steps to read for
+    torch, b, _ = _torch()
+    c = _recurrence_case(2, T, D, "bf16")
+    lengths = torch.tensor([n, T], dtype=torch.int32, device="cuda:0")
+    y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"], lengths=lengths)
+    ref = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"], lengths=lengths)
+    state, adjoint = c["t_y0"].clone(), c["t_dyT"].clone()
+    assert torch.equal(b.recurrence_forward(c["t_x"], c["t_gate"], y0=state, yT=state, lengths=lengths)[0], y)
+    assert torch.equal(state, yT)
+    got = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=adjoint, y0=c["t_y0"], lengths=lengths, dL_dy0=adjoint)
+    assert all(torch.equal(p, q) for p, q in zip(got, ref))
+
+
 def test_recurrence_flags_gradients_that_overflow():
     torch, b, _ = _torch()
     c = _recurrence_case(2, 200, 34, "f16")
