@@ -305,7 +305,7 @@ const char* mpode_last_error(const mpode_ctx* ctx);
  *   - The low format is that of the block's tensors; states, adjoints, statistics, weights and weight gradients are float32.  Results are
  *     rounded to the low format once, when written, and are the same bits in every run.
  *   - Strides count elements and 0 means contiguous; channels lie side by side.  Any element-aligned pointer is taken; rows that are multiples
- *     of 16 bytes (4 bytes in the recurrence) from pointers aligned like that are read and written in wider accesses.
+ *     of 16 bytes (in the recurrence also of two elements) from pointers aligned like that are read and written in wider accesses.
  *   - flag_dev (device word, or NULL) is set to 1 when a low-format value that was written is not finite, and left alone otherwise: the finiteness test of Alg. 2.
  */
 const char* mpode_operator_error(void);
@@ -331,7 +331,7 @@ typedef struct {
 /*
  * y0_dev: fp32 [n_seq][width] or NULL (zero).  lengths_dev: int [n_seq] or NULL (all n_steps); values are clamped to 0 .. n_steps.  Elements of x,
  * gate and y behind a sequence's length are not read, and y is not written there unless zero_behind.  yT_dev: NULL, or fp32 [n_seq][width], the state behind the last step (y0
- * where the length is 0); it may be y0_dev.  y_dev may be x_dev.  n_steps = 1 with yT_dev = y0_dev is the form for serving token by token.
+ * where the length is 0); it may be y0_dev.  y_dev may be x_dev where the strides agree.  n_steps = 1 with yT_dev = y0_dev is the form for serving token by token.
  */
 mpode_status mpode_recurrence_forward(const mpode_recurrence_desc* desc, void* cuda_stream, const void* x_dev, const void* gate_dev,
                                       const float* y0_dev, const int* lengths_dev, void* y_dev, float* yT_dev);

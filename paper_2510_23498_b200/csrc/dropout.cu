@@ -65,6 +65,7 @@ extern "C" mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long l
     if (rows == 0) return MPODE_OK;
     if (rows > (1ll << 40)) return operator_fail(MPODE_ERR_UNSUPPORTED, "mpode_dropout: %lld rows", rows);
     if (!x_dev || !out_dev || !rng_dev) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: null pointer argument");
+    if (x_dev == out_dev && ld_x != ld_out && rows > 1) return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: out over x with other strides");
     const size_t es = low_size(low);
     if (misaligned(x_dev, es) || misaligned(out_dev, es) || misaligned(rng_dev, 8) || misaligned(flag_dev, 4))
         return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: a pointer is not aligned to its elements");

@@ -1064,9 +1064,9 @@ mpode_status check(const mpode_recurrence_desc* d, RecArgs& a) {
     if ((d->n_steps > 1 && (a.in_step < lo || a.out_step < lo)) || (d->n_seq > 1 && d->n_steps > 0 && (a.in_seq < lo || a.out_seq < lo)))
         return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: a stride is smaller than the width %d", d->width);
     // (the last element of one sequence lies before the first of the next, or the last sequence of one step before the first of the next)
-    const long long S = d->n_seq - 1, N = d->n_steps - 1;
-    if (S > 0 && N > 0 && ((a.in_seq <= N * a.in_step + lo - 1 && a.in_step <= S * a.in_seq + lo - 1) ||
-                           (a.out_seq <= N * a.out_step + lo - 1 && a.out_step <= S * a.out_seq + lo - 1)))
+    const __int128 S = d->n_seq - 1, N = d->n_steps - 1;
+    const auto overlap = [&](long long by_seq, long long by_step) { return by_seq <= N * by_step + lo - 1 && by_step <= S * by_seq + lo - 1; };
+    if (S > 0 && N > 0 && (overlap(a.in_seq, a.in_step) || overlap(a.out_seq, a.out_step)))
         return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: the strides make rows overlap");
     a.n_seq = d->n_seq; a.n_steps = d->n_steps; a.width = d->width; a.zero_behind = d->zero_behind;
     if (d->n_steps <= 1) a.in_step = a.out_step = lo;
@@ -1075,6 +1075,10 @@ mpode_status check(const mpode_recurrence_desc* d, RecArgs& a) {
     return MPODE_OK;
 }
 mpode_status check_pointers(const mpode_recurrence_desc& d, const RecArgs& a) {
+    // outputs over inputs of the other strides: y over x, dL_dx over dL_dy
+    const bool alike = a.in_step == a.out_step && (d.n_seq <= 1 || a.in_seq == a.out_seq);
+    if (d.n_steps > 0 && !alike && (a.y == nullptr ? a.out == a.x || a.out == a.gate : a.out == a.dy || a.out2 == a.dy))
+        return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: an output lies on an input of other strides");
     const void* const low[] = {a.x, a.gate, a.y, a.dy, a.out, a.out2};
     for (const void* q : low)
         if (misaligned(q, low_size(d.low))) return operator_fail(MPODE_ERR_INVALID_ARG, "recurrence: a pointer is not aligned to its elements");

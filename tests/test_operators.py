@@ -114,6 +114,17 @@ def test_recurrence_refuses_bad_arguments():
     assert _recurrence(lib, n_seq=0, at={i: None for i in range(6)}) == b.OK            # nothing to do
 
 
+def test_recurrence_refuses_outputs_over_inputs_of_other_strides_and_strides_beyond_64_bits():
+    from paper_2510_23498_b200 import binding as b
+    lib = b.load_library()
+    for kw in (dict(at={4: AT[0]}, in_step_stride=16, in_seq_stride=48), dict(at={4: AT[0]}, in_step_stride=16, in_seq_stride=8), dict(at={4: AT[1]}, out_seq_stride=32),
+               dict(n_seq=(1 << 20) + 1, in_seq_stride=1 << 44, in_step_stride=1 << 22, n_steps=(1 << 30) + 1)):
+        assert _recurrence(lib, **kw) == b.ERR_INVALID_ARG, kw
+        assert b"recurrence" in lib.mpode_operator_error()
+    for i in (7, 8):
+        assert _recurrence(lib, "backward", at={i: AT[5]}, out_seq_stride=32) == b.ERR_INVALID_ARG
+
+
 def _residual(lib, direction="forward", rows=4, at=None, scale_exp=0, nbytes=1 << 30, **kw):
     from paper_2510_23498_b200 import binding
     f = dict(low=1, width=64, post_norm=1, pre_norm=1, eps=1e-5, h=1.0, p_drop=0.0)
@@ -153,7 +164,7 @@ def test_dropout_refuses_bad_arguments():
         return lib.mpode_dropout(low, None, rows, width, x, ld_x, out, ld_out, p, rng, 0, flag)
 
     for kw in (dict(low=5), dict(rows=-1), dict(width=0), dict(p=-0.1), dict(p=1.1), dict(p=float("nan")), dict(ld_x=15), dict(ld_out=8), dict(x=None),
-               dict(out=None), dict(rng=None), dict(rng=AT[2] + 4), dict(x=AT[0] + 1), dict(flag=AT[3] + 1)):
+               dict(out=None), dict(rng=None), dict(rng=AT[2] + 4), dict(x=AT[0] + 1), dict(flag=AT[3] + 1), dict(out=AT[0], ld_x=32)):
         assert call(**kw) == b.ERR_INVALID_ARG, kw
     assert call(rows=1 << 41) == b.ERR_UNSUPPORTED
     assert call(rows=0, x=None, out=None, rng=None) == b.OK
