@@ -78,7 +78,7 @@ residual_backward_kernel(const ResArgs p, const int blocks) {
         const float s_u = st.y, r_y = in.broken ? __int_as_float(0x7fffffff) : st.w;
         float2 m0 = pair(0.f), m1 = pair(0.f), n0, n1;
         Oct kept;                                           // w_pre e, then c t sig
-        kept.fill(0.f);
+        kept.fill(in.broken ? __int_as_float(0x7fffffff) : 0.f);
         if (has_dz) {
             const float2 k = pair(p.cot_in * r_y);
 #pragma unroll

@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
             }
             KeptRow keep;
             if (p.drop.on) keep.draw(p.drop, (uint64_t)row * groups_row, q, seed, step);
-            const float2 k = pair((in.broken ? __int_as_float(0x7fffffff) : p.h) * p.drop.scale * rstd_u);
+            const float2 k = pair(p.h * p.drop.scale * rstd_u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const Quad u = in.template get<1>(h), yh = in.template get<0>(h);
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(Lane<WARPS, CLUSTER>::kThreads, 1024 / Lane<WA
                 y.v[2 * h + 1] = yh.v[1];
             }
         }
+        if (in.broken) y.fill(__int_as_float(0x7fffffff));
         in.sync();                                          // everyone has read this stage
         if (in.leader && row + (long long)in.kStages * q.step < p.rows) request(row + (long long)in.kStages * q.step, in.slot());
         in.done();
