@@ -170,7 +170,7 @@ struct Affine {
     }
 };
 
-constexpr int kMaxWarps = 8, kMaxCluster = 16;
+constexpr int kMaxWarps = 8, kPipedWarps = 11, kMaxCluster = 16;
 
 // Shared memory of the exchange inside a block or a cluster: maps of the block's warps and of the cluster's blocks, two sets in turn.  Places of warps and
 // blocks that do not exist hold the identity, so that the loops over them have fixed lengths and their loads go ahead of the arithmetic.
@@ -186,9 +186,9 @@ constexpr size_t kBlockExchange = offsetof(Exchange, block);
 // map of round k + 2 behind its second half of round k, for which the maps of round k had been read; states of round k + 2 are written when all maps of
 // it are there, behind the reads of round k's.
 struct __align__(16) Scan {
-    float warp[2][kMaxWarps][3][32 * V];
+    float warp[2][kPipedWarps][3][32 * V];
     float block[2][kMaxCluster][3][32 * V];
-    float start[2][kMaxWarps][32 * V];
+    float start[2][kPipedWarps][32 * V];
     unsigned long long maps[2], bytes[2], starts[2];
 };
 __device__ __forceinline__ void lds(float (&f)[V], const float* p) {
@@ -364,9 +364,10 @@ enum Access : int {
     STAGED = 0,     // rows of multiples of 16 bytes from aligned pointers: bulk tensor copies to shared memory, neighbouring channels a lane
     PAIRS = 1,      // even widths and strides, pointers aligned to two elements: neighbouring channels a lane, one access
     SINGLES = 2,    // anything: channels 32 apart a lane, an access each
-    PIPED = 3       // STAGED, in clusters: the next round's maps are on their way while this round's are waited for
+    PIPED = 3       // STAGED, in clusters: a round's maps are on their way while those of the one before are waited for
 };
 __host__ __device__ constexpr bool staged_rows(int access) { return access == STAGED || access == PIPED; }
+__host__ __device__ constexpr int most_warps(int access) { return access == PIPED ? kPipedWarps : kMaxWarps; }
 // Which channels and steps a thread works on.  Channels behind the last one are the last one again (the last pair), and the same values go to the same
 // places: a condition at each store costs more than the rest of the second run (1320 cycles a round of 16 steps instead of 520).
 struct Place { int seq, tile, lane, col[2], len, rank; unsigned slot; };      // tile: the first channel of the warp
@@ -529,11 +530,11 @@ template <typename T, int L, int N, int ACCESS> struct Tile<T, L, N, ACCESS, tru
 };
 
 template <typename T, bool COUPLED, int L, int ACCESS>
-__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
+__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_forward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T>;
     constexpr int kArrays = 2;
     extern __shared__ __align__(128) char staged[];
-    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kMaxStages : 1];
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? most_warps(ACCESS) * kMaxStages : 1];
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
@@ -716,12 +717,12 @@ template <typename T, bool COUPLED, int ACCESS> __global__ void __launch_bounds_
 // Steps counted from the end: step i of a warp's tile is time n_steps - 1 - (base + slot * L + i).
 // Arrays of the tile: gate, cotangent, state in front of the step, x (coupled only)
 template <typename T, bool COUPLED, int L, int ACCESS>
-__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kMaxWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
+__global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMaxWarps), ACCESS == PIPED ? 1 : 2) recurrence_backward_kernel(const RecArgs p, const __grid_constant__ RecMaps maps, const int blocks) {
     using W = Word<T>;
     constexpr int kArrays = COUPLED ? 4 : 3;
     using word = typename W::type;
     extern __shared__ __align__(128) char staged[];
-    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? kMaxWarps * kMaxStages : 1];
+    __shared__ unsigned long long arrived[staged_rows(ACCESS) ? most_warps(ACCESS) * kMaxStages : 1];
     constexpr bool kScan = ACCESS == PIPED;                 // the last warp scans
     const int warps = kScan ? (int)blockDim.y - 1 : (int)blockDim.y;
     const bool alone = !kScan && blocks == 1 && warps == 1;
@@ -921,7 +922,7 @@ bool round_fits(const RecArgs& a, long long steps, int es) {
     return step < (1ll << 32) && (steps * step + a.width) * es < (1ll << 32);
 }
 // Blocks of a cluster: of the sizes that the GPU holds as many of at once as there are tiles, the largest (65536 steps of 1024 channels, 16 tiles: 148 SMs hold 15
-// clusters of 8 blocks and 22 of 6, 197 and 140 us).  `room` asks the runtime how many clusters of a size there is room for.
+// clusters of 8 blocks and 22 of 6, with the last cluster of 8 behind the others 1.4 times the time).  `room` asks the runtime how many clusters of a size there is room for.
 template <typename Room> Shape shape_of(const mpode_recurrence_desc& d, const RecArgs& a, int steps_of_warp, Room&& room) {
     Shape s;
     s.tiles = (long long)d.n_seq * ((d.width + 63) / 64);
@@ -994,7 +995,7 @@ bool map_of(const void* p, const mpode_recurrence_desc& d, long long seq, long l
 template <typename T, int L, int N> constexpr size_t smem_bytes(int access, int warps, int stages, int blocks) {
     return (staged_rows(access) ? warps * stages * kStageBytes<T, L, N> : 0) + (access == PIPED ? sizeof(Scan) : blocks > 1 ? sizeof(Exchange) : kBlockExchange);
 }
-template <typename T, int L, int N> constexpr size_t most_bytes(int access) { return smem_bytes<T, L, N>(access, kMaxWarps, kMaxStages, access == STAGED ? 1 : kMaxCluster); }
+template <typename T, int L, int N> constexpr size_t most_bytes(int access) { return smem_bytes<T, L, N>(access, most_warps(access), kMaxStages, access == STAGED ? 1 : kMaxCluster); }
 // How many clusters of a size the current device holds at once with one block an SM (asked once; the piped kernels are alike in what they need)
 int cluster_room(int blocks) {
     static std::atomic<int> known[kMaxDevices][kMaxCluster + 1];
@@ -1003,7 +1004,7 @@ int cluster_room(int blocks) {
     if (n > 0) return n - 1;
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
-    n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kMaxWarps + 1), most_bytes<T, L, 2>(PIPED), blocks);
+    n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kPipedWarps + 1), most_bytes<T, L, 2>(PIPED), blocks);
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }
@@ -1015,7 +1016,7 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
         else recurrence_steps_kernel<T, COUPLED, SINGLES><<<grid, 128, 0, st>>>(a);
         return cudaGetLastError();
     }
-    const Shape s = shape_of(d, a, L, cluster_room);
+    Shape s = shape_of(d, a, L, cluster_room);
     RecMaps maps;
     // Three rounds in shared memory, or two where two blocks of 8 warps share an SM (us with 2 / 3: backward of 8 x 4096 x 2048 bfloat16, 256 tiles, 143 / 152;
     // 8 x 2048 x 1024 float32, 128 tiles, 87 / 80; 128 x 128 x 2048, 2 warps a block, 96 / 82)
@@ -1037,7 +1038,14 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
             ok = ok && map_of(a.y, d, a.out_seq, a.out_step, L, tm, &maps.m[2]);
             if (COUPLED) ok = ok && map_of(a.x, d, a.in_seq, a.in_step, L, tm, &maps.m[3]);
         }
-        if (ok) return s.blocks > 1 ? go(Way<PIPED>()) : go(Way<STAGED>());
+        if (ok && s.blocks > 1) {
+            // many rounds: more warps hide one another's phases (us with 8 / 11: 65536 steps of 1024 bfloat16 channels 123 / 109, backward of 32768 127 / 109;
+            // few rounds: 4 x 2048 x 512, 16.4 / 18.5).  Twelve warps with the scanning one are three a scheduler, with 168 registers a thread; a thirteenth leaves 128 (117, 113)
+            const long long steps = (long long)kPipedWarps * s.blocks * L;
+            if (d.n_steps >= 8 * steps && round_fits(a, steps, (int)low_size(d.low))) s.warps = kPipedWarps;
+            return go(Way<PIPED>());
+        }
+        if (ok) return go(Way<STAGED>());
     }
     return words_fit(d, a) ? go(Way<PAIRS>()) : go(Way<SINGLES>());
 }

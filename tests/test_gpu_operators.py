@@ -124,6 +124,8 @@ CASES = [
     # tiles brought to shared memory ahead: blocks by themselves (enough channels in all), and clusters over several rounds
     (80, 300, 64, "bf16", dict(ragged=True)), (75, 290, 72, "f32", dict(layout="time")), (20, 700, 200, "f16", dict(ragged=True, layout="half")),
     (1, 5000, 64, "bf16", {}), (2, 4500, 40, "f16", dict(ragged=True)), (1, 2600, 72, "f32", dict(layout="half")), (3, 3000, 328, "bf16", dict(ragged=True, layout="time")),
+    # clusters of more warps, for many rounds
+    (1, 24001, 64, "bf16", {}), (2, 12000, 72, "f32", dict(ragged=True)), (3, 23000, 40, "f16", dict(ragged=True, layout="time")),
     # many short sequences
     (300, 5, 66, "bf16", dict(ragged=True)), (40, 33, 96, "f32", dict(ragged=True, layout="time")),
     # slices of wider rows at odd addresses
