@@ -453,17 +453,23 @@ __device__ __forceinline__ void rounds(unsigned base, unsigned stride, unsigned 
     }
 }
 
-// the cache lines of a row's part of `bytes` bytes
-template <typename T> __device__ __forceinline__ void touch_row(const char* p, int bytes) {
-    asm volatile("prefetch.global.L1 [%0];" ::"l"(p));
-    asm volatile("prefetch.global.L1 [%0];" ::"l"(p + bytes - 1));
-    if (sizeof(T) == 4) asm volatile("prefetch.global.L1 [%0];" ::"l"(p + bytes / 2));
+// Asks for rows that a warp is going to read: N arrays of L rows, `bytes` bytes of each (64 channels at most) from at(array, row) on, null for one that is not
+// there.  A request a cache line; one for each sector, to the nearest cache, costs more than it saves (37 x 1000 x 785 float16 backward 125 us instead of 115,
+// without requests 127).
+template <typename T, int L, int N, typename At> __device__ __forceinline__ void touch_rows(int bytes, At&& at) {
+    constexpr int S = sizeof(T) == 4 ? 3 : 2;               // lines of 128 bytes that 64 channels reach into
+#pragma unroll
+    for (int j = 0; j < N * L * S; j += 32) {
+        const int r = (j + threadIdx.x) / S, line = j + threadIdx.x - r * S;
+        const char* const p = r < N * L ? at(r / L, r % L) : nullptr;
+        if (p != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + min(128 * line, bytes - 1)));
+    }
 }
 
 // Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
 //   STAGED, PIPED: brought to shared memory two or three rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
 //           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
-//   else:   loaded into registers when the round starts, from the cache, for which a lane has asked for one row of the round a round ahead.
+//   else:   loaded into registers when the round starts, from the cache, for which the lanes have asked for its rows a round ahead.
 template <typename T> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 constexpr int kMaxStages = 3;
 template <typename T, int L, int N> constexpr int kStageBytes = N * L * kRowBytes<T>;      // of a warp
@@ -471,12 +477,12 @@ template <typename T, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS
     using word = typename Word<T>::type;
     word w[N][L];
     unsigned apart;
-    // step i of array k lies at base + off + i * step bytes; steps lo .. hi - 1 exist
-    __device__ __forceinline__ void load(int k, const char* base, unsigned off, unsigned step, int lo, int hi) {
+    // step i of array k lies at base + off + i * step bytes; steps lo .. hi - 1 exist (FULL: all)
+    template <bool FULL> __device__ __forceinline__ void load(int k, const char* base, unsigned off, unsigned step, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < L; ++i, off += step) {
-            w[k][i] = word{};
-            if (i >= lo && i < hi) w[k][i] = load_pair<T, ACCESS>(base, off, apart);
+            if (!FULL) w[k][i] = word{};
+            if (FULL || (i >= lo && i < hi)) w[k][i] = load_pair<T, ACCESS>(base, off, apart);
         }
     }
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
@@ -579,15 +585,15 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         if constexpr (staged_rows(ACCESS))
             if (base < (unsigned)q.len && elected()) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
     };
-    auto load = [&](unsigned base) {
+    auto load = [&](auto full, unsigned base) {
         if constexpr (!staged_rows(ACCESS)) {
             const int n = count(base);
-            tile.load(0, g, in_at, in_step, 0, n);
-            tile.load(1, x, in_at, in_step, 0, n);
+            tile.template load<full.value>(0, g, in_at, in_step, 0, n);
+            tile.template load<full.value>(1, x, in_at, in_step, 0, n);
             x += in_round; g += in_round;
-            const int k = threadIdx.x / L, i = threadIdx.x % L;
-            if (k < 2 && i < count(base + stride))
-                touch_row<T>((k == 0 ? g : x) + (unsigned)(in_at - (q.col[0] - q.tile) * es + i * in_step), min(64, p.width - q.tile) * (int)es);
+            const int ahead = count(base + stride);
+            const unsigned first = in_at - (q.col[0] - q.tile) * es;
+            touch_rows<T, L, 2>(min(64, p.width - q.tile) * (int)es, [&](int k, int i) { return i < ahead ? (k == 0 ? g : x) + (unsigned)(first + i * in_step) : nullptr; });
         }
     };
     if constexpr (staged_rows(ACCESS)) {
@@ -604,9 +610,9 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         const int n = count(base);
         int stage = 0;
         if constexpr (staged_rows(ACCESS)) stage = tile.wait(broken);
-        else load(base);
         r.stage = stage;
         auto run = [&](auto full) {
+            load(full, base);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float f[V], none[V];
@@ -773,24 +779,25 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
                 tile.request(stage, maps, (COUPLED ? 13u : 5u) | (p.dy != nullptr ? 2u : 0u), q.tile, q.seq, p.time_major != 0, t0, t0 - 1);
             }
     };
-    auto load = [&](unsigned base) {
+    auto load = [&](auto full, unsigned base) {
         if constexpr (!staged_rows(ACCESS)) {
+            constexpr bool F = full.value;
             int lo, hi;
             range(base, lo, hi);
             const int before = base + q.slot * L + hi == (unsigned)p.n_steps ? hi - 1 : hi;     // time 0 has no stored state in front of it
-            tile.load(0, g, in_at, 0u - in_step, lo, hi);
-            if (p.dy != nullptr) tile.load(1, dy, out_at, 0u - out_step, lo, hi);
-            tile.load(2, y, out_at, 0u - out_step, lo, before);
-            if constexpr (COUPLED) tile.load(3, x, in_at, 0u - in_step, lo, hi);
+            tile.template load<F>(0, g, in_at, 0u - in_step, lo, hi);
+            if (p.dy != nullptr) tile.template load<F>(1, dy, out_at, 0u - out_step, lo, hi);
+            tile.template load<F>(2, y, out_at, 0u - out_step, lo, before);
+            if constexpr (COUPLED) tile.template load<F>(3, x, in_at, 0u - in_step, lo, hi);
             x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
-            const int k = threadIdx.x / L, i = threadIdx.x % L;
             range(base + stride, lo, hi);
-            const bool last = k == 2 && base + stride + q.slot * L + i + 1 == (unsigned)p.n_steps;
-            if (k < kArrays && (k != 1 || p.dy != nullptr) && i >= lo && i < hi && !last) {
-                const unsigned to_tile = (q.col[0] - q.tile) * es;
+            const unsigned to_tile = (q.col[0] - q.tile) * es;
+            const int zero = (int)(p.n_steps - 1 - (base + stride + q.slot * L));
+            touch_rows<T, L, kArrays>(min(64, p.width - q.tile) * (int)es, [&](int k, int i) {
                 const char* const from = k == 0 ? g : k == 1 ? dy : k == 2 ? y : x;
-                touch_row<T>(from + (unsigned)((k == 0 || k == 3 ? in_at - i * in_step : out_at - i * out_step) - to_tile), min(64, p.width - q.tile) * (int)es);
-            }
+                const bool there = i >= lo && i < hi && (k != 1 || p.dy != nullptr) && (k != 2 || i != zero);
+                return there ? from + (unsigned)((k == 0 || k == 3 ? in_at - i * in_step : out_at - i * out_step) - to_tile) : nullptr;
+            });
         }
     };
     if constexpr (staged_rows(ACCESS)) {
@@ -809,9 +816,9 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         int stage = 0, lo, hi;
         range(base, lo, hi);
         if constexpr (staged_rows(ACCESS)) stage = tile.wait(broken);
-        else load(base);
         r.stage = stage;
         auto run = [&](auto full) {
+            load(full, base);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 float f[V];
