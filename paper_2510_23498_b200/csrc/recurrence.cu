@@ -676,9 +676,11 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         }
     };
     rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, whole, first, second);
-    if (p.zero_behind)
-        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps)
-            store_pair<T, ACCESS>((char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es, 0, apart, typename W::type{});
+    if (p.zero_behind) {
+        const long long n = blocks * warps, apace = n * out_step;
+        long long i = (long long)q.len + q.slot;
+        for (char* to = (char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es; i < p.n_steps; i += n, to += apace) store_pair<T, ACCESS>(to, 0, apart, typename W::type{});
+    }
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written, and every block has read its y0
     if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
@@ -907,12 +909,14 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         }
     };
     rounds<ACCESS == PIPED, Turn>(base, stride, (unsigned)p.n_steps, whole, first, second);
-    if (p.zero_behind)
-        for (long long i = (long long)q.len + q.slot; i < p.n_steps; i += blocks * warps) {
-            const long long to = (q.seq * p.in_seq + i * p.in_step + q.col[0]) * es;
-            store_pair<T, ACCESS>((char*)p.out + to, 0, apart, typename W::type{});
-            store_pair<T, ACCESS>((char*)p.out2 + to, 0, apart, typename W::type{});
+    if (p.zero_behind) {
+        const long long n = blocks * warps, apace = n * in_step;
+        long long i = (long long)q.len + q.slot, to = (q.seq * p.in_seq + i * p.in_step + q.col[0]) * es;
+        for (; i < p.n_steps; i += n, to += apace) {
+            store_pair<T, ACCESS>((char*)p.out + to, 0, apart, word{});
+            store_pair<T, ACCESS>((char*)p.out2 + to, 0, apart, word{});
         }
+    }
     warp_flag_or(p.flag, largest.nonfinite());
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // as in the forward pass
     if (!kScan && p.last != nullptr && q.slot == 0) {
