@@ -16,9 +16,9 @@ struct DropArgs {
 };
 
 // One thread, one group of eight columns at a time: 16-byte accesses where the layout allows.  FLAT: rows of whole groups one behind the other, where a
-// group's place needs no division.  Bound by the generator's wide products beside the bytes: 8192 x 8192 bfloat16 take 59 us (41 for the bytes alone), with one, two or
-// four groups in flight alike.
-template <typename T, bool VEC, bool FLAT> __global__ void __launch_bounds__(256, 6) dropout_kernel(const DropArgs p) {
+// group's place needs no division.  Bound by the generator's wide products beside the bytes: 8192 x 8192 bfloat16 take 57 us (41 for the bytes alone), with one, two or
+// four groups in flight alike.  Eight blocks an SM in 32 registers where that needs no memory for them (six: 60 us).
+template <typename T, bool VEC, bool FLAT> __global__ void __launch_bounds__(256, VEC && sizeof(T) == 2 ? 8 : 6) dropout_kernel(const DropArgs p) {
     const uint64_t seed = p.d.rng[0], step = p.d.rng[1];
     Largest<T> largest;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < p.groups; i += (long long)gridDim.x * 256) {
