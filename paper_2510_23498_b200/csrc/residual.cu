@@ -4,7 +4,7 @@
 //
 // This file: argument checks, how rows are spread over the GPU, and the weights' gradients' last sums; the passes are in residual_forward.cu and
 // residual_backward.cu.  Bound by the bytes of its rows (16-bit formats: 14 an element forward, 22 backward): a row is read once from memory and
-// written once.  Eight neighbouring columns a thread (16-byte accesses, one counter of the generator); a row takes one warp up to 256 columns, a block of
+// written once.  Eight columns a thread, in two fours (neighbouring lanes share the generator's counters); a row takes one warp up to 256 columns, a block of
 // up to 8 warps up to 2048, and a cluster of up to 8 blocks beyond that, whose partial sums meet in distributed shared memory.  All sums, statistics,
 // gates and gradients are float32; what is stored in the low format is rounded once, when it is written.
 #include "residual.cuh"
