@@ -83,9 +83,10 @@ struct Ops {
     }
 };
 
-// -sigmoid(g) = -b, and the slope b (1 - b), which is e b^2 with e = exp(-g).  16-bit gates: the device's approximate power and quotient (2^-22
-// relative, and the argument's rounding adds |g| 2^-24), which cost 3 instructions a channel where the accurate ones of float32 cost 15; for the slope
-// the exponent is kept below 2^126, so that e b^2 is finite: b is 1e-38 instead of less, which no float32 state feels.
+// -sigmoid(g) = -b, and the slope b (1 - b), which is (e b) b with e = exp(-g), in this order: e b is 1 - b, where b b would leave float32's range below
+// g = -44.  16-bit gates: the device's approximate power and quotient (2^-22 relative, and the argument's rounding adds |g| 2^-24), which cost 3 instructions
+// a channel where the accurate ones of float32 cost 15.  A b below 2^-126 is zero there (the quotient has no smaller numbers); for the slope the exponent
+// is kept at 2^127, so that e b is then zero too.
 template <typename T, bool SLOPE> __device__ __forceinline__ void negated_gate(const float (&g)[V], float (&nb)[V], float (&slope)[V]) {
     float e[V];
     if constexpr (sizeof(T) == 4) {
@@ -103,7 +104,7 @@ template <typename T, bool SLOPE> __device__ __forceinline__ void negated_gate(c
         Ops::mul(e, g, k);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (SLOPE) asm("min.NaN.f32 %0, %0, %1;" : "+f"(e[v]) : "f"(126.f));
+            if (SLOPE) asm("min.NaN.f32 %0, %0, %1;" : "+f"(e[v]) : "f"(127.f));
             asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[v]));
             k[v] = -1.f;
         }
@@ -111,8 +112,8 @@ template <typename T, bool SLOPE> __device__ __forceinline__ void negated_gate(c
 #pragma unroll
         for (int v = 0; v < V; ++v) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb[v]) : "f"(d[v]));
         if (SLOPE) {
-            Ops::mul(slope, nb, nb);
-            Ops::mul(slope, slope, e);
+            Ops::mul(slope, e, nb);
+            Ops::mul(slope, slope, nb);
         }
     }
 }

@@ -282,8 +282,9 @@ struct KeptRow {
     }
 };
 
-// sigmoid and its slope sig (1 - sig) = e sig^2 with e = exp(-g).  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the
-// argument's rounding adds |g| 2^-24); the exponent is kept below 2^126, so that e sig^2 is finite.
+// sigmoid and its slope sig (1 - sig) = (e sig) sig with e = exp(-g), in this order: e sig is 1 - sig, where sig sig would leave float32's range below
+// g = -44.  16-bit gates: the device's approximate power and reciprocal (2^-22 relative, and the argument's rounding adds |g| 2^-24).  A sigmoid below
+// 2^-126 is zero there (the reciprocal has no smaller numbers); for the slope the exponent is kept at 2^127, so that e sig is then zero too.
 template <typename T, bool SLOPE> __device__ __forceinline__ float2 gate_of(float2 g, float2& slope) {
     float2 e, s;
     if constexpr (sizeof(T) == 4) {
@@ -293,15 +294,15 @@ template <typename T, bool SLOPE> __device__ __forceinline__ float2 gate_of(floa
     } else {
         e = __fmul2_rn(g, pair(-1.4426950408889634f));
         if (SLOPE) {
-            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(126.f));
-            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(126.f));
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(127.f));
+            asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(127.f));
         }
         asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
         asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
         const float2 d = __fadd2_rn(e, pair(1.f));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
-        if (SLOPE) slope = __fmul2_rn(__fmul2_rn(s, s), e);
+        if (SLOPE) slope = __fmul2_rn(__fmul2_rn(e, s), s);
     }
     return s;
 }

@@ -1,0 +1,76 @@
+"""Sequence and residual operators on the GPU where float32 ends: gates whose slope is near the smallest normal number.
+
+Tolerances as in test_gpu_operators.py."""
+import numpy as np
+import pytest
+
+from oracle import operators as orc
+from test_gpu_operators import E, _check_residual, _close, _np, _recurrence_case, _recurrence_error, _residual_case, _stored, _torch, _up
+
+pytestmark = pytest.mark.gpu
+
+FAR = [-40.0, -46.0, -50.0, -51.0, -52.0, -60.0, -75.0, -86.0, -100.0, -np.inf]
+
+
+@pytest.mark.parametrize("T", [1, 40, 1300, 5000])
+@pytest.mark.parametrize("D", [48, 33])
+@pytest.mark.parametrize("coupled", [True, False])
+def test_recurrence_gradients_of_bfloat16_gates_far_below_zero(T, D, coupled):
+    # The slope b (1 - b) of these gates is 1e-18 to 1e-38, an ordinary bfloat16 number.  Relative error of b and of the slope: the power's argument is rounded (86 * 2^-24
+    # = 2^-17.6), the power, the quotient and three products 2^-21 together: below 2^-16.  Below 2^-126 b counts as zero: off by that times the other factors.
+    torch, b, _ = _torch()
+    rng = np.random.default_rng(17)
+    c = _recurrence_case(2, T, D, "bf16", gate=rng.choice(FAR + [30.0, np.inf, 0.0], size=(2, T, D)))
+    y = _up(rng.normal(size=(2, T, D)), torch.bfloat16)
+    got = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], y0=c["t_y0"], coupled=coupled)
+    _check_far(c, _np(y), got, coupled)
+
+
+@pytest.mark.parametrize("T", [1, 40, 5000])
+def test_recurrence_gradients_of_float16_gates_far_below_zero(T):
+    # The same where a large adjoint brings the gradients into float16's range (steps that forget nothing hand it on unchanged)
+    torch, b, _ = _torch()
+    rng = np.random.default_rng(18)
+    c = _recurrence_case(2, T, 48, "f16", gate=rng.choice([-50.0, -51.0, -52.0, -60.0, -100.0, -np.inf], size=(2, T, 48)))
+    c["dyT"], c["dy"] = c["dyT"] * 2.0 ** 72, 0 * c["dy"]
+    y = _up(rng.normal(size=(2, T, 48)), torch.float16)
+    got = b.recurrence_backward(c["t_x"], c["t_gate"], y, None, dL_dyT=_up(c["dyT"]), y0=c["t_y0"])
+    _check_far(c, _np(y), got, True)
+
+
+def _check_far(c, y, got, coupled):
+    dx, dg, dy0, lmag, rmag = orc.recurrence_backward(c["x"], c["gate"], y, c["dy"], c["dyT"], c["y0"], c["lengths"], coupled)
+    T = y.shape[1]
+    err = _recurrence_error(T, np.concatenate([lmag, np.abs(c["dyT"])[:, None]], 1))
+    b, a = orc.sigmoid(c["gate"])
+    before = np.concatenate([c["y0"][:, None], y[:, :-1]], 1)
+    other = np.abs(c["x"]) + np.abs(before) if coupled else np.abs(before)
+    el = err + 2.0 ** -16 * lmag
+    _close(_np(got[0]), dx, _stored(dx, c["low"], b * el + 2.0 ** -126 * lmag if coupled else el), "dx")
+    _close(_np(got[1]), dg, _stored(dg, c["low"], other * (a * b * el + 2.0 ** -126 * lmag)), "dgate")
+    _close(_np(got[2]), dy0, err[:, 0], "dy0")
+
+
+@pytest.mark.parametrize("M,D", [(40, 64), (9, 785), (6, 2048), (5, 4096)])
+def test_residual_gradients_of_bfloat16_gates_far_below_zero(M, D):
+    torch, b, _ = _torch()
+    c = _residual_case(M, D, "bf16")
+    g = np.random.default_rng(19).choice(FAR + [0.0, 30.0, np.inf], size=(M, D))
+    c["t_gate"] = _up(g, torch.bfloat16)
+    c["gate"] = _np(c["t_gate"])
+    step = b.ResidualStep(D, low="bf16", h=0.3, site=21)
+    w = dict(gate=c["t_gate"], w_post=c["t_w_post"], scale=c["t_scale"], w_pre=c["t_w_pre"])
+    got = step.forward(c["t_y"], c["t_u"], **w)
+    grads = step.backward(got[0], c["t_u"], got[2], dL_dy=c["t_dy"], dL_dz=c["t_dz"], **w)
+    h, eps = float(np.float32(0.3)), float(np.float32(1e-5))
+    _check_residual(c, ("rms", "rms"), h, got, {**grads, "dscale": None, "dw_post": None}, eps=eps)
+    # The weights' sums may have such gates alone: beside the relative error, sigmoids below 2^-126 count as zero and are off by that times the other factors
+    y1 = _np(got[0])
+    ref = orc.residual_backward(y1, c["u"], c["gate"], c["w_post"], c["scale"], c["w_pre"], h, "rms", "rms", eps, c["factors"], c["dy"], c["dz"])
+    n2, _, ry = orc.norm(y1, "rms", eps)
+    dzw = np.abs(c["dz"] * c["w_pre"])
+    amag = np.abs(c["dy"]) + ry[:, None] * (dzw + np.abs(n2) * (dzw * np.abs(n2)).mean(1, keepdims=True))
+    mag = h * amag * np.abs(orc.norm(c["u"], "rms", eps)[0])
+    sig = orc.sigmoid(c["gate"])[0]
+    for key, w in (("dscale", c["w_post"]), ("dw_post", c["scale"])):
+        _close(_np(grads[key]), ref[key], (mag * np.abs(w) * ((4 * E + M * 2.0 ** -24) * sig + 2.0 ** -126)).sum(0), key)
