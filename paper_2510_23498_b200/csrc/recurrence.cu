@@ -25,6 +25,7 @@
 
 #include "cluster.cuh"
 #include "operators.h"
+#include "recurrence_tiles.h"
 #include "rows.cuh"
 #include "tensormap.h"
 
@@ -469,7 +470,8 @@ template <typename T, int L, int N, typename At> __device__ __forceinline__ void
 
 // Where a warp finds its steps: a tile of N arrays, L steps of two channels a lane.
 //   STAGED, PIPED: brought to shared memory two or three rounds ahead (each warp its own stages and barriers, so that no other warp has to be waited for), read from there
-//           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)
+//           as often as needed.  (Asynchronous copies of 16 bytes a lane in their place took 320 cycles a round of 2200 for issuing them.)  A tile that reaches
+//           behind its sequence's length, one a warp at most, comes as asynchronous copies of a lane's two channels, row by row.
 //   else:   loaded into registers when the round starts, from the cache, for which the lanes have asked for its rows a round ahead.
 template <typename T> constexpr int kRowBytes = 32 * V * (int)sizeof(T);
 constexpr int kMaxStages = 3;
@@ -488,6 +490,10 @@ template <typename T, int L, int N, int ACCESS, bool SHARED = staged_rows(ACCESS
     }
     __device__ __forceinline__ word get(int, int k, int i) const { return w[k][i]; }
 };
+// (a call, because it is rare: in line it cost every round of the piped kernel 4 %; a tile that is read when its turn has come cost 37 x 1000 x 784 46 us instead of 41)
+template <int BYTES> __device__ __noinline__ void copy_rows(unsigned to, unsigned pitch, const char* from, long long step, int count) {
+    for (; count > 0; --count, to += pitch, from += step) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
 template <typename T, int L, int N, int ACCESS> struct Tile<T, L, N, ACCESS, true> {
     using word = typename Word<T>::type;
     static constexpr int kRow = kRowBytes<T>, kArray = L * kRow;
@@ -514,6 +520,15 @@ template <typename T, int L, int N, int ACCESS> struct Tile<T, L, N, ACCESS, tru
                              ::"r"(at + (stage * N + k) * kArray), "l"(reinterpret_cast<unsigned long long>(&maps.m[k])), "r"(bar + 8 * stage), "r"(tile),
                                "r"(time_major ? seq : t), "r"(time_major ? t : seq) : "memory");
             }
+    }
+    // all lanes: `count` rows of array k from row lo of the tile on, which lies at `from`; then, when all are under way, that there are no more
+    __device__ __forceinline__ void request_rows(int stage, int k, int lo, int count, const char* from, long long step) const {
+        copy_rows<sizeof(word)>(lane + (stage * N + k) * kArray + lo * kRow, kRow, from, step, count);
+    }
+    __device__ __forceinline__ void rows_requested(int stage) const {
+        asm volatile("cp.async.mbarrier.arrive.shared.b64 [%0];" ::"r"(bar + 8 * stage) : "memory");      // (holds the phase open until this lane's are there)
+        __syncwarp();
+        if (threadIdx.x == 0) bar_arrive(bar + 8 * stage);
     }
     // the next round's stage, once it is there
     __device__ __forceinline__ int wait(bool& broken) {
@@ -582,9 +597,20 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         const unsigned t0 = base + q.slot * L;
         return t0 < (unsigned)q.len ? (int)min((unsigned)L, (unsigned)q.len - t0) : 0;
     };
+    const unsigned copied = staged_rows(ACCESS) ? copied_below(q.slot * L, L, q.len, p.n_steps) : 0u;
     auto request = [&](unsigned base, int stage) {
         if constexpr (staged_rows(ACCESS))
-            if (base < (unsigned)q.len && elected()) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
+            if (base < copied && elected()) tile.request(stage, maps, 3u, q.tile, q.seq, p.time_major != 0, (int)(base + q.slot * L), 0);
+    };
+    // the tile that is not copied: in the last round only
+    auto request_rows = [&](unsigned base, int stage) {
+        if constexpr (staged_rows(ACCESS))
+            if (base >= copied && base < (unsigned)q.len) {
+                const long long from = (long long)base * in_step + in_at;
+                tile.request_rows(stage, 0, 0, count(base), g + from, in_step);
+                tile.request_rows(stage, 1, 0, count(base), x + from, in_step);
+                tile.rows_requested(stage);
+            }
     };
     auto load = [&](auto full, unsigned base) {
         if constexpr (!staged_rows(ACCESS)) {
@@ -599,7 +625,10 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
     };
     if constexpr (staged_rows(ACCESS)) {
         tile.bind(staged, arrived, q.lane, p.stages);
-        for (int k = 0; k < p.stages; ++k) request(k * stride, k);
+        for (int k = 0; k < p.stages; ++k) {
+            request(k * stride, k);
+            request_rows(k * stride, k);
+        }
     } else tile.apart = apart;
     if (blocks > 1) cluster_wait();
     // A round's two halves: gates and the map of this warp's steps, published; then the steps again from the state in front of them
@@ -674,6 +703,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         if constexpr (staged_rows(ACCESS)) {
             __syncwarp();                                   // all lanes have read this stage
             request(r.base + p.stages * stride, stage);
+            request_rows(r.base + p.stages * stride, stage);
         }
     };
     rounds<ACCESS == PIPED, Turn>(0u, stride, (unsigned)q.len, whole, first, second);
@@ -805,7 +835,20 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
     };
     if constexpr (staged_rows(ACCESS)) {
         tile.bind(staged, arrived, q.lane, p.stages);
-        for (int k = 0; k < p.stages; ++k) request(base + k * stride, k);
+        int lo, hi;
+        range(base, lo, hi);
+        if (copied_back(base + q.slot * L, skipped)) request(base, 0);
+        else {                                              // (in the first round only)
+            const long long t = (long long)p.n_steps - base - q.slot * L - hi;                      // the earliest step that exists
+            const long long in = (q.seq * p.in_seq + q.col[0]) * es + t * in_step, outer = (q.seq * p.out_seq + q.col[0]) * es + t * out_step;
+            const int before = t == 0 ? 1 : 0;                                                      // time 0 has no stored state in front of it
+            tile.request_rows(0, 0, L - hi, hi - lo, (const char*)p.gate + in, in_step);
+            if (p.dy != nullptr) tile.request_rows(0, 1, L - hi, hi - lo, (const char*)p.dy + outer, out_step);
+            tile.request_rows(0, 2, L - hi + before, hi - lo - before, (const char*)p.y + outer + (before - 1ll) * out_step, out_step);
+            if (COUPLED) tile.request_rows(0, 3, L - hi, hi - lo, (const char*)p.x + in, in_step);
+            tile.rows_requested(0);
+        }
+        for (int k = 1; k < p.stages; ++k) request(base + k * stride, k);
     } else tile.apart = apart;
     auto get = [&](int stage, int k, int i) { return tile.get(stage, k, staged_rows(ACCESS) ? L - 1 - i : i); };
     if (blocks > 1) cluster_wait();
@@ -821,6 +864,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         if constexpr (staged_rows(ACCESS)) stage = tile.wait(broken);
         r.stage = stage;
         auto run = [&](auto full) {
+            if (staged_rows(ACCESS) && !full.value && lo > 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (a tile of rows; a copy goes there next)
             load(full, base);
 #pragma unroll
             for (int i = 0; i < L; ++i) {

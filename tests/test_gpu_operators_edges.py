@@ -1,4 +1,4 @@
-"""Sequence and residual operators on the GPU where float32 ends: gates whose slope is near the smallest normal number.
+"""Sequence and residual operators on the GPU at their edges: gates whose slope is near the smallest normal number, what lies behind the lengths.
 
 Tolerances as in test_gpu_operators.py."""
 import numpy as np
@@ -74,3 +74,31 @@ def test_residual_gradients_of_bfloat16_gates_far_below_zero(M, D):
     sig = orc.sigmoid(c["gate"])[0]
     for key, w in (("dscale", c["w_post"]), ("dw_post", c["scale"])):
         _close(_np(grads[key]), ref[key], (mag * np.abs(w) * ((4 * E + M * 2.0 ** -24) * sig + 2.0 ** -126)).sum(0), key)
+
+
+@pytest.mark.parametrize("B,T,D,low,layout", [(80, 300, 64, "bf16", "plain"), (75, 290, 72, "f32", "time"), (20, 700, 200, "f16", "half"), (300, 20, 64, "bf16", "plain"),
+                                              (2, 4500, 40, "f16", "plain"), (3, 3000, 328, "bf16", "time"), (2, 12000, 72, "f32", "half"), (3, 23000, 40, "f16", "plain")])
+@pytest.mark.parametrize("coupled", [True, False])
+def test_recurrence_uses_nothing_behind_the_lengths_where_tiles_are_copied(B, T, D, low, layout, coupled):
+    # Blocks by themselves and clusters: NaN behind the lengths changes no result, given outputs stay as they are there
+    torch, b, _ = _torch()
+    c = _recurrence_case(B, T, D, low, layout=layout)
+    lengths = [(T, 0, 1, T // 2, T - 1, T // 3 + 5, 16, 17)[s % 8] for s in range(B)][::-1]
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda:0")
+    kw = dict(y0=c["t_y0"], lengths=n, coupled=coupled)
+
+    def copied(t):
+        return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device).copy_(t)
+
+    y, yT = b.recurrence_forward(c["t_x"], c["t_gate"], **kw)
+    traj, dy = copied(c["t_x"]).copy_(y), copied(c["t_dy"])
+    ref = b.recurrence_backward(c["t_x"], c["t_gate"], traj, dy, dL_dyT=c["t_dyT"], **kw)
+    off = torch.arange(T, device="cuda:0")[None, :, None] >= n[:, None, None]
+    dirty = [copied(t).masked_fill_(off, float("nan")) for t in (c["t_x"], c["t_gate"], traj, dy)]
+    out = copied(c["t_x"]).fill_(7.0)
+    _, got = b.recurrence_forward(dirty[0], dirty[1], y=out, **kw)
+    assert torch.equal(got, yT) and torch.equal(out, torch.where(off, torch.full_like(y, 7.0), y))
+    dx, dg, flag = copied(out).fill_(5.0), copied(out).fill_(6.0), torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    _, _, dy0 = b.recurrence_backward(*dirty, dL_dyT=c["t_dyT"], dL_dx=dx, dL_dgate=dg, flag=flag, **kw)
+    assert torch.equal(dx, torch.where(off, torch.full_like(y, 5.0), ref[0])) and torch.equal(dg, torch.where(off, torch.full_like(y, 6.0), ref[1]))
+    assert torch.equal(dy0, ref[2]) and int(flag) == 0
