@@ -617,6 +617,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
             const int n = count(base);
             tile.template load<full.value>(0, g, in_at, in_step, 0, n);
             tile.template load<full.value>(1, x, in_at, in_step, 0, n);
+            if (alone) __syncwarp();                        // lanes behind the last channel have read before the others write results over these rows
             x += in_round; g += in_round;
             const int ahead = count(base + stride);
             const unsigned first = in_at - (q.col[0] - q.tile) * es;
@@ -713,6 +714,8 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
         for (char* to = (char*)p.out + (q.seq * p.out_seq + i * p.out_step + q.col[0]) * es; i < p.n_steps; i += n, to += apace) store_pair<T, ACCESS>(to, 0, apart, typename W::type{});
     }
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // nobody leaves while its shared memory may be written, and every block has read its y0
+    else if (alone) __syncwarp();                           // every lane, or warp, has read its y0
+    else __syncthreads();
     if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = COUPLED ? -carry[v] : carry[v];
@@ -822,6 +825,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
             if (p.dy != nullptr) tile.template load<F>(1, dy, out_at, 0u - out_step, lo, hi);
             tile.template load<F>(2, y, out_at, 0u - out_step, lo, before);
             if constexpr (COUPLED) tile.template load<F>(3, x, in_at, 0u - in_step, lo, hi);
+            if (alone) __syncwarp();                        // as in the forward pass
             x -= in_round; g -= in_round; y -= out_round; dy -= out_round;
             range(base + stride, lo, hi);
             const unsigned to_tile = (q.col[0] - q.tile) * es;
@@ -964,6 +968,8 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
     }
     warp_flag_or(p.flag, largest.nonfinite());
     if (blocks > 1) { cluster_arrive(); cluster_wait(); }   // as in the forward pass
+    else if (alone) __syncwarp();
+    else __syncthreads();
     if (!kScan && p.last != nullptr && q.slot == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.last[states + q.col[v]] = carry[v];

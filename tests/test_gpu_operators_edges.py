@@ -102,3 +102,24 @@ def test_recurrence_uses_nothing_behind_the_lengths_where_tiles_are_copied(B, T,
     _, _, dy0 = b.recurrence_backward(*dirty, dL_dyT=c["t_dyT"], dL_dx=dx, dL_dgate=dg, flag=flag, **kw)
     assert torch.equal(dx, torch.where(off, torch.full_like(y, 5.0), ref[0])) and torch.equal(dg, torch.where(off, torch.full_like(y, 6.0), ref[1]))
     assert torch.equal(dy0, ref[2]) and int(flag) == 0
+
+
+@pytest.mark.parametrize("T,D,low", [(9, 34, "bf16"), (9, 33, "f16"), (12, 35, "f32"), (20, 63, "bf16")])
+def test_recurrence_in_place_where_a_warp_runs_alone(T, D, low):
+    # So many sequences that each gets one warp, whose last lanes run its last channels again: results over x, gate, dL_dy and the states, with lengths and without
+    torch, b, _ = _torch()
+    B = 5000
+    rng = np.random.default_rng(4)
+    _, _, dt = _torch()
+    x, gate, dy = (_up(rng.normal(size=(B, T, D)), dt[low]) for _ in range(3))
+    y0, dyT = _up(rng.normal(size=(B, D))), _up(rng.normal(size=(B, D)))
+    for n in (None, torch.arange(B, dtype=torch.int32, device="cuda:0") % (T + 1)):
+        y, yT = b.recurrence_forward(x, gate, y0=y0, lengths=n)
+        ref = b.recurrence_backward(x, gate, y, dy, dL_dyT=dyT, y0=y0, lengths=n)
+        over, state = x.clone(), y0.clone()
+        b.recurrence_forward(over, gate, y0=state, lengths=n, y=over, yT=state)
+        off = torch.zeros_like(y, dtype=torch.bool) if n is None else torch.arange(T, device="cuda:0")[None, :, None] >= n[:, None, None]
+        assert torch.equal(over, torch.where(off, x, y)) and torch.equal(state, yT)
+        dx, dg, adjoint = dy.clone(), gate.clone(), dyT.clone()
+        b.recurrence_backward(x, dg, y, dx, dL_dyT=adjoint, y0=y0, lengths=n, dL_dx=dx, dL_dgate=dg, dL_dy0=adjoint)
+        assert torch.equal(dx, torch.where(off, dy, ref[0])) and torch.equal(dg, torch.where(off, gate, ref[1])) and torch.equal(adjoint, ref[2])
