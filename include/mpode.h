@@ -316,7 +316,8 @@ const char* mpode_operator_error(void);
  *                    grid's steps enter by adding log h_i to the gate;
  *     coupled == 0 : y_i = (1 - b_i) y_{i-1} + x_i.
  * The time loop of this linear equation runs as a scan in one pass over the data, split over the SMs where a batch has few channels.
- * The state is float32 and never rounded; what is stored is Q16(y_i).
+ * The state is float32 and never rounded; what is stored is Q16(y_i).  A state or adjoint that is infinite is handed on as it is where no step follows, and may become
+ * a NaN with the next step (inf - b inf).
  */
 typedef struct {
     mpode_dtype low;              /* x, gate, y and their cotangents */

@@ -119,6 +119,10 @@ template <typename T, bool SLOPE> __device__ __forceinline__ void negated_gate(c
     }
 }
 
+// -b of a step that does not exist, and 1 - A of the identity map, negative: s + kKeep s is s for every float32 number in one rounding, and infinity for an
+// infinite s, where 0 s would be a NaN
+constexpr float kKeep = 1.17549435e-38f;
+
 // One step of the state s, nb = -b.  The coupled forward pass runs on s = -y, where b x is taken away without a change of sign: s - b s - b x.
 template <bool COUPLED> __device__ __forceinline__ void step_forward(float (&s)[V], const float (&nb)[V], const float (&x)[V]) {
     float kept[V];
@@ -132,7 +136,7 @@ struct Map {
     float A[V], nC[V], u[V];
     __device__ __forceinline__ Map() {
 #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = 1.f; nC[v] = 0.f; u[v] = 0.f; }
+        for (int v = 0; v < V; ++v) { A[v] = 1.f; nC[v] = kKeep; u[v] = 0.f; }
     }
     __device__ __forceinline__ void decay(const float (&nb)[V]) {
         float one[V], left[V];
@@ -210,7 +214,7 @@ __device__ __forceinline__ void put(float (&t)[3][32 * V], const Affine& a) {
 __device__ __forceinline__ void exchange_begin(Exchange& ex, int warps, int blocks) {
     Affine id;
 #pragma unroll
-    for (int v = 0; v < V; ++v) { id.m[v] = id.u[v] = 0.f; id.k[v] = 1.f; }
+    for (int v = 0; v < V; ++v) { id.m[v] = kKeep; id.k[v] = 1.f; id.u[v] = 0.f; }
     for (int set = 0; set < 2; ++set) {
         for (int w = warps + threadIdx.y; w < kMaxWarps; w += warps) put(ex.warp[set][w], id);
         if (blocks > 1)
@@ -651,7 +655,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
                 negated_gate<T, false>(f, r.nb[i], none);
                 if (!full.value && i >= n) {                // a step that does not exist keeps the state
 #pragma unroll
-                    for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
+                    for (int v = 0; v < V; ++v) r.nb[i][v] = kKeep;
                 }
             }
             if (alone) return;
@@ -877,7 +881,7 @@ __global__ void __launch_bounds__(32 * (ACCESS == PIPED ? kPipedWarps + 1 : kMax
                 negated_gate<T, true>(f, r.nb[i], r.slope[i]);
                 if (!full.value && (i < lo || i >= hi)) {                                       // a step that does not exist keeps the adjoint
 #pragma unroll
-                    for (int v = 0; v < V; ++v) r.nb[i][v] = 0.f;
+                    for (int v = 0; v < V; ++v) r.nb[i][v] = kKeep;
                 }
             }
             if (alone) return;

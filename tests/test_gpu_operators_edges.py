@@ -1,4 +1,4 @@
-"""Sequence and residual operators on the GPU at their edges: gates whose slope is near the smallest normal number, what lies behind the lengths.
+"""Sequence and residual operators on the GPU at their edges: gates whose slope is near the smallest normal number, states that are infinite, what lies behind the lengths, results over inputs.
 
 Tolerances as in test_gpu_operators.py."""
 import numpy as np
@@ -123,3 +123,61 @@ def test_recurrence_in_place_where_a_warp_runs_alone(T, D, low):
         dx, dg, adjoint = dy.clone(), gate.clone(), dyT.clone()
         b.recurrence_backward(x, dg, y, dx, dL_dyT=adjoint, y0=y0, lengths=n, dL_dx=dx, dL_dgate=dg, dL_dy0=adjoint)
         assert torch.equal(dx, torch.where(off, dy, ref[0])) and torch.equal(dg, torch.where(off, gate, ref[1])) and torch.equal(adjoint, ref[2])
+
+
+# alone in a warp, several warps with single and paired accesses, tiles staged in shared memory, clusters, clusters with a scanning warp
+INF_SHAPES = [(3, 3, 48, "bf16"), (5, 9, 64, "bf16"), (5, 9, 33, "f32"), (4, 128, 64, "bf16"), (80, 300, 64, "bf16"), (80, 300, 64, "f32"), (1, 1100, 31, "f16"),
+              (2, 2600, 40, "f32"), (2, 4500, 40, "bf16"), (1, 24001, 64, "bf16"), (300, 20, 64, "bf16"), (5000, 20, 64, "bf16"), (5000, 20, 63, "f32")]
+
+
+def _ends(B, T):
+    """Lengths that end in the middle of a tile, at its edge and nowhere."""
+    return [(T, 0, 1, T // 2, T - 1, min(T, 8), min(T, 16), min(T, 17))[s % 8] for s in range(B)]
+
+
+@pytest.mark.parametrize("B,T,D,low", INF_SHAPES)
+@pytest.mark.parametrize("coupled", [True, False])
+def test_recurrence_hands_on_a_state_that_is_infinite(B, T, D, low, coupled):
+    # A state that becomes infinite with the last step is infinite in y and in yT, whatever runs behind it; with no step at all it is the initial state
+    torch, b, _ = _torch()
+    c = _recurrence_case(B, T, D, low)
+    c["t_gate"].clamp_(min=-5)                                    # b x is infinite for an infinite x
+    lengths = _ends(B, T)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda:0")
+    clean, cleanT = b.recurrence_forward(c["t_x"], c["t_gate"], y0=c["t_y0"], lengths=n, coupled=coupled)
+    x, y0, y_ref, T_ref = c["t_x"].clone(), c["t_y0"].clone(), clean.clone(), cleanT.clone()
+    for s, m in enumerate(lengths):
+        for channel, value in ((1, float("inf")), (D - 1, float("-inf"))):
+            if m > 0:
+                x[s, m - 1, channel] = value
+                y_ref[s, m - 1, channel] = value
+            else:
+                y0[s, channel] = value
+            T_ref[s, channel] = value
+    y, yT = b.recurrence_forward(x, c["t_gate"], y0=y0, lengths=n, coupled=coupled)
+    assert torch.equal(y, y_ref) and torch.equal(yT, T_ref)
+
+
+@pytest.mark.parametrize("B,T,D,low", INF_SHAPES)
+@pytest.mark.parametrize("coupled", [True, False])
+def test_recurrence_hands_back_an_adjoint_that_is_infinite(B, T, D, low, coupled):
+    # It reaches the last step of the sequence, where b times it is infinite, unchanged; with no step at all it is the adjoint of the initial state
+    torch, b, _ = _torch()
+    c = _recurrence_case(B, T, D, low)
+    c["t_gate"].clamp_(min=-5)
+    lengths = _ends(B, T)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda:0")
+    kw = dict(y0=c["t_y0"], lengths=n, coupled=coupled)
+    y, _ = b.recurrence_forward(c["t_x"], c["t_gate"], **kw)
+    clean = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=c["t_dyT"], **kw)
+    dyT = c["t_dyT"].clone()
+    dyT[:, 1], dyT[:, D - 1] = float("inf"), float("-inf")
+    dx, dg, dy0 = b.recurrence_backward(c["t_x"], c["t_gate"], y, c["t_dy"], dL_dyT=dyT, **kw)
+    for s, m in enumerate(lengths):
+        if m > 0:
+            assert float(dx[s, m - 1, 1]) == float("inf") and float(dx[s, m - 1, D - 1]) == float("-inf"), (s, m)
+        else:
+            assert torch.equal(dy0[s], dyT[s])
+    rest = [i for i in range(D) if i not in (1, D - 1)]
+    for got, ref in zip((dx, dg, dy0), clean):
+        assert torch.equal(got[..., rest], ref[..., rest])
