@@ -74,12 +74,11 @@ extern "C" mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long l
     const bool vec = width % 8 == 0 && !misaligned(x_dev, 16) && !misaligned(out_dev, 16) && (ld_x * es) % 16 == 0 && (ld_out * es) % 16 == 0;
     const long long blocks = (a.groups + 255) / 256, most = 148 * 16;
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-    with_low(low, [&](auto t) {
+    return operator_launched(with_low(low, [&](auto t) {
         using T = decltype(t);
-        if (vec && ld_x == width && ld_out == width) dropout_kernel<T, true, true><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-        else if (vec) dropout_kernel<T, true, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-        else dropout_kernel<T, false, false><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-        return cudaSuccess;
-    });
-    return operator_launched(cudaGetLastError(), "mpode_dropout");
+        const cudaStream_t st = (cudaStream_t)cuda_stream;
+        if (vec && ld_x == width && ld_out == width) return launch_grid(dropout_kernel<T, true, true>, grid, 256, st, a);
+        if (vec) return launch_grid(dropout_kernel<T, true, false>, grid, 256, st, a);
+        return launch_grid(dropout_kernel<T, false, false>, grid, 256, st, a);
+    }), "mpode_dropout");
 }

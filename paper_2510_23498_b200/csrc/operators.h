@@ -1,6 +1,8 @@
 // Internal interface of the operators that work without a context: the gated linear recurrence (recurrence.cu), the residual step with its
 // norms (residual.cu) and dropout (dropout.cu).  Their C entry points check the arguments and launch; nothing else of the library calls them.
 #pragma once
+#include <utility>
+
 #include "common.cuh"
 
 namespace mpode {
@@ -18,6 +20,15 @@ template <typename F> inline cudaError_t with_low(mpode_dtype dt, F&& f) {
     if (dt == MPODE_F32) return f(float{});
     if (dt == MPODE_BF16) return f(__nv_bfloat16{});
     return f(__half{});
+}
+
+// A launch with its own status.  (Behind <<<>>> only the thread's last error could be asked, which an earlier call may have left.)
+template <typename... P, typename... A> inline cudaError_t launch_grid(void (*kernel)(P...), unsigned grid, unsigned block, cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 
 // How many clusters of `blocks` blocks of this kernel the current device holds at once (0 when that cannot be told).  Clusters beyond that number would run

@@ -1078,9 +1078,8 @@ template <typename T, bool COUPLED, bool BACKWARD> cudaError_t run(const mpode_r
     constexpr int L = BACKWARD ? kBackwardSteps<T> : kForwardSteps<T>, N = BACKWARD ? (COUPLED ? 4 : 3) : 2;
     if (!BACKWARD && d.n_steps <= kFewSteps) {
         const unsigned grid = (unsigned)(((long long)d.n_seq * ((d.width + 1) / 2) + 127) / 128);
-        if (words_fit(d, a)) recurrence_steps_kernel<T, COUPLED, PAIRS><<<grid, 128, 0, st>>>(a);
-        else recurrence_steps_kernel<T, COUPLED, SINGLES><<<grid, 128, 0, st>>>(a);
-        return cudaGetLastError();
+        return words_fit(d, a) ? launch_grid(recurrence_steps_kernel<T, COUPLED, PAIRS>, grid, 128, st, a)
+                               : launch_grid(recurrence_steps_kernel<T, COUPLED, SINGLES>, grid, 128, st, a);
     }
     Shape s = shape_of(d, a, L, cluster_room);
     RecMaps maps;
