@@ -398,6 +398,20 @@ def _refuse(message: str):
     raise MpodeError(ERR_INVALID_ARG, message)
 
 
+def _int32(**sizes):
+    """Sizes that the C structures hold in 32 bits (ctypes would cut them off)."""
+    for name, n in sizes.items():
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise MpodeError(ERR_UNSUPPORTED, "%s %d does not fit 32 bits" % (name, n))
+
+
+def _site(n) -> int:
+    n = int(n)
+    if not -0x80000000 <= n <= 0xffffffff:
+        _refuse("site %d does not fit 32 bits" % n)
+    return n
+
+
 def _low_of(t) -> int:
     low = _LOW.get(t.dtype)
     if low is None:
@@ -458,6 +472,9 @@ def _like(t):
 def _sequences(x):
     if x.dim() != 3:
         _refuse("x has to be [n_seq, n_steps, width]")
+    n, steps, width = x.shape
+    if n > 0x7fffffff or steps > 0x7fffffff or width > 0x7fffffff:
+        _int32(n_seq=n, n_steps=steps, width=width)
     return x.shape
 
 
@@ -554,7 +571,8 @@ class ResidualStep:
     def __init__(self, width: int, low: str = "bf16", post_norm: str = "rms", pre_norm: str = "rms", eps: float = 1e-5, h: float = 1.0,
                  p: float = 0.0, site: int = 0):
         _, torch = _load()
-        self.width, self.p, self.h, self.eps, self.site = int(width), float(p), float(h), float(eps), int(site)
+        self.width, self.p, self.h, self.eps, self.site = int(width), float(p), float(h), float(eps), _site(site)
+        _int32(width=self.width)
         self.low, self.post_norm, self.pre_norm = DTYPES[low], NORMS[post_norm], NORMS[pre_norm]
         self.low_torch = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[low]
 
@@ -564,6 +582,8 @@ class ResidualStep:
     def _shape(self, y, w_post, scale, w_pre, rng):
         if y.dim() != 2 or y.shape[1] != self.width:
             _refuse("the state has to be [rows, %d]" % self.width)
+        if y.shape[0] > 0x7fffffff:
+            _int32(rows=y.shape[0])
         one, f32 = (self.width,), _torch.float32
         _expect("w_post", w_post, one, f32)
         _expect("scale", scale, one, f32)
@@ -599,6 +619,7 @@ class ResidualStep:
         f32, low = torch.float32, self.low_torch
         shape = self._shape(y_new, w_post, scale, w_pre, rng)
         rows = shape[0]
+        _int32(scale_exp=int(scale_exp))
         _expect("stats", stats, (rows, 4), f32)
         _expect("flag", flag, (1,), torch.int32)
         ld_y, ld_u, ld_gate = _rows("y_new", y_new, shape, f32), _rows("u", u, shape, low), _rows("gate", gate, shape, low)
@@ -645,7 +666,9 @@ def dropout(x, p: float, rng, site: int = 0, out=None, flag=None):
             _refuse("x and out have to be contiguous, or 2-D with their columns side by side")
         shape = (x.numel() // max(x.shape[-1], 1), x.shape[-1])
         ld_x = ld_out = shape[1]
+    if shape[1] > 0x7fffffff:
+        _int32(width=shape[1])
     _expect("rng", rng, (2,), torch.int64)
     _expect("flag", flag, (1,), torch.int32)
-    _run(lib.mpode_dropout, low, (x, rng, out, flag), (shape[0], shape[1], _ptr(x), ld_x, _ptr(out), ld_out, p, _ptr(rng), site, _ptr(flag)))
+    _run(lib.mpode_dropout, low, (x, rng, out, flag), (shape[0], shape[1], _ptr(x), ld_x, _ptr(out), ld_out, p, _ptr(rng), _site(site), _ptr(flag)))
     return out
