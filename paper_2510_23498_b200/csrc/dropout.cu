@@ -69,7 +69,7 @@ extern "C" mpode_status mpode_dropout(mpode_dtype low, void* cuda_stream, long l
     const size_t es = low_size(low);
     if (misaligned(x_dev, es) || misaligned(out_dev, es) || misaligned(rng_dev, 8) || misaligned(flag_dev, 4))
         return operator_fail(MPODE_ERR_INVALID_ARG, "mpode_dropout: a pointer is not aligned to its elements");
-    DropArgs a{x_dev, out_dev, ld_x, ld_out, 0, width, (width + 7) / 8, make_dropout(p, rng_dev, site), flag_dev};
+    DropArgs a{x_dev, out_dev, ld_x, ld_out, 0, width, width / 8 + (width % 8 != 0), make_dropout(p, rng_dev, site), flag_dev};
     a.groups = rows * a.groups_row;
     const bool vec = width % 8 == 0 && !misaligned(x_dev, 16) && !misaligned(out_dev, 16) && (ld_x * es) % 16 == 0 && (ld_out * es) % 16 == 0;
     const long long blocks = (a.groups + 255) / 256, most = 148 * 16;

@@ -52,7 +52,7 @@ ResShape shape_of(int rows, int width, int at_once) {
     s.warps = 1;
     while (s.warps * 256 < width && s.warps < kResWarps) s.warps *= 2;
     s.groups = s.warps == 1 ? kResGroups : 1;
-    const int need = (rows + s.groups - 1) / s.groups;
+    const int need = rows / s.groups + (rows % s.groups != 0);
     int most = at_once * (s.warps >= 8 || s.warps == 1 ? 1 : 8 / s.warps);
     most = most / s.blocks > 0 ? most / s.blocks : 1;
     s.clusters = need < most ? need : most;

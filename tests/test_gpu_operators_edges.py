@@ -181,3 +181,14 @@ def test_recurrence_hands_back_an_adjoint_that_is_infinite(B, T, D, low, coupled
     rest = [i for i in range(D) if i not in (1, D - 1)]
     for got, ref in zip((dx, dg, dy0), clean):
         assert torch.equal(got[..., rest], ref[..., rest])
+
+
+def test_dropout_of_one_row_of_two_to_the_31_columns_less_one():
+    # One row's groups are numbered like as many rows of eight columns
+    torch, b, _ = _torch()
+    n = (1 << 31) - 1
+    words = torch.tensor([5, 6], dtype=torch.int64, device="cuda:0")
+    row, eights = (torch.ones(n + 1, dtype=torch.bfloat16, device="cuda:0") for _ in range(2))
+    b.dropout(row[:n], 0.25, words, site=2, out=row[:n])
+    b.dropout(eights.view(-1, 8), 0.25, words, site=2, out=eights.view(-1, 8))
+    assert torch.equal(row[:n], eights[:n]) and float(row[n]) == 1

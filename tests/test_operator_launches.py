@@ -18,3 +18,21 @@ def test_a_call_answers_for_its_own_launch_alone(tmp_path):
         begin(); say(mpode_residual_forward(&r, nullptr, 8, (const float*)at(0), at(1), nullptr, nullptr, nullptr, nullptr, nullptr, (float*)to(2), to(3), nullptr));
     }""")
     assert out == ["0:1"] * 5 + ["4:1"] * 5
+
+
+def test_the_largest_sizes_have_grids(tmp_path):
+    # 2^31 - 1 columns or rows: rounding up to whole groups once left 32 bits, and the launch was refused
+    out = run(tmp_path, """
+    for (int width : {0x7fffffff, 0x7ffffff9, 0x7ffffff8}) {
+        launches = 0; grid = dim3(0);
+        const mpode_status s = mpode_dropout(MPODE_BF16, nullptr, 1, width, at(0), 0, to(1), 0, 0.5f, at(2), 0, nullptr);
+        printf("%d:%lld:%u ", (int)s, launches, grid.x);
+    }
+    for (int rows : {0x7fffffff, 0x7ffffff9, 0x7ffffff8}) {
+        launches = 0; grid = dim3(0);
+        mpode_residual_desc r{MPODE_BF16, 8, MPODE_NORM_RMS, MPODE_NORM_RMS, 1e-5f, 1.f, 0.f, 0, 0, 0, 0, 0};
+        const mpode_status s = mpode_residual_forward(&r, nullptr, rows, (const float*)at(0), at(1), nullptr, nullptr, nullptr, nullptr, nullptr, (float*)to(2), to(3), nullptr);
+        const size_t n = mpode_residual_workspace_bytes(&r, rows);
+        printf("%d:%lld:%d:%d ", (int)s, launches, grid.x >= 1 && grid.x <= 65536, n >= 64 && n <= (1u << 30));
+    }""")
+    assert out == ["0:1:2368"] * 3 + ["0:1:1:1"] * 3
