@@ -386,7 +386,7 @@ mpode_status mpode_residual_forward(const mpode_residual_desc* desc, void* cuda_
  * dL_dz_dev: NULL (zero) or low, the cotangent of z.  With the adjoint scale S = 2^scale_exp of Alg. 2 (-100 .. 100): dL_dz_dev is read as S times the
  * cotangent, dL_du_dev and dL_dgate_dev are written as Q16(S times theirs), everything in float32 is unscaled.  Out: dL_dy_dev fp32 (may be
  * dL_dy_new_dev), dL_du_dev low (may be u_dev), dL_dgate_dev low (may be gate_dev), and the weights' gradients fp32 [width], each NULL or overwritten (added to when
- * accumulate != 0).  Those need mpode_residual_workspace_bytes of device memory, 256-byte aligned, which holds nothing between calls; calls
+ * accumulate != 0, also where one buffer takes the gradients of weights that are shared).  Those need mpode_residual_workspace_bytes of device memory, 256-byte aligned, which holds nothing between calls; calls
  * that overlap on the GPU, captured graphs among them, need a workspace each.
  */
 size_t mpode_residual_workspace_bytes(const mpode_residual_desc* desc, int rows);

@@ -163,6 +163,9 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
     a.cot_in = ldexpf(1.f, -scale_exp); a.cot_out = ldexpf(1.f, scale_exp);
     a.flag = flag_dev;
     const bool weights = dL_dw_post_dev || dL_dscale_dev || dL_dw_pre_dev;
+    const auto meet = [&](const float* p, const float* q) { return p && q && p < q + desc->width && q < p + desc->width; };
+    const bool shared = meet(dL_dw_post_dev, dL_dscale_dev) || meet(dL_dw_post_dev, dL_dw_pre_dev) || meet(dL_dscale_dev, dL_dw_pre_dev);
+    if (shared && !accumulate) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: weight gradients in one another's place (they can be added there: accumulate)", who);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     int partials = 0;
     if (rows > 0) {
@@ -191,7 +194,17 @@ mpode_status mpode_residual_backward(const mpode_residual_desc* desc, void* cuda
     }
     if (!weights) return MPODE_OK;
     FinishArgs f{a.partial, w_post_dev, scale_dev, dL_dw_post_dev, dL_dscale_dev, dL_dw_pre_dev, partials, desc->width, accumulate};
-    return operator_launched(launch_chain(residual_finish_kernel, dim3((2 * desc->width + 7) / 8), dim3(512), 0, st, f), who);
+    const auto finish = [&] { return operator_launched(launch_chain(residual_finish_kernel, dim3((2 * desc->width + 7) / 8), dim3(512), 0, st, f), who); };
+    if (!shared) return finish();
+    // one sum after another into the buffer that they share
+    for (int k = 0; k < 3; ++k) {
+        f.dw_post = k == 0 ? dL_dw_post_dev : nullptr;
+        f.dscale = k == 1 ? dL_dscale_dev : nullptr;
+        f.dw_pre = k == 2 ? dL_dw_pre_dev : nullptr;
+        const mpode_status s = f.dw_post || f.dscale || f.dw_pre ? finish() : MPODE_OK;
+        if (s != MPODE_OK) return s;
+    }
+    return MPODE_OK;
 }
 
 }  // extern "C"

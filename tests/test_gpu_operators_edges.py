@@ -192,3 +192,25 @@ def test_dropout_of_one_row_of_two_to_the_31_columns_less_one():
     b.dropout(row[:n], 0.25, words, site=2, out=row[:n])
     b.dropout(eights.view(-1, 8), 0.25, words, site=2, out=eights.view(-1, 8))
     assert torch.equal(row[:n], eights[:n]) and float(row[n]) == 1
+
+
+@pytest.mark.parametrize("M,D", [(50, 96), (700, 2048), (40, 785), (30, 4096)])
+def test_residual_gradients_of_shared_weights_meet_in_one_buffer(M, D):
+    # One weight in two or three places: its gradients are added to one buffer, in the order dw_post, dscale, dw_pre, the same bits every time
+    torch, b, _ = _torch()
+    c = _residual_case(M, D, "bf16")
+    step = b.ResidualStep(D, low="bf16")
+    for names in (("dw_post", "dw_pre"), ("dw_post", "dscale"), ("dw_post", "dscale", "dw_pre")):
+        w = dict(gate=c["t_gate"], w_post=c["t_w_post"], scale=c["t_scale"], w_pre=c["t_w_pre"])
+        y, z, stats = step.forward(c["t_y"], c["t_u"], **w)
+        one = step.backward(y, c["t_u"], stats, dL_dy=c["t_dy"], dL_dz=c["t_dz"], **w)
+        buffer = torch.ones(D, device="cuda:0")
+        into = {k: buffer if k in names else torch.zeros(D, device="cuda:0") for k in ("dw_post", "dscale", "dw_pre")}
+        got = step.backward(y, c["t_u"], stats, dL_dy=c["t_dy"], dL_dz=c["t_dz"], accumulate_into=into, **w)
+        want = torch.ones(D, device="cuda:0")
+        for k in ("dw_post", "dscale", "dw_pre"):
+            if k in names:
+                want += one[k]
+            else:
+                assert torch.equal(got[k], one[k])
+        assert torch.equal(buffer, want)

@@ -36,3 +36,26 @@ def test_the_largest_sizes_have_grids(tmp_path):
         printf("%d:%lld:%d:%d ", (int)s, launches, grid.x >= 1 && grid.x <= 65536, n >= 64 && n <= (1u << 30));
     }""")
     assert out == ["0:1:2368"] * 3 + ["0:1:1:1"] * 3
+
+
+def test_weight_gradients_in_one_buffer_are_added_one_after_another(tmp_path):
+    # One kernel that writes them all would race where two of them lie over one another.  Overwriting one another has no meaning and is refused.
+    out = run(tmp_path, """
+    mpode_residual_desc r{MPODE_BF16, 64, MPODE_NORM_RMS, MPODE_NORM_RMS, 1e-5f, 1.f, 0.f, 0, 0, 0, 0, 0};
+    auto call = [&](int post, int scale, int pre, int off, int accumulate) {
+        launches = 0;
+        auto grad = [&](int i) { return i ? (float*)to(i) : nullptr; };
+        const mpode_status s = mpode_residual_backward(&r, nullptr, 8, (const float*)at(0), at(1), at(2), (const float*)at(3), (const float*)at(4), (const float*)at(5), nullptr,
+            (const float*)at(6), (const float*)at(7), at(8), 0, (float*)to(9), to(10), to(11), grad(post), grad(scale), pre ? grad(pre) + off : nullptr, accumulate, nullptr, to(20), 1 << 24);
+        printf("%d:%lld ", (int)s, launches);
+    };
+    for (int accumulate : {0, 1}) {
+        call(12, 13, 14, 0, accumulate);
+        call(12, 13, 12, 0, accumulate);
+        call(12, 12, 12, 0, accumulate);
+        call(0, 12, 12, 0, accumulate);
+        call(12, 0, 12, 63, accumulate);
+        call(12, 0, 12, 64, accumulate);
+        call(0, 0, 12, 0, accumulate);
+    }""")
+    assert out == ["0:2", "1:0", "1:0", "1:0", "1:0", "0:2", "0:2"] + ["0:2", "0:4", "0:4", "0:3", "0:3", "0:2", "0:2"]
