@@ -31,7 +31,7 @@ template <typename... P, typename... A> inline cudaError_t launch_grid(void (*ke
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 
-// How many clusters of `blocks` blocks of this kernel the current device holds at once (0 when that cannot be told).  Clusters beyond that number would run
+// How many clusters of `blocks` blocks of this kernel the current device holds at once (-1 when that cannot be told).  Clusters beyond that number would run
 // behind the others: the groups of SMs that a cluster has to fit into leave some of them idle.
 inline int clusters_at_once(const void* kernel, dim3 block, size_t smem, int blocks) {
     cudaLaunchConfig_t cfg{};
@@ -50,7 +50,7 @@ inline int clusters_at_once(const void* kernel, dim3 block, size_t smem, int blo
         cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess)
         return n;
     (void)cudaGetLastError();
-    return 0;
+    return -1;
 }
 
 }  // namespace mpode

@@ -1071,6 +1071,7 @@ int cluster_room(int blocks) {
     using T = __nv_bfloat16;
     constexpr int L = kForwardSteps<T>;
     n = clusters_at_once((const void*)recurrence_forward_kernel<T, true, L, PIPED>, dim3(32, kPipedWarps + 1), most_bytes<T, L, 2>(PIPED), blocks);
+    if (n < 0) return 0;                                    // (asked again by the next call)
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }

@@ -334,6 +334,7 @@ template <typename K> int room_of(std::atomic<int> (&known)[kMaxDevices][2][kRes
     int n = slot.load(std::memory_order_relaxed);
     if (n > 0) return n - 1;
     n = clusters_at_once((const void*)(wide ? kernel32 : kernel16), dim3(32 * kResWarps), wide ? smem32 : smem16, blocks);
+    if (n < 0) return 0;                                    // (asked again by the next call)
     slot.store(n + 1, std::memory_order_relaxed);
     return n;
 }

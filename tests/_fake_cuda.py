@@ -9,6 +9,7 @@ RUNTIME = r"""
 #include <string.h>
 #include "mpode.h"
 static cudaError_t stale = cudaSuccess, refuse = cudaSuccess;      // what an earlier call has left; what a launch answers
+static cudaError_t occupancy = cudaSuccess;                        // what the question for clusters answers
 static long long launches = 0;
 static dim3 grid;
 extern "C" {
@@ -21,7 +22,7 @@ cudaError_t __cudaPopCallConfiguration(dim3*, dim3*, size_t*, void*) { return cu
 cudaError_t cudaLaunchKernel(const void*, dim3 g, dim3, void**, size_t, cudaStream_t) { ++launches; grid = g; return refuse; }
 cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t* c, const void*, void**) { ++launches; grid = c->gridDim; return refuse; }
 cudaError_t cudaFuncSetAttribute(const void*, cudaFuncAttribute, int) { return cudaSuccess; }
-cudaError_t cudaOccupancyMaxActiveClusters(int* n, const void*, const cudaLaunchConfig_t*) { *n = 8; return cudaSuccess; }
+cudaError_t cudaOccupancyMaxActiveClusters(int* n, const void*, const cudaLaunchConfig_t*) { *n = 8; return occupancy; }
 cudaError_t cudaDeviceGetAttribute(int* v, cudaDeviceAttr, int) { *v = 148; return cudaSuccess; }
 cudaError_t cudaGetDevice(int* d) { *d = 0; return cudaSuccess; }
 cudaError_t cudaGetLastError() { const cudaError_t e = stale; stale = cudaSuccess; return e; }

@@ -59,3 +59,19 @@ def test_weight_gradients_in_one_buffer_are_added_one_after_another(tmp_path):
         call(0, 0, 12, 0, accumulate);
     }""")
     assert out == ["0:2", "1:0", "1:0", "1:0", "1:0", "0:2", "0:2"] + ["0:2", "0:4", "0:4", "0:3", "0:3", "0:2", "0:2"]
+
+
+def test_a_question_that_failed_is_asked_again(tmp_path):
+    # How many clusters the device holds: one call's failure to tell must not decide every later call's shape
+    out = run(tmp_path, """
+    mpode_recurrence_desc d{MPODE_BF16, 1, 5000, 64, 1, 0, 0, 0, 0, 0};
+    mpode_residual_desc r{MPODE_BF16, 8192, MPODE_NORM_RMS, MPODE_NORM_RMS, 1e-5f, 1.f, 0.f, 0, 0, 0, 0, 0};
+    for (int k = 0; k < 3; ++k) {
+        occupancy = k == 0 ? cudaErrorMemoryAllocation : cudaSuccess;
+        mpode_recurrence_forward(&d, nullptr, at(0), at(1), nullptr, nullptr, to(2), nullptr);
+        printf("%u ", grid.x);
+        mpode_residual_forward(&r, nullptr, 1000, (const float*)at(0), at(1), nullptr, nullptr, nullptr, nullptr, nullptr, (float*)to(2), to(3), nullptr);
+        printf("%u ", grid.x);
+    }""")
+    # one sequence of 64 channels: a block, or a cluster of 16; rows of four blocks: as many as the grid's limit holds, or the 8 clusters that fit
+    assert out == ["1", "592", "16", "32", "16", "32"]
