@@ -304,8 +304,12 @@ const char* mpode_last_error(const mpode_ctx* ctx);
  *   - Arguments are checked before anything is queued; mpode_operator_error returns the message of the last call of this host thread that failed.
  *   - The low format is that of the block's tensors; states, adjoints, statistics, weights and weight gradients are float32.  Results are
  *     rounded to the low format once, when written, and are the same bits in every run.
- *   - Strides count elements and 0 means contiguous; channels lie side by side.  Any element-aligned pointer is taken; rows that are multiples
- *     of 16 bytes (in the recurrence also of two elements) from pointers aligned like that are read and written in wider accesses.
+ *   - Between, float32 arithmetic.  Sigmoids, their slopes and reciprocal roots are within 2^-20 of their value (16-bit formats: the device's approximate power and
+ *     reciprocal, whose rounded argument adds |gate| 2^-24); a sigmoid below 2^-126 counts as zero.  Scaled cotangents are formed unscaled and then scaled: what
+ *     lies below 2^-126 in front of the scale is lost.
+ *   - Strides count elements and 0 means contiguous; channels lie side by side.  Any element-aligned pointer is taken; from pointers to 16-byte
+ *     boundaries, rows at distances that are multiples of 16 bytes are read and written in wider accesses: in the recurrence where the width is a multiple of 16 bytes too
+ *     (of two elements: pairs), in the residual step and in dropout where it is a multiple of 8 elements.
  *   - flag_dev (device word, or NULL) is set to 1 when a low-format value that was written is not finite, and left alone otherwise: the finiteness test of Alg. 2.
  */
 const char* mpode_operator_error(void);

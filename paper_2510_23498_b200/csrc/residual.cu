@@ -58,7 +58,9 @@ ResShape shape_of(int rows, int width, int at_once) {
     s.clusters = need < most ? need : most;
     return s;
 }
-constexpr int kForwardBlocks = 148 * 4, kBackwardBlocks = 148 * 3;      // blocks of 8 warps
+// Blocks of 8 warps: what an SM holds of 16-bit rows.  (Not everywhere: backward it holds two of float32 rows above 1024 columns, whose stages take 80 KB, and two of
+// eight rows of one warp, with 122 to 126 registers a thread; the third then runs behind them.)
+constexpr int kForwardBlocks = 148 * 4, kBackwardBlocks = 148 * 3;
 
 mpode_status check(const mpode_residual_desc* d, int rows, const char* who) {
     if (d == nullptr) return operator_fail(MPODE_ERR_INVALID_ARG, "%s: null descriptor", who);

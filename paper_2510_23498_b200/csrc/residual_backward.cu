@@ -6,8 +6,8 @@
 // where the last means are taken only with MEANVAR; dw_post = scale S and dscale = w_post S come from one sum over the rows, formed behind the last one.
 //
 // A row goes through three phases with a sum over the row between them.  Its inputs lie in shared memory and are read again in the next phase: what a
-// thread keeps of its eight columns are two gradients and two weights (32 registers) and one product, so that three blocks of 8 warps fit an SM and one's
-// sums are hidden behind another's arithmetic.
+// thread keeps of its eight columns are two gradients and two weights (32 registers) and one product, so that three blocks of 8 warps of 16-bit rows fit an SM
+// (two of float32 rows, by their stages) and one's sums are hidden behind another's arithmetic.
 #include "residual.cuh"
 
 namespace mpode {
